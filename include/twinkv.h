@@ -329,6 +329,163 @@ int twinkv_compact(const void* keys, const void* values, int dtype, int d, int n
                    int64_t workspace_bytes, void* stream);
 
 /*
+ * ---- The layer around the cache: what makes its keys, and what attends over it ----
+ *
+ * Rows of channels.  In the calls below q, k, v and their outputs are addressed like the keys above:
+ * element (head, token, c) at p[head*head_stride + token*token_stride + c], pointer and byte strides
+ * multiples of 16, so a projection's token-major output (head_stride = d, token_stride = heads*d) is
+ * taken as it is.  d is 64 or 128; bf16 or fp32, one type in a call.  `group` query heads share a KV
+ * head: query head h*group + g reads KV head h.  These are inference calls: none has a gradient.
+ */
+
+/*
+ * Per-head RMS norm of queries and keys and the rotary position embedding (the keys as the cache
+ * stores them, Sec. 3.2) in one pass.  With y = x * weight / sqrt(mean(x^2) + eps):
+ *   out[c]       = y[c] * cos[c] - y[c + d/2] * sin[c]
+ *   out[c + d/2] = y[c + d/2] * cos[c] + y[c] * sin[c],   c in [0, d/2).
+ *
+ *   q [n_q_heads][T][d], k [n_k_heads][T][d]; either may be NULL with 0 heads.  An output may be its
+ *             input (same pointer and strides); any other overlap is not allowed.
+ *   q_weight, k_weight  [d] fp32, 16-byte aligned.  Nullable, each: that side is not normalised (y = x).
+ *   eps       finite, >= 0.
+ *   rope      [n_pos][d] fp32, 16-byte aligned: cos for the d/2 channel pairs, then sin.  NULL: no
+ *             rotation (positions is then not read).
+ *   positions [T] int32: each token's row of the table.  A token whose position lies outside
+ *             [0, n_pos) gets NaN in its outputs (its cache then reports TWINKV_PROBLEM_NONFINITE).
+ * Everything is computed in fp32 and rounded once, to the output's type.
+ */
+int twinkv_qk_norm_rope(const void* q, const void* k, int dtype, int d, int n_q_heads, int n_k_heads,
+                        int64_t T, int64_t q_head_stride, int64_t q_token_stride,
+                        int64_t k_head_stride, int64_t k_token_stride, const float* q_weight,
+                        const float* k_weight, float eps, const float* rope, int64_t n_pos,
+                        const int32_t* positions, void* q_out, int64_t qo_head_stride,
+                        int64_t qo_token_stride, void* k_out, int64_t ko_head_stride,
+                        int64_t ko_token_stride, void* stream);
+
+/*
+ * Causal attention over a sliding window and the first tokens (sinks): the attention of a policy that
+ * keeps n_sink leading and `window` trailing tokens.  Sequence s has query tokens [cu_q[s], cu_q[s+1])
+ * and keys [cu_k[s], cu_k[s+1]); its queries are its last tokens: query i of m over n keys stands at
+ * position p = n - m + i and sees the keys j <= p with p - j < window or j < n_sink.
+ * A window >= n is plain causal attention; m = n a whole prompt, m = 1 a decode step.
+ *
+ *   out = softmax over the seen keys of (scale * q . k_j), times v_j.  A query that sees no key (window
+ *         and n_sink 0, or p < 0) gets 0.
+ *   lse   [n_heads*group][T_q] fp32: log of the sum of exp(scale * q . k_j); -inf where none is seen.
+ *         Nullable.
+ *   window, n_sink  >= 0.  scale finite.
+ *   workspace  twinkv_attention_workspace_bytes(...) bytes (may be NULL when that is 0).
+ * Scores, the running maximum and sums are fp32; for bf16 the weights are rounded to bf16 (to nearest)
+ * for the product with v.  A key or value that a query does not see never changes its result, NaN and
+ * infinities included.
+ */
+int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype, int d, int n_heads,
+                          int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k,
+                          int64_t q_head_stride, int64_t q_token_stride, int64_t k_head_stride,
+                          int64_t k_token_stride, int64_t v_head_stride, int64_t v_token_stride,
+                          int64_t window, int64_t n_sink, float scale, void* out,
+                          int64_t out_head_stride, int64_t out_token_stride, float* lse,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Bytes of workspace twinkv_sink_attention needs for this batch; negative (-TWINKV_E_*) on invalid
+ * arguments.  For twinkv_cache4_attention: cu_k = the cache's cu_rows, window = INT64_MAX, n_sink = 0.
+ */
+int64_t twinkv_attention_workspace_bytes(int dtype, int d, int n_heads, int group, int n_seqs,
+                                         const int64_t* cu_q, const int64_t* cu_k, int64_t window,
+                                         int64_t n_sink);
+
+/*
+ * A cache held in 4 bits.  Every 32 channels of a row share a scale 2^(byte - 127); an element is a
+ * sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6 (one sign, two exponent, one mantissa bit) times it:
+ * 17/32 byte an element.  With a the largest magnitude of the 32, the byte is the smallest in [1, 252]
+ * with a / scale < 7 (252 where none is); each element goes to the nearest value, ties to the even
+ * code, magnitudes above 6 to 6.  32 channels of which one is NaN or infinite are stored as zeros, and the
+ * problem reports TWINKV_PROBLEM_NONFINITE.
+ *
+ * Sequence s has rows [cu_rows[s], cu_rows[s+1]) of every head, a multiple of 32; how many of them are
+ * in use is a count per problem (h, s), kept by the caller on the device (lengths may differ from head
+ * to head).  C = cu_rows[n_seqs]; the four arrays are 16-byte aligned:
+ *   k_codes   [n_heads][C][d/2]: byte b of a row holds channel 2b (low nibble) and 2b + 1
+ *   k_scales  [n_heads][C][d/32]
+ *   v_codes   [n_heads][C/8][d][4]: 8 rows a block; byte b of a channel holds rows 2b (low) and 2b + 1;
+ *             place 64a + 4i + n holds channel 64a + 16n + i
+ *   v_scales  [n_heads][C/8][d/32][8]
+ * so that matrix operands are read 16 bytes a lane without reordering.  Unused rows may hold anything.
+ */
+typedef struct twinkv_cache4 {
+  int d;                   /* 64 or 128 */
+  int n_heads, n_seqs;
+  const int64_t* cu_rows;  /* (host) [n_seqs + 1], consumed before the call returns */
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+} twinkv_cache4;
+
+/* Bytes of workspace the three calls below need for n_seqs sequences (0 for small batches). */
+int64_t twinkv_cache4_workspace_bytes(int n_seqs);
+
+/*
+ * twinkv_compact into a 4-bit cache: the keys and values at the retained positions of every problem,
+ * in position order, as the first rows of its part of the cache.
+ *
+ *   keys, values  [n_heads][T][d] as in twinkv_compact; both required.  n_heads, n_seqs and d are the
+ *                 cache's.
+ *   retained      [n_heads][T] uint8, nonzero = keep.
+ *   pos_out       [n_heads][C] int32: the position in the sequence of each row's token; -1 on rows not
+ *                 in use.
+ *   len_out       [n_heads * n_seqs] int32: rows in use (0 when the problem keeps more positions than
+ *                 it has rows: TWINKV_PROBLEM_BUDGET_MISMATCH, nothing is stored).
+ *   status        [n_heads * n_seqs] int32 TWINKV_PROBLEM_*.
+ */
+int twinkv_cache4_compact(const void* keys, const void* values, int dtype, const int64_t* cu_seqlens,
+                          int64_t head_stride, int64_t token_stride, int64_t v_head_stride,
+                          int64_t v_token_stride, const uint8_t* retained, const twinkv_cache4* cache,
+                          int32_t* pos_out, int32_t* len_out, int32_t* status, void* workspace,
+                          int64_t workspace_bytes, void* stream);
+
+/*
+ * Appends the keys and values of new tokens: those of sequence s, [cu_new[s], cu_new[s+1]), become rows
+ * len .. of each of its problems.
+ *
+ *   len_in, len_out  [n_heads * n_seqs] int32: rows in use before and after.  May be the same array.
+ *                    A problem whose new tokens do not fit (or whose len_in is negative) is left as it
+ *                    is, len_out = len_in, with TWINKV_PROBLEM_BUDGET_MISMATCH.
+ *   status           [n_heads * n_seqs] int32 TWINKV_PROBLEM_*.
+ */
+int twinkv_cache4_append(const void* keys, const void* values, int dtype, const int64_t* cu_new,
+                         int64_t head_stride, int64_t token_stride, int64_t v_head_stride,
+                         int64_t v_token_stride, const twinkv_cache4* cache, const int32_t* len_in,
+                         int32_t* len_out, int32_t* status, void* workspace, int64_t workspace_bytes,
+                         void* stream);
+
+/*
+ * The values that rows of the cache stand for (exact in both types), for a second repair of a cache
+ * that has grown, or to move it: row r of sequence s in the output, r < cu_out[s+1] - cu_out[s], is
+ * cache row first + r of the problem; rows outside [0, len) are zeros.
+ *
+ *   first     [n_heads * n_seqs] int32; NULL: 0.
+ *   keys_out, values_out  [n_heads][cu_out[n_seqs]][d] dense, 16-byte aligned; either may be NULL.
+ */
+int twinkv_cache4_read(const twinkv_cache4* cache, const int32_t* len, const int32_t* first, int dtype,
+                       const int64_t* cu_out, void* keys_out, void* values_out, void* workspace,
+                       int64_t workspace_bytes, void* stream);
+
+/*
+ * Attention over a 4-bit cache: q [n_heads*group][T_q][d], the query tokens [cu_q[s], cu_q[s+1]) of
+ * sequence s being the last tokens of its cache: query i of m sees rows [0, len - (m - 1 - i)) of each
+ * problem (one query: all of them).  out and lse as in twinkv_sink_attention (0 and -inf where nothing
+ * is seen); q and out are `dtype`.  len is taken as at most the problem's rows.
+ * The products are exact in the cached values; scores and sums are fp32.
+ */
+int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* cu_q,
+                            int64_t q_head_stride, int64_t q_token_stride, const twinkv_cache4* cache,
+                            const int32_t* len, float scale, void* out, int64_t out_head_stride,
+                            int64_t out_token_stride, float* lse, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+
+/*
  * Profiling hook.  For calls made afterwards from the calling thread, record the given
  * hipEvent_t handles on the call's stream immediately before and immediately after the
  * launch of the call's main kernel -- the similarity kernel (the fused contraction +

@@ -57,6 +57,20 @@ SIGNATURES = {
     "twinkv_levels_workspace_bytes": (_I64, [_I, _I, _I, _I, _PI64, _I, _I]),
     "twinkv_compact": (_I, [_VP, _VP, _I, _I, _I, _I, _PI64, _I64, _I64, _I64, _I64, _VP, _PI64,
                             _VP, _VP, _VP, _VP, _VP, _I64, _VP]),
+    "twinkv_qk_norm_rope": (_I, [_VP, _VP, _I, _I, _I, _I, _I64, _I64, _I64, _I64, _I64, _VP, _VP, _F,
+                                 _VP, _I64, _VP, _VP, _I64, _I64, _VP, _I64, _I64, _VP]),
+    "twinkv_attention_workspace_bytes": (_I64, [_I, _I, _I, _I, _I, _PI64, _PI64, _I64, _I64]),
+    "twinkv_sink_attention": (_I, [_VP, _VP, _VP, _I, _I, _I, _I, _I, _PI64, _PI64, _I64, _I64, _I64,
+                                   _I64, _I64, _I64, _I64, _I64, _F, _VP, _I64, _I64, _VP, _VP, _I64,
+                                   _VP]),
+    "twinkv_cache4_workspace_bytes": (_I64, [_I]),
+    "twinkv_cache4_compact": (_I, [_VP, _VP, _I, _PI64, _I64, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP,
+                                   _VP, _I64, _VP]),
+    "twinkv_cache4_append": (_I, [_VP, _VP, _I, _PI64, _I64, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP,
+                                  _I64, _VP]),
+    "twinkv_cache4_read": (_I, [_VP, _VP, _VP, _I, _PI64, _VP, _VP, _VP, _I64, _VP]),
+    "twinkv_cache4_attention": (_I, [_VP, _I, _I, _PI64, _I64, _I64, _VP, _VP, _F, _VP, _I64, _I64, _VP,
+                                     _VP, _I64, _VP]),
     "twinkv_status_string": (ctypes.c_char_p, [_I]),
     "twinkv_version": (_I, []),
     "twinkv_profile_sim_events": (None, [_VP, _VP]),
@@ -613,3 +627,330 @@ def compact(keys, retained, capacity, values=None, cu_seqlens=None, *, want_pos:
         _ptr(out["values"]), _ptr(out["pos"]), out["stats"].data_ptr(), ws.data_ptr(), _nbytes(ws),
         _stream(dev))
     return {k: v for k, v in out.items() if v is not None}
+
+
+# ---------------------------------------------------------------- the layer around the cache
+
+def _i64_view(values) -> ctypes.Array:
+    """Host offsets as a C array over an int64 copy of them."""
+    arr = np.array(values, dtype=np.int64)
+    return (ctypes.c_int64 * len(arr)).from_buffer(arr)
+
+
+def _rows(x, name: str, dtype=None, d=None, dev=None):
+    """A (heads, T, d) tensor (or (T, d)) of a supported type, as the library addresses it: any head
+    and token strides of a multiple of 16 bytes, channels contiguous; others are copied.  Returns it with
+    its dtype code."""
+    torch = _torch()
+    if x.dim() == 2:
+        x = x.unsqueeze(0)
+    if x.dim() != 3:
+        raise ValueError(f"{name} must be (heads, T, d) or (T, d)")
+    if x.dtype == torch.bfloat16:
+        dt = TWINKV_BF16
+    elif x.dtype == torch.float32:
+        dt = TWINKV_F32
+    else:
+        raise ValueError(f"unsupported {name} dtype {x.dtype}")
+    if dtype is not None and x.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {x.dtype}")
+    if d is not None and x.shape[2] != d:
+        raise ValueError(f"{name} must have {d} channels, got {x.shape[2]}")
+    if dev is not None and x.device != dev:
+        raise ValueError(f"{name} must be on {dev}")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be on a GPU")
+    h, t, c = x.stride()
+    lanes = 16 // x.element_size()
+    if c != 1 or t % lanes or h % lanes or t < x.shape[2] or x.data_ptr() % 16:
+        x = x.clone(memory_format=torch.contiguous_format)
+    return x, dt
+
+
+def _out_rows(out, shape, like, name: str):
+    """The caller's output rows (written in place, so they must be addressable as they are), or new ones."""
+    torch = _torch()
+    if out is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device)
+    if tuple(out.shape) != tuple(shape) or out.dtype != like.dtype or out.device != like.device:
+        raise ValueError(f"{name} must be {tuple(shape)} {like.dtype} on {like.device}, got "
+                         f"{tuple(out.shape)} {out.dtype} on {out.device}")
+    h, t, c = out.stride()
+    lanes = 16 // out.element_size()
+    if c != 1 or t % lanes or h % lanes or t < shape[2] or out.data_ptr() % 16:
+        raise ValueError(f"{name} must have contiguous channels and strides of multiples of 16 bytes")
+    return out
+
+
+def _small(x, shape, dtype, dev, name: str):
+    """A contiguous, 16-byte aligned operand of one exact shape and type (None stays None)."""
+    if x is None:
+        return None
+    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or x.device != dev:
+        raise ValueError(f"{name} must be {tuple(shape)} {dtype} on {dev}, got {tuple(x.shape)} {x.dtype} on {x.device}")
+    x = x.contiguous()
+    return x if x.data_ptr() % 16 == 0 else x.clone()
+
+
+def _scratch(workspace, nbytes: int, dev, fn: str):
+    """(tensor, pointer, bytes) of a workspace; nothing where nothing is needed."""
+    if nbytes < 0:
+        raise TwinKVError(fn, -nbytes)
+    if nbytes == 0 and workspace is None:
+        return None, None, 0
+    ws = _workspace(workspace, nbytes, dev)
+    return ws, ws.data_ptr(), _nbytes(ws)
+
+
+def qk_norm_rope(q, k, q_weight=None, k_weight=None, eps: float = 1e-6, rope=None, positions=None, *,
+                 q_out=None, k_out=None) -> dict:
+    """RMS norm of each head of q (Hq, T, d) and k (Hk, T, d) (a weight (d,) float32 each; None: not
+    normalised) and the rotary embedding by ``rope`` (n_pos, d) float32 (cos of the d/2 pairs, then
+    sin; None: no rotation) at ``positions`` (T,) int32.  Channel c turns with c + d/2.  A projection's
+    token-major output goes in as its (H, T, d) view.  q or k may be None.  The outputs may be the
+    inputs."""
+    torch = _torch()
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("q or k is required")
+    given_q, given_k = q, k
+    dt = T = d = None
+    if q is not None:
+        q, dt = _rows(q, "q")
+        _, T, d = q.shape
+    if k is not None:
+        k, dt = _rows(k, "k", some.dtype, d, some.device)
+        if T is not None and k.shape[1] != T:
+            raise ValueError(f"k must have {T} tokens, got {k.shape[1]}")
+        _, T, d = k.shape
+    dev = some.device
+    f32 = torch.float32
+    q_weight = _small(q_weight, (d,), f32, dev, "q_weight")
+    k_weight = _small(k_weight, (d,), f32, dev, "k_weight")
+    if rope is not None:
+        if positions is None:
+            raise ValueError("positions is required with rope")
+        rope = _small(rope, (rope.shape[0], d), f32, dev, "rope")
+        positions = _small(positions, (T,), torch.int32, dev, "positions")
+    out = {}
+    args = {"q": (None, 0, 0, 0, None, 0, 0), "k": (None, 0, 0, 0, None, 0, 0)}
+    for name, x, given, to in (("q", q, given_q, q_out), ("k", k, given_k, k_out)):
+        if x is None:
+            continue
+        if to is not None and to.dim() == 2:
+            to = to.unsqueeze(0)
+        o = out[name] = _out_rows(to, x.shape, x, f"{name}_out")
+        args[name] = (x.data_ptr(), x.shape[0], x.stride(0), x.stride(1), o.data_ptr(), o.stride(0), o.stride(1))
+    qa, ka = args["q"], args["k"]
+    _launch(dev, "twinkv_qk_norm_rope", qa[0], ka[0], dt, d, qa[1], ka[1], T, qa[2], qa[3], ka[2], ka[3],
+            _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(rope), 0 if rope is None else rope.shape[0],
+            None if rope is None else positions.data_ptr(), qa[4], qa[5], qa[6], ka[4], ka[5], ka[6], _stream(dev))
+    return out
+
+
+def attention_workspace_bytes(dtype: int, d: int, n_heads: int, group: int, cu_q, cu_k, window: int,
+                              n_sink: int) -> int:
+    cq, ck = _i64_view(cu_q), _i64_view(cu_k)
+    n = int(lib().twinkv_attention_workspace_bytes(dtype, d, n_heads, group, len(cq) - 1, cq, ck, int(window),
+                                                   int(n_sink)))
+    if n < 0:
+        raise TwinKVError("twinkv_attention_workspace_bytes", -n)
+    return n
+
+
+def _group(n_q: int, n_heads: int) -> int:
+    if n_heads == 0 or n_q % n_heads or n_q == 0:
+        raise ValueError(f"{n_q} query heads do not divide over {n_heads} KV heads")
+    return n_q // n_heads
+
+
+def sink_attention(q, k, v, window: int, n_sink: int = 4, scale: Optional[float] = None, cu_q=None, cu_k=None,
+                   *, want_lse: bool = False, out=None, workspace=None) -> dict:
+    """Causal attention over a sliding window and the first ``n_sink`` tokens.  q (Hq, Tq, d) are the
+    last tokens of each sequence, k and v (H, Tk, d) all of its tokens; query head h reads KV head
+    h // (Hq // H).  A query at position p sees j <= p with p - j < window or j < n_sink.  scale defaults to
+    1 / sqrt(d).  Returns out, and lse (Hq, Tq) float32 with ``want_lse``."""
+    torch = _torch()
+    q, dt = _rows(q, "q")
+    Hq, Tq, d = q.shape
+    dev = q.device
+    k, _ = _rows(k, "k", q.dtype, d, dev)
+    v, _ = _rows(v, "v", q.dtype, d, dev)
+    H, Tk, _ = k.shape
+    if tuple(v.shape) != (H, Tk, d):
+        raise ValueError("v must match k in shape")
+    group = _group(Hq, H)
+    cq, ck = _i64_view(_cu(cu_q, Tq)), _i64_view(_cu(cu_k, Tk))
+    n_seqs = len(cq) - 1
+    if len(ck) - 1 != n_seqs:
+        raise ValueError("cu_q and cu_k must list the same number of sequences")
+    if window < 0 or n_sink < 0:
+        raise ValueError("window and n_sink must not be negative")
+    res = {"out": _out_rows(out, (Hq, Tq, d), q, "out")}
+    if want_lse:
+        res["lse"] = torch.empty((Hq, Tq), dtype=torch.float32, device=dev)
+    o = res["out"]
+    window, n_sink = min(int(window), 1 << 62), min(int(n_sink), 1 << 62)
+    nb = lib().twinkv_attention_workspace_bytes(dt, d, H, group, n_seqs, cq, ck, window, n_sink)
+    ws, wp, wn = _scratch(workspace, int(nb), dev, "twinkv_attention_workspace_bytes")
+    _launch(dev, "twinkv_sink_attention", q.data_ptr(), k.data_ptr(), v.data_ptr(), dt, d, H, group, n_seqs, cq, ck,
+            q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1), window, n_sink,
+            float(d ** -0.5 if scale is None else scale), o.data_ptr(), o.stride(0), o.stride(1),
+            _ptr(res.get("lse")), wp, wn, _stream(dev))
+    return res
+
+
+class _Cache4Struct(ctypes.Structure):
+    _fields_ = [("d", _I), ("n_heads", _I), ("n_seqs", _I), ("cu_rows", _PI64), ("k_codes", _VP),
+                ("k_scales", _VP), ("v_codes", _VP), ("v_scales", _VP)]
+
+
+class Cache4:
+    """A cache held in 4 bits (layout in include/twinkv.h): sequence s has the rows
+    [cu_rows[s], cu_rows[s + 1]) of every head, a multiple of 32.  Takes the four arrays as they are;
+    ``Cache4.empty`` reserves them.  How many rows a problem uses is a separate int32 tensor
+    (n_heads, n_seqs), which cache4_compact and cache4_append return."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, cu_rows):
+        torch = _torch()
+        cu = np.array(cu_rows, dtype=np.int64)
+        if cu.ndim != 1 or len(cu) < 2 or cu[0] != 0 or np.any(np.diff(cu) < 0) or np.any(cu % 32):
+            raise ValueError("cu_rows must start at 0, never decrease, and be multiples of 32")
+        if k_codes.dim() != 3:
+            raise ValueError("k_codes must be (n_heads, C, d / 2)")
+        H, C, d = k_codes.shape[0], int(cu[-1]), 2 * k_codes.shape[2]
+        dev = k_codes.device
+        for name, x, shape in (("k_codes", k_codes, (H, C, d // 2)), ("k_scales", k_scales, (H, C, d // 32)),
+                               ("v_codes", v_codes, (H, C // 8, d, 4)), ("v_scales", v_scales, (H, C // 8, d // 32, 8))):
+            if tuple(x.shape) != shape or x.dtype != torch.uint8 or x.device != dev or not x.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous uint8 {shape} tensor on {dev}, got {tuple(x.shape)} {x.dtype}")
+        if not k_codes.is_cuda:
+            raise ValueError("the cache must be on a GPU")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.cu_rows, self.n_heads, self.n_seqs, self.d, self.device = cu, H, len(cu) - 1, d, dev
+        self._cu = (ctypes.c_int64 * len(cu)).from_buffer(cu)
+        self._struct = _Cache4Struct(d, H, len(cu) - 1, ctypes.cast(self._cu, _PI64), k_codes.data_ptr(),
+                                     k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
+        self._handle = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, n_heads: int, capacity, d: int, device="cuda"):
+        """Reserves ``capacity[s]`` rows for sequence s of every head, each rounded up to 32."""
+        torch = _torch()
+        cu = np.concatenate([[0], np.cumsum([(int(c) + 31) // 32 * 32 for c in np.atleast_1d(capacity)])])
+        C = int(cu[-1])
+        return cls(*(torch.empty(shape, dtype=torch.uint8, device=device) for shape in (
+            (n_heads, C, d // 2), (n_heads, C, d // 32), (n_heads, C // 8, d, 4), (n_heads, C // 8, d // 32, 8))), cu)
+
+    def _lens(self, x, name: str):
+        return _small(x, (self.n_heads, self.n_seqs), _torch().int32, self.device, name)
+
+    def _offsets(self, cu, T: int, name: str):
+        cu = _cu(cu, T)
+        if len(cu) - 1 != self.n_seqs:
+            raise ValueError(f"{name} must list the cache's {self.n_seqs} sequences")
+        return _i64_view(cu)
+
+
+def _cache4_rows(keys, values, cache: Cache4):
+    keys, dt = _rows(keys, "keys", None, cache.d, cache.device)
+    values, _ = _rows(values, "values", keys.dtype, cache.d, cache.device)
+    if keys.shape[0] != cache.n_heads or values.shape != keys.shape:
+        raise ValueError(f"keys and values must be ({cache.n_heads}, T, {cache.d})")
+    return keys, values, dt
+
+
+def _cache4_scratch(workspace, cache: Cache4):
+    return _scratch(workspace, int(lib().twinkv_cache4_workspace_bytes(cache.n_seqs)), cache.device,
+                    "twinkv_cache4_workspace_bytes")
+
+
+def cache4_compact(keys, values, retained, cache: Cache4, cu_seqlens=None, *, workspace=None) -> dict:
+    """``compact`` into a 4-bit cache: the keys and values (n_heads, T, d) at the retained positions of
+    every problem become the first rows of its part of ``cache``.  Returns len (n_heads, n_seqs) int32, pos
+    (n_heads, C) int32 (-1 on rows not in use) and status (n_heads, n_seqs) int32; a problem that keeps more
+    than its rows stores nothing (PROBLEM_BUDGET_MISMATCH, len 0)."""
+    torch = _torch()
+    keys, values, dt = _cache4_rows(keys, values, cache)
+    H, T, _ = keys.shape
+    dev = cache.device
+    cu = cache._offsets(cu_seqlens, T, "cu_seqlens")
+    if retained is None:
+        raise ValueError("retained is required")
+    ret = _mask(retained, H, T, dev, "retained")
+    out = {"len": torch.empty((H, cache.n_seqs), dtype=torch.int32, device=dev),
+           "pos": torch.empty((H, int(cache.cu_rows[-1])), dtype=torch.int32, device=dev),
+           "status": torch.empty((H, cache.n_seqs), dtype=torch.int32, device=dev)}
+    ws, wp, wn = _cache4_scratch(workspace, cache)
+    _launch(dev, "twinkv_cache4_compact", keys.data_ptr(), values.data_ptr(), dt, cu, keys.stride(0), keys.stride(1),
+            values.stride(0), values.stride(1), ret.data_ptr(), cache._handle, out["pos"].data_ptr(),
+            out["len"].data_ptr(), out["status"].data_ptr(), wp, wn, _stream(dev))
+    return out
+
+
+def cache4_append(keys, values, cache: Cache4, length, cu_new=None, *, len_out=None, workspace=None) -> dict:
+    """The keys and values (n_heads, T, d) of new tokens, [cu_new[s], cu_new[s + 1]) of sequence s, as the
+    rows after the ``length`` (n_heads, n_seqs) int32 ones in use.  Returns len (``len_out`` if given, which
+    may be ``length`` itself) and status; a problem whose new tokens do not fit stays as it is."""
+    torch = _torch()
+    keys, values, dt = _cache4_rows(keys, values, cache)
+    dev = cache.device
+    cu = cache._offsets(cu_new, keys.shape[1], "cu_new")
+    n_in = cache._lens(length, "length")
+    if len_out is None:
+        len_out = torch.empty((cache.n_heads, cache.n_seqs), dtype=torch.int32, device=dev)
+    elif cache._lens(len_out, "len_out").data_ptr() != len_out.data_ptr():
+        raise ValueError("len_out must be contiguous and 16-byte aligned")
+    status = torch.empty((cache.n_heads, cache.n_seqs), dtype=torch.int32, device=dev)
+    ws, wp, wn = _cache4_scratch(workspace, cache)
+    _launch(dev, "twinkv_cache4_append", keys.data_ptr(), values.data_ptr(), dt, cu, keys.stride(0), keys.stride(1),
+            values.stride(0), values.stride(1), cache._handle, n_in.data_ptr(), len_out.data_ptr(),
+            status.data_ptr(), wp, wn, _stream(dev))
+    return {"len": len_out, "status": status}
+
+
+def cache4_read(cache: Cache4, length, dtype, first=None, cu_out=None, *, want_keys: bool = True,
+                want_values: bool = True, workspace=None) -> dict:
+    """The values that cached rows stand for, in ``dtype``: keys and values (n_heads, cu_out[-1], d), row
+    r of sequence s being cache row first + r (``first`` (n_heads, n_seqs) int32, default 0; ``cu_out``
+    defaults to all of the cache's rows).  Rows that are not in use are zeros."""
+    torch = _torch()
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"unsupported dtype {dtype}")
+    dev = cache.device
+    cu = np.asarray(cache.cu_rows if cu_out is None else cu_out, dtype=np.int64)
+    cu = cache._offsets(cu, int(cu[-1]) if cu.ndim == 1 and len(cu) else 0, "cu_out")
+    n = cache._lens(length, "length")
+    f = cache._lens(first, "first")
+    shape = (cache.n_heads, int(cu[-1]), cache.d)
+    out = {name: torch.empty(shape, dtype=dtype, device=dev)
+           for name, want in (("keys", want_keys), ("values", want_values)) if want}
+    ws, wp, wn = _cache4_scratch(workspace, cache)
+    _launch(dev, "twinkv_cache4_read", cache._handle, n.data_ptr(), _ptr(f),
+            TWINKV_BF16 if dtype == torch.bfloat16 else TWINKV_F32, cu, _ptr(out.get("keys")), _ptr(out.get("values")),
+            wp, wn, _stream(dev))
+    return out
+
+
+def cache4_attention(q, cache: Cache4, length, scale: Optional[float] = None, cu_q=None, *,
+                     want_lse: bool = False, out=None, workspace=None) -> dict:
+    """Attention of q (Hq, Tq, d), the last tokens [cu_q[s], cu_q[s + 1]) of each cached sequence, over the
+    ``length`` (n_heads, n_seqs) int32 rows in use: query i of m sees the first length - (m - 1 - i) of
+    them.  scale defaults to 1 / sqrt(d).  Returns out, and lse (Hq, Tq) float32 with ``want_lse``."""
+    torch = _torch()
+    dev = cache.device
+    q, dt = _rows(q, "q", None, cache.d, dev)
+    Hq, Tq, d = q.shape
+    group = _group(Hq, cache.n_heads)
+    cq = cache._offsets(cu_q, Tq, "cu_q")
+    n = cache._lens(length, "length")
+    res = {"out": _out_rows(out, (Hq, Tq, d), q, "out")}
+    if want_lse:
+        res["lse"] = torch.empty((Hq, Tq), dtype=torch.float32, device=dev)
+    o = res["out"]
+    nb = lib().twinkv_attention_workspace_bytes(dt, d, cache.n_heads, group, cache.n_seqs, cq, cache._cu, 1 << 62, 0)
+    ws, wp, wn = _scratch(workspace, int(nb), dev, "twinkv_attention_workspace_bytes")
+    _launch(dev, "twinkv_cache4_attention", q.data_ptr(), dt, group, cq, q.stride(0), q.stride(1), cache._handle,
+            n.data_ptr(), float(d ** -0.5 if scale is None else scale), o.data_ptr(), o.stride(0), o.stride(1),
+            _ptr(res.get("lse")), wp, wn, _stream(dev))
+    return res

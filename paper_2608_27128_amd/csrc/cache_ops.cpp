@@ -1,0 +1,491 @@
+// Host layer of the operators around the cache (include/twinkv.h): argument validation, the
+// per-sequence words, the split of the attention's keys, and the kernel launches (K6 norm and rotation,
+// K7 4-bit cache, K8 / K9 attention).  Nothing here allocates.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "cache_ops.h"
+#include "twinkv.h"
+#include "twinkv_internal.h"
+
+namespace twinkv {
+namespace {
+
+constexpr int64_t kMaxTokens = kAttnMaxKeys;  // of a batch: token indices are 32-bit inside the kernels
+constexpr int kMaxHeads = 65535;              // a grid's second dimension
+constexpr size_t kAlign = 256;
+
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+char* aligned_base(void* ws) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(ws);
+  return reinterpret_cast<char*>((p + kAlign - 1) / kAlign * kAlign);
+}
+
+int hip_status(int e) { return e == 0 ? TWINKV_OK : TWINKV_E_HIP; }
+
+// A launch of `blocks` workgroups of `threads`: a grid dimension's threads are counted in 32 bits.
+bool grid_ok(int64_t blocks, int threads) { return blocks * threads <= (int64_t)UINT32_MAX; }
+
+int check_type(int dtype, int d) {
+  return (dtype != TWINKV_BF16 && dtype != TWINKV_F32) || (d != 64 && d != 128) ? TWINKV_E_UNSUPPORTED : TWINKV_OK;
+}
+
+int check_cu(int n_seqs, const int64_t* cu) {
+  if (cu == nullptr) return TWINKV_E_NULL;
+  if (n_seqs < 1 || cu[0] != 0) return TWINKV_E_ARG;
+  for (int s = 0; s < n_seqs; ++s)
+    if (cu[s + 1] < cu[s]) return TWINKV_E_ARG;
+  return cu[n_seqs] > kMaxTokens ? TWINKV_E_ARG : TWINKV_OK;
+}
+
+// Rows of d channels at strides (elements); a pointer may be null where there is nothing to address.
+int check_rows(const void* p, int dtype, int d, int64_t head_stride, int64_t token_stride, bool empty) {
+  if (p == nullptr) return empty ? TWINKV_OK : TWINKV_E_NULL;
+  const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
+  if (token_stride < d || head_stride < 0) return TWINKV_E_ARG;
+  if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return TWINKV_E_ARG;
+  return token_stride * esz % 16 != 0 || head_stride * esz % 16 != 0 ? TWINKV_E_ARG : TWINKV_OK;
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Collects a call's per-sequence words: into the kernel arguments, or piece by piece into the workspace.
+class WordWriter {
+ public:
+  WordWriter(SeqWords& to, int64_t n_words, void* far, void* stream)
+      : to_(to), far_(n_words > kTabWords ? static_cast<int32_t*>(far) : nullptr), stream_(stream) {
+    to_.far = far_;
+  }
+  void put(int32_t w) {
+    if (n_ == kTabWords) flush();
+    to_.near[n_++] = w;
+  }
+  int finish() {
+    if (far_ != nullptr && n_ > 0) flush();
+    return error_;
+  }
+
+ private:
+  void flush() {
+    if (error_ == 0) error_ = launch_upload(to_.near, 4 * (size_t)n_, far_ + done_, stream_);
+    done_ += n_;
+    n_ = 0;
+  }
+  SeqWords& to_;
+  int32_t* far_;
+  void* stream_;
+  int n_ = 0, error_ = 0;
+  int64_t done_ = 0;
+};
+
+size_t words_bytes(int n_seqs, int per_seq) {
+  const int64_t n = ((int64_t)n_seqs + 1) * per_seq;
+  return n > kTabWords ? align_up(4 * (size_t)n) : 0;
+}
+
+// ---- the 4-bit cache ----
+
+int check_cache(const twinkv_cache4* c) {
+  if (c == nullptr) return TWINKV_E_NULL;
+  if (c->d != 64 && c->d != 128) return TWINKV_E_UNSUPPORTED;
+  if (c->n_heads < 1 || c->n_heads > kMaxHeads) return TWINKV_E_ARG;
+  const int rc = check_cu(c->n_seqs, c->cu_rows);
+  if (rc != TWINKV_OK) return rc;
+  if ((int64_t)c->n_heads * c->n_seqs > (int64_t)INT32_MAX / 4) return TWINKV_E_ARG;
+  for (int s = 0; s < c->n_seqs; ++s)
+    if (c->cu_rows[s + 1] % kCacheTile != 0) return TWINKV_E_ARG;
+  if (c->cu_rows[c->n_seqs] > 0 && (c->k_codes == nullptr || c->k_scales == nullptr || c->v_codes == nullptr ||
+                                    c->v_scales == nullptr))
+    return TWINKV_E_NULL;
+  if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales))
+    return TWINKV_E_ARG;
+  return TWINKV_OK;
+}
+
+Cache4 device_cache(const twinkv_cache4* c) {
+  return Cache4{static_cast<uint8_t*>(c->k_codes), static_cast<uint8_t*>(c->k_scales), static_cast<uint8_t*>(c->v_codes),
+                static_cast<uint8_t*>(c->v_scales), c->cu_rows[c->n_seqs]};
+}
+
+// Blocks of 8 cache rows that n rows touch, at any first row.
+int64_t blocks_of(int64_t n, bool aligned) {
+  return n == 0 ? 0 : (n + (aligned ? kCacheBlock - 1 : 2 * kCacheBlock - 2)) / kCacheBlock;
+}
+
+enum class Blocks { kCache, kTokens };  // every row of the cache, or the rows the call's tokens take
+
+// The words and the block list of a call whose token offsets are cu.
+int cache_words(const twinkv_cache4* c, const int64_t* cu, Blocks which, Cache4Args& a, void* workspace,
+                int64_t workspace_bytes, void* stream) {
+  int64_t blocks = 0;
+  for (int s = 0; s < c->n_seqs; ++s)
+    blocks += which == Blocks::kCache ? blocks_of(c->cu_rows[s + 1] - c->cu_rows[s], true)
+                                      : blocks_of(cu[s + 1] - cu[s], false);
+  if (!grid_ok(blocks, 64) || !grid_ok((int64_t)c->n_heads * c->n_seqs, 1024)) return TWINKV_E_ARG;
+  const size_t need = words_bytes(c->n_seqs, kCacheSeqWords);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < (int64_t)(need + kAlign))) return TWINKV_E_WORKSPACE;
+  WordWriter w(a.seq, ((int64_t)c->n_seqs + 1) * kCacheSeqWords, need > 0 ? aligned_base(workspace) : nullptr, stream);
+  int64_t at = 0;
+  for (int s = 0; s <= c->n_seqs; ++s) {
+    w.put((int32_t)cu[s]);
+    w.put((int32_t)c->cu_rows[s]);
+    w.put((int32_t)at);
+    if (s < c->n_seqs)
+      at += which == Blocks::kCache ? blocks_of(c->cu_rows[s + 1] - c->cu_rows[s], true)
+                                    : blocks_of(cu[s + 1] - cu[s], false);
+  }
+  a.cache = device_cache(c);
+  a.n_heads = c->n_heads;
+  a.n_seqs = c->n_seqs;
+  a.n_blocks = (int)blocks;
+  return hip_status(w.finish());
+}
+
+void set_rows(Cache4Args& a, const void* keys, const void* values, int dtype, int64_t head_stride,
+              int64_t token_stride, int64_t v_head_stride, int64_t v_token_stride) {
+  const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
+  a.keys = static_cast<const char*>(keys);
+  a.values = static_cast<const char*>(values);
+  a.head_stride = head_stride * esz;
+  a.token_stride = token_stride * esz;
+  a.v_head_stride = v_head_stride * esz;
+  a.v_token_stride = v_token_stride * esz;
+}
+
+// ---- attention ----
+
+// How a call's rows and keys are cut into items (attn.hip, attn4.hip).
+struct AttnPlan {
+  int64_t window = 0, n_sink = 0;
+  int split_tiles = 0;
+  int64_t items = 0, parts = 0;  // per head
+};
+
+int64_t row_tiles(int64_t nq, int group) { return (nq * group + kAttnRows - 1) / kAttnRows; }
+
+// The most key tiles a row tile of the sequence goes through.
+int64_t key_tiles(int64_t nq, int64_t nk, int group, const AttnPlan& p) {
+  const int64_t queries = std::min<int64_t>(nq, kAttnRows / group + 2);
+  const int64_t near = std::min(nk, p.window + queries), sinks = std::min(nk, p.n_sink);
+  const int64_t apart = (near + kAttnTile - 1) / kAttnTile + (sinks + kAttnTile - 1) / kAttnTile;
+  return std::min(apart, (nk + kAttnTile - 1) / kAttnTile) + 1;
+}
+
+int64_t splits_of(int64_t tiles, int split_tiles) {
+  return std::max<int64_t>(1, (tiles + split_tiles - 1) / split_tiles);
+}
+
+// Items go to workgroups of 4 waves; the whole work is cut into about kItems of them, a split no shorter than
+// two tiles a wave.
+constexpr int64_t kItems = 1024;
+
+int attn_plan(int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
+              int64_t n_sink, AttnPlan& p) {
+  p.window = std::min<int64_t>(window, kAttnMaxKeys);
+  p.n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
+  int64_t work = 0;  // key tiles, over all heads
+  for (int s = 0; s < n_seqs; ++s) {
+    const int64_t nq = cu_q[s + 1] - cu_q[s];
+    work += n_heads * row_tiles(nq, group) * key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p);
+  }
+  const int64_t each = std::max<int64_t>(8, (work + kItems - 1) / kItems);
+  p.split_tiles = (int)std::min<int64_t>((each + 3) / 4 * 4, kAttnMaxKeys / 64);
+  for (int s = 0; s < n_seqs; ++s) {
+    const int64_t nq = cu_q[s + 1] - cu_q[s];
+    const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
+    p.items += row_tiles(nq, group) * splits;
+    if (splits > 1) p.parts += row_tiles(nq, group) * splits;
+  }
+  return grid_ok(p.items, 256) ? TWINKV_OK : TWINKV_E_ARG;
+}
+
+struct AttnLayout {
+  size_t words = 0, part_o = 0, part_ml = 0, total = 0;
+};
+AttnLayout attn_layout(const AttnPlan& p, int d, int n_heads, int n_seqs) {
+  AttnLayout L;
+  size_t off = words_bytes(n_seqs, kAttnSeqWords);
+  const size_t rows = (size_t)n_heads * (size_t)p.parts * kAttnRows;
+  L.part_o = off;
+  off = align_up(off + 4 * rows * (size_t)d);
+  L.part_ml = off;
+  off = align_up(off + 8 * rows);
+  L.total = off > 0 ? off + kAlign : 0;
+  return L;
+}
+
+int check_heads(int n_heads, int group) {
+  return n_heads < 1 || n_heads > kMaxHeads || group < 1 || (int64_t)n_heads * group > (int64_t)INT32_MAX / 4
+             ? TWINKV_E_ARG : TWINKV_OK;
+}
+
+// Rows are numbered in 32 bits inside a sequence.
+int check_queries(int n_seqs, const int64_t* cu_q, int group) {
+  for (int s = 0; s < n_seqs; ++s)
+    if ((cu_q[s + 1] - cu_q[s]) * group > kMaxTokens) return TWINKV_E_ARG;
+  return TWINKV_OK;
+}
+
+// The queries' and outputs' side of a call, the plan, the words and the parts.
+int attn_args(const void* q, int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q,
+              const int64_t* cu_k, int64_t q_head_stride, int64_t q_token_stride, int64_t window, int64_t n_sink,
+              float scale, void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse,
+              void* workspace, int64_t workspace_bytes, void* stream, AttnArgs& a) {
+  AttnPlan p;
+  int rc = attn_plan(n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+  if (rc != TWINKV_OK) return rc;
+  const AttnLayout L = attn_layout(p, d, n_heads, n_seqs);
+  if (L.total > 0 && (workspace == nullptr || workspace_bytes < (int64_t)L.total)) return TWINKV_E_WORKSPACE;
+  char* ws = L.total > 0 ? aligned_base(workspace) : nullptr;
+  const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
+  a.q = static_cast<const char*>(q);
+  a.k = nullptr;
+  a.v = nullptr;
+  a.out = static_cast<char*>(out);
+  a.q_head = q_head_stride * esz;
+  a.q_token = q_token_stride * esz;
+  a.k_head = a.k_token = a.v_head = a.v_token = 0;
+  a.o_head = out_head_stride * esz;
+  a.o_token = out_token_stride * esz;
+  a.cache = Cache4{nullptr, nullptr, nullptr, nullptr, 0};
+  a.len = nullptr;
+  a.lse = lse;
+  a.Tq = cu_q[n_seqs];
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634074);
+  a.window = (int)p.window;
+  a.n_sink = (int)p.n_sink;
+  a.n_heads = n_heads;
+  a.group = group;
+  a.n_seqs = n_seqs;
+  a.items = (int)p.items;
+  a.parts = (int)p.parts;
+  a.split_tiles = p.split_tiles;
+  a.part_o = reinterpret_cast<float*>(ws + L.part_o);
+  a.part_ml = reinterpret_cast<float*>(ws + L.part_ml);
+  WordWriter w(a.seq, ((int64_t)n_seqs + 1) * kAttnSeqWords, ws, stream);
+  int64_t item = 0, part = 0;
+  for (int s = 0; s <= n_seqs; ++s) {
+    int64_t splits = 1, tiles = 0;
+    if (s < n_seqs) {
+      const int64_t nq = cu_q[s + 1] - cu_q[s];
+      tiles = row_tiles(nq, group);
+      splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
+    }
+    w.put((int32_t)cu_q[s]);
+    w.put((int32_t)cu_k[s]);
+    w.put((int32_t)item);
+    w.put((int32_t)splits);
+    w.put((int32_t)part);
+    item += tiles * splits;
+    if (splits > 1) part += tiles * splits;
+  }
+  return hip_status(w.finish());
+}
+
+}  // namespace
+}  // namespace twinkv
+
+using namespace twinkv;
+
+extern "C" {
+
+int twinkv_qk_norm_rope(const void* q, const void* k, int dtype, int d, int n_q_heads, int n_k_heads, int64_t T,
+                        int64_t q_head_stride, int64_t q_token_stride, int64_t k_head_stride,
+                        int64_t k_token_stride, const float* q_weight, const float* k_weight, float eps,
+                        const float* rope, int64_t n_pos, const int32_t* positions, void* q_out,
+                        int64_t qo_head_stride, int64_t qo_token_stride, void* k_out, int64_t ko_head_stride,
+                        int64_t ko_token_stride, void* stream) {
+  int rc = check_type(dtype, d);
+  if (rc != TWINKV_OK) return rc;
+  if (n_q_heads < 0 || n_k_heads < 0 || T < 0 || T > kMaxTokens) return TWINKV_E_ARG;
+  if ((int64_t)n_q_heads + n_k_heads > kMaxHeads) return TWINKV_E_ARG;
+  if (!std::isfinite(eps) || eps < 0.0f) return TWINKV_E_ARG;
+  const bool no_q = n_q_heads == 0 || T == 0, no_k = n_k_heads == 0 || T == 0;
+  if ((rc = check_rows(q, dtype, d, q_head_stride, q_token_stride, no_q)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(q_out, dtype, d, qo_head_stride, qo_token_stride, no_q)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(k, dtype, d, k_head_stride, k_token_stride, no_k)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(k_out, dtype, d, ko_head_stride, ko_token_stride, no_k)) != TWINKV_OK) return rc;
+  if (!aligned16(q_weight) || !aligned16(k_weight) || !aligned16(rope)) return TWINKV_E_ARG;
+  if (rope != nullptr) {
+    if (n_pos < 0) return TWINKV_E_ARG;
+    if (positions == nullptr && T > 0) return TWINKV_E_NULL;
+  }
+  if (no_q && no_k) return TWINKV_OK;
+  if (!grid_ok((T + 31) / 32, 256)) return TWINKV_E_ARG;
+  const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
+  NormRopeArgs a;
+  // heads a unit of lanes goes through with its token's cos and sin: as many as leave units for every
+  // SIMD of the machine (about 16000 rows of lanes)
+  const int64_t rows = T * ((int64_t)n_q_heads + n_k_heads);
+  a.per_unit = (int)std::min<int64_t>(std::max<int64_t>(rows / 16384, 1), 8);
+  auto side = [&](const void* in, void* out, int64_t ih, int64_t it, int64_t oh, int64_t ot, const float* weight,
+                  int heads) {
+    return NormRopeSide{static_cast<const char*>(in), static_cast<char*>(out), ih * esz, it * esz, oh * esz, ot * esz,
+                        weight, heads, (heads + a.per_unit - 1) / a.per_unit};
+  };
+  a.q = side(q, q_out, q_head_stride, q_token_stride, qo_head_stride, qo_token_stride, q_weight, n_q_heads);
+  a.k = side(k, k_out, k_head_stride, k_token_stride, ko_head_stride, ko_token_stride, k_weight, n_k_heads);
+  a.T = T;
+  a.n_pos = n_pos;
+  a.rope = rope;
+  a.pos = positions;
+  a.eps = eps;
+  return hip_status(launch_norm_rope(a, dtype, d, stream));
+}
+
+int64_t twinkv_attention_workspace_bytes(int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q,
+                                         const int64_t* cu_k, int64_t window, int64_t n_sink) {
+  int rc = check_type(dtype, d);
+  if (rc == TWINKV_OK) rc = check_heads(n_heads, group);
+  if (rc == TWINKV_OK) rc = check_cu(n_seqs, cu_q);
+  if (rc == TWINKV_OK) rc = check_cu(n_seqs, cu_k);
+  if (rc == TWINKV_OK) rc = check_queries(n_seqs, cu_q, group);
+  if (rc == TWINKV_OK && (window < 0 || n_sink < 0)) rc = TWINKV_E_ARG;
+  if (rc != TWINKV_OK) return -rc;
+  AttnPlan p;
+  rc = attn_plan(n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+  return rc != TWINKV_OK ? -rc : (int64_t)attn_layout(p, d, n_heads, n_seqs).total;
+}
+
+int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype, int d, int n_heads, int group,
+                          int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t q_head_stride,
+                          int64_t q_token_stride, int64_t k_head_stride, int64_t k_token_stride,
+                          int64_t v_head_stride, int64_t v_token_stride, int64_t window, int64_t n_sink, float scale,
+                          void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse, void* workspace,
+                          int64_t workspace_bytes, void* stream) {
+  int rc = check_type(dtype, d);
+  if (rc != TWINKV_OK) return rc;
+  if ((rc = check_heads(n_heads, group)) != TWINKV_OK) return rc;
+  if ((rc = check_cu(n_seqs, cu_q)) != TWINKV_OK) return rc;
+  if ((rc = check_cu(n_seqs, cu_k)) != TWINKV_OK) return rc;
+  if ((rc = check_queries(n_seqs, cu_q, group)) != TWINKV_OK) return rc;
+  if (window < 0 || n_sink < 0 || !std::isfinite(scale)) return TWINKV_E_ARG;
+  const bool no_q = cu_q[n_seqs] == 0, no_k = cu_k[n_seqs] == 0;
+  if ((rc = check_rows(q, dtype, d, q_head_stride, q_token_stride, no_q)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(out, dtype, d, out_head_stride, out_token_stride, no_q)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(k, dtype, d, k_head_stride, k_token_stride, no_k)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(v, dtype, d, v_head_stride, v_token_stride, no_k)) != TWINKV_OK) return rc;
+  if (no_q) return TWINKV_OK;
+  AttnArgs a;
+  rc = attn_args(q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride, window, n_sink, scale,
+                 out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
+  if (rc != TWINKV_OK) return rc;
+  const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
+  a.k = static_cast<const char*>(k);
+  a.v = static_cast<const char*>(v);
+  a.k_head = k_head_stride * esz;
+  a.k_token = k_token_stride * esz;
+  a.v_head = v_head_stride * esz;
+  a.v_token = v_token_stride * esz;
+  const int e = launch_attn(a, dtype, d, stream);
+  if (e != 0 || a.parts == 0) return hip_status(e);
+  return hip_status(launch_attn_join(a, dtype, d, stream));
+}
+
+int64_t twinkv_cache4_workspace_bytes(int n_seqs) {
+  if (n_seqs < 1) return -TWINKV_E_ARG;
+  const size_t n = words_bytes(n_seqs, kCacheSeqWords);
+  return n > 0 ? (int64_t)(n + kAlign) : 0;
+}
+
+int twinkv_cache4_compact(const void* keys, const void* values, int dtype, const int64_t* cu_seqlens,
+                          int64_t head_stride, int64_t token_stride, int64_t v_head_stride, int64_t v_token_stride,
+                          const uint8_t* retained, const twinkv_cache4* cache, int32_t* pos_out, int32_t* len_out,
+                          int32_t* status, void* workspace, int64_t workspace_bytes, void* stream) {
+  int rc = check_cache(cache);
+  if (rc != TWINKV_OK) return rc;
+  if ((rc = check_type(dtype, cache->d)) != TWINKV_OK) return rc;
+  if ((rc = check_cu(cache->n_seqs, cu_seqlens)) != TWINKV_OK) return rc;
+  const int64_t T = cu_seqlens[cache->n_seqs], C = cache->cu_rows[cache->n_seqs];
+  if ((rc = check_rows(keys, dtype, cache->d, head_stride, token_stride, T == 0)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(values, dtype, cache->d, v_head_stride, v_token_stride, T == 0)) != TWINKV_OK) return rc;
+  if ((retained == nullptr && T > 0) || (pos_out == nullptr && C > 0) || len_out == nullptr || status == nullptr)
+    return TWINKV_E_NULL;
+  Cache4Args a = {};
+  rc = cache_words(cache, cu_seqlens, Blocks::kCache, a, workspace, workspace_bytes, stream);
+  if (rc != TWINKV_OK) return rc;
+  set_rows(a, keys, values, dtype, head_stride, token_stride, v_head_stride, v_token_stride);
+  a.retained = retained;
+  a.T = T;
+  a.pos = pos_out;
+  a.len_out = len_out;
+  a.status = status;
+  if (launch_cache4_positions(a, stream) != 0) return TWINKV_E_HIP;
+  return hip_status(launch_cache4_gather(a, dtype, cache->d, stream));
+}
+
+int twinkv_cache4_append(const void* keys, const void* values, int dtype, const int64_t* cu_new, int64_t head_stride,
+                         int64_t token_stride, int64_t v_head_stride, int64_t v_token_stride,
+                         const twinkv_cache4* cache, const int32_t* len_in, int32_t* len_out, int32_t* status,
+                         void* workspace, int64_t workspace_bytes, void* stream) {
+  int rc = check_cache(cache);
+  if (rc != TWINKV_OK) return rc;
+  if ((rc = check_type(dtype, cache->d)) != TWINKV_OK) return rc;
+  if ((rc = check_cu(cache->n_seqs, cu_new)) != TWINKV_OK) return rc;
+  const bool none = cu_new[cache->n_seqs] == 0;
+  if ((rc = check_rows(keys, dtype, cache->d, head_stride, token_stride, none)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(values, dtype, cache->d, v_head_stride, v_token_stride, none)) != TWINKV_OK) return rc;
+  if (len_in == nullptr || len_out == nullptr || status == nullptr) return TWINKV_E_NULL;
+  Cache4Args a = {};
+  rc = cache_words(cache, cu_new, Blocks::kTokens, a, workspace, workspace_bytes, stream);
+  if (rc != TWINKV_OK) return rc;
+  set_rows(a, keys, values, dtype, head_stride, token_stride, v_head_stride, v_token_stride);
+  a.len_in = len_in;
+  a.len_out = len_out;
+  a.status = status;
+  int64_t most = 0;
+  for (int s = 0; s < cache->n_seqs; ++s) most = std::max(most, cu_new[s + 1] - cu_new[s]);
+  return hip_status(launch_cache4_append(a, (int)std::max<int64_t>(most, 1), dtype, cache->d, stream));
+}
+
+int twinkv_cache4_read(const twinkv_cache4* cache, const int32_t* len, const int32_t* first, int dtype,
+                       const int64_t* cu_out, void* keys_out, void* values_out, void* workspace,
+                       int64_t workspace_bytes, void* stream) {
+  int rc = check_cache(cache);
+  if (rc != TWINKV_OK) return rc;
+  if ((rc = check_type(dtype, cache->d)) != TWINKV_OK) return rc;
+  if ((rc = check_cu(cache->n_seqs, cu_out)) != TWINKV_OK) return rc;
+  if (len == nullptr) return TWINKV_E_NULL;
+  if (!aligned16(keys_out) || !aligned16(values_out)) return TWINKV_E_ARG;
+  Cache4Args a = {};
+  rc = cache_words(cache, cu_out, Blocks::kTokens, a, workspace, workspace_bytes, stream);
+  if (rc != TWINKV_OK) return rc;
+  a.len_in = len;
+  a.first = first;
+  a.keys_out = static_cast<char*>(keys_out);
+  a.values_out = static_cast<char*>(values_out);
+  a.C_out = cu_out[cache->n_seqs];
+  return hip_status(launch_cache4_read(a, dtype, cache->d, stream));
+}
+
+int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* cu_q, int64_t q_head_stride,
+                            int64_t q_token_stride, const twinkv_cache4* cache, const int32_t* len, float scale,
+                            void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse, void* workspace,
+                            int64_t workspace_bytes, void* stream) {
+  int rc = check_cache(cache);
+  if (rc != TWINKV_OK) return rc;
+  const int d = cache->d, n_seqs = cache->n_seqs;
+  if ((rc = check_type(dtype, d)) != TWINKV_OK) return rc;
+  if ((rc = check_heads(cache->n_heads, group)) != TWINKV_OK) return rc;
+  if ((rc = check_cu(n_seqs, cu_q)) != TWINKV_OK) return rc;
+  if ((rc = check_queries(n_seqs, cu_q, group)) != TWINKV_OK) return rc;
+  if (!std::isfinite(scale)) return TWINKV_E_ARG;
+  const bool no_q = cu_q[n_seqs] == 0;
+  if ((rc = check_rows(q, dtype, d, q_head_stride, q_token_stride, no_q)) != TWINKV_OK) return rc;
+  if ((rc = check_rows(out, dtype, d, out_head_stride, out_token_stride, no_q)) != TWINKV_OK) return rc;
+  if (len == nullptr) return TWINKV_E_NULL;
+  if (no_q) return TWINKV_OK;
+  AttnArgs a;
+  rc = attn_args(q, dtype, d, cache->n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride,
+                 INT64_MAX, 0, scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
+  if (rc != TWINKV_OK) return rc;
+  a.cache = device_cache(cache);
+  a.len = len;
+  const int e = launch_attn4(a, dtype, d, stream);
+  if (e != 0 || a.parts == 0) return hip_status(e);
+  return hip_status(launch_attn_join(a, dtype, d, stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,238 @@
+// K8: attention over the 4-bit cache, and the join of split rows (for K9 too).
+//
+// Few rows (the query heads of a KV head, times the new tokens) meet all cached rows, so the cache is
+// what has to be read: HBM-bound, as long as the unpacking stays cheap.  Four waves share a tile of 16 rows and
+// take 32 cached rows at a time each:
+//  * scores: K q^T on v_mfma_f32_16x16x32_bf16.  A lane converts 8 codes in 4 instructions, with their
+//    scale (v_cvt_scalef32_pk_bf16_fp4; a code times a power of two is exact in bf16).  The channels are
+//    dealt to the lane groups in runs of d/4, so that a lane's codes of a row are one 16-byte load and
+//    share one scale; the order of a contraction is free as long as q has the same.
+//  * the product with the values: the scale of a value belongs to its row, a contraction place, so it
+//    multiplies the weights instead (one product of 16 rows x 32 keys per group of 32 channels; a power
+//    of two, so the weight's rounding to bf16 is the only one).
+//  * fp32 queries: q and the scaled weights as sums of three bf16 (24 bits), three products each.
+// The keys are split over workgroups when there are too few problems for the machine (attn_split.h).
+#include <hip/hip_runtime.h>
+
+#include "attn_split.h"
+
+namespace twinkv {
+namespace {
+
+template <typename T>
+constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+
+__device__ inline bf16x8 codes8(unsigned w, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// x as a sum of N bf16, the largest first.
+template <int N>
+__device__ inline void split8(const float (&x)[8], bf16x8 (&p)[N]) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[n][e] = (bf16)r[e];
+      r[e] -= (float)p[n][e];
+    }
+  }
+}
+
+// One wave's 32 rows of the cache in registers.
+template <int D>
+struct Tile4 {
+  u32x4 k[2];          // d 64: words 0, 1
+  unsigned ks[2];
+  u32x4 v[D / 64];
+  u32x4 vs[D / 64];    // [d/32] groups of 8 bytes
+  __device__ void load(const Cache4& c, int64_t row, int i, int g) {  // row: of the cache, a multiple of 32
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int64_t r = row + 8 * (i >> 2) + 4 * m + (i & 3);
+      if constexpr (D == 128) {
+        k[m] = *reinterpret_cast<const u32x4*>(c.k_codes + r * 64 + g * 16);
+        ks[m] = c.k_scales[r * 4 + g];
+      } else {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(c.k_codes + r * 32 + g * 8);
+        k[m] = u32x4{w[0], w[1], 0u, 0u};
+        ks[m] = c.k_scales[r * 2 + (g >> 1)];
+      }
+    }
+    const int64_t b = row / kCacheBlock + g;
+#pragma unroll
+    for (int a = 0; a < D / 64; ++a) {
+      v[a] = *reinterpret_cast<const u32x4*>(c.v_codes + (b * D + a * 64 + i * 4) * 4);
+      vs[a] = *reinterpret_cast<const u32x4*>(c.v_scales + b * (D / 4) + a * 16);
+    }
+  }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kAttnWaves) void attn4_kernel(const AttnArgs a) {
+  constexpr int kSteps = D / 32;
+  constexpr int N = kParts<T>;
+  __shared__ float s_join[join_floats<D>()];
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const AttnItem p = attn_item(a, (int)blockIdx.x, (int)blockIdx.y);
+  const int len = min(max(a.len[(int64_t)p.h * a.n_seqs + p.s], 0), p.nk);
+  const int n_rows = p.nq * a.group, row0 = p.rt * kAttnRows;
+  const int last = min(row0 + kAttnRows, n_rows) - 1;
+  // rows past the problem's are computed as if they saw everything, and not written
+  const int row = min(row0 + i, n_rows - 1);
+  const int query = row / a.group;
+  const int lim = len - (p.nq - 1 - query);
+  const int lim_all = len - (p.nq - 1 - row0 / a.group);      // every row sees so many
+  const int lim_any = len - (p.nq - 1 - last / a.group);      // no row sees more
+  const int t0 = p.split * a.split_tiles * kAttnTile;
+  const int t1 = min(lim_any, t0 + a.split_tiles * kAttnTile);
+
+  bf16x8 q[N][kSteps];
+  {
+    const int64_t head = (int64_t)p.h * a.group + (row - query * a.group);
+    const char* src = a.q + head * a.q_head + (int64_t)(p.q0 + query) * a.q_token;
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      float x[8];
+      Vec8<T>::load(src + (g * (D / 4) + j * 8) * (int)sizeof(T)).to(x);
+      bf16x8 parts[N];
+      split8<N>(x, parts);
+#pragma unroll
+      for (int n = 0; n < N; ++n) q[n][j] = parts[n];
+    }
+  }
+  Cache4 c = a.cache;
+  c.k_codes += (int64_t)p.h * c.C * (D / 2);
+  c.k_scales += (int64_t)p.h * c.C * (D / 32);
+  c.v_codes += (int64_t)p.h * c.C * (D / 2);
+  c.v_scales += (int64_t)p.h * c.C * (D / 32);
+
+  RowStats st;
+  f32x4 acc[D / 16];
+#pragma unroll
+  for (int n = 0; n < D / 16; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr int kStep = kAttnTile * kAttnWaves;
+  Tile4<D> next;
+  const int first = t0 + wave * kAttnTile;
+  if (first < t1) next.load(c, p.k0 + first, i, g);
+  for (int t = first; t < t1; t += kStep) {
+    Tile4<D> now = next;
+    if (t + kStep < t1) next.load(c, p.k0 + t + kStep, i, g);
+
+    float s[8];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float scale = __uint_as_float(now.ks[m] << 23);
+      f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        const bf16x8 k = codes8(now.k[m][j], scale);
+#pragma unroll
+        for (int n = N - 1; n >= 0; --n) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[n][j], d, 0, 0, 0);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[4 * m + r] = d[r] * a.scale_log2;
+    }
+    if (t + kAttnTile > lim_all) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (t + 8 * g + e >= lim) s[e] = kNegInf;
+      if (t + kAttnTile > len) {  // rows not in use: their scales may be anything
+        const int use = min(max(len - (t + 8 * g), 0), 8);
+        const unsigned lo = use >= 4 ? ~0u : (1u << (8 * use)) - 1u;
+        const unsigned hi = use >= 8 ? ~0u : use <= 4 ? 0u : (1u << (8 * (use - 4))) - 1u;
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) now.vs[x] = u32x4{now.vs[x][0] & lo, now.vs[x][1] & hi, now.vs[x][2] & lo, now.vs[x][3] & hi};
+      }
+    }
+    st.update(s, acc);
+#pragma unroll
+    for (int grp = 0; grp < D / 32; ++grp) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const unsigned w = now.vs[grp >> 1][(grp & 1) * 2 + (e >> 2)];
+        x[e] = s[e] * __uint_as_float(((w >> (8 * (e & 3))) & 255u) << 23);
+      }
+      bf16x8 w[N];
+      split8<N>(x, w);
+#pragma unroll
+      for (int b = 2 * grp; b < 2 * grp + 2; ++b) {
+        const bf16x8 v = codes8(now.v[b >> 2][b & 3], 1.0f);
+#pragma unroll
+        for (int n = N - 1; n >= 0; --n) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], v, acc[b], 0, 0, 0);
+      }
+    }
+  }
+  join_waves<T, D>(a, p, row0, st, acc, s_join, [](int n, int lane16) { return n * 16 + lane16; });
+}
+
+// The join: for each row tile with splits, the parts' sums brought to one maximum.
+template <typename T, int D>
+__global__ __launch_bounds__(kAttnRows* D / 8) void attn_join_kernel(const AttnArgs a) {
+  const AttnItem p = attn_item(a, (int)blockIdx.x, (int)blockIdx.y);
+  const int splits = p.splits;
+  if (p.split != 0 || splits <= 1) return;
+  const int r = threadIdx.x / (D / 8), c = threadIdx.x % (D / 8) * 8;
+  const int row = p.rt * kAttnRows + r;
+  if (row >= p.nq * a.group) return;
+  const int64_t part = p.part * kAttnRows + r;
+  const float* ml = a.part_ml + part * 2;
+  const float* o = a.part_o + part * D + c;
+  float top = kNegInf;
+  for (int k = 0; k < splits; ++k) top = fmaxf(top, ml[(int64_t)k * kAttnRows * 2]);
+  float sum = 0.0f, f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int k = 0; k < splits; ++k) {
+    const float m = ml[(int64_t)k * kAttnRows * 2];
+    const float w = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+    sum += w * ml[(int64_t)k * kAttnRows * 2 + 1];
+    float x[8];
+    load8(o + (int64_t)k * kAttnRows * D, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] += w * x[e];
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] *= inv;
+  const int i = row / a.group, g = row - i * a.group;
+  const int64_t head = (int64_t)p.h * a.group + g;
+  Vec8<T>::from(f).store(a.out + head * a.o_head + (int64_t)(p.q0 + i) * a.o_token + c * (int)sizeof(T));
+  if (a.lse != nullptr && c == 0)
+    a.lse[head * a.Tq + p.q0 + i] = sum == 0.0f ? kNegInf : top * 0.69314718055994530942f + logf(sum);
+}
+
+template <typename T, int D>
+int run4(const AttnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((attn4_kernel<T, D>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T, int D>
+int run_join(const AttnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((attn_join_kernel<T, D>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(kAttnRows * D / 8), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int launch_attn4(const AttnArgs& a, int dtype, int d, void* stream) {
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == 0) return d == 128 ? run4<bf16, 128>(a, s) : run4<bf16, 64>(a, s);
+  return d == 128 ? run4<float, 128>(a, s) : run4<float, 64>(a, s);
+}
+
+int launch_attn_join(const AttnArgs& a, int dtype, int d, void* stream) {
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == 0) return d == 128 ? run_join<bf16, 128>(a, s) : run_join<bf16, 64>(a, s);
+  return d == 128 ? run_join<float, 128>(a, s) : run_join<float, 64>(a, s);
+}
+
+}  // namespace twinkv
