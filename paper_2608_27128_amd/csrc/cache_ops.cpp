@@ -159,15 +159,16 @@ void set_rows(Cache4Args& a, const void* keys, const void* values, int dtype, in
 // How a call's rows and keys are cut into items (attn.hip, attn4.hip).
 struct AttnPlan {
   int64_t window = 0, n_sink = 0;
+  int rows = kAttnRows;          // of a tile
   int split_tiles = 0;
   int64_t items = 0, parts = 0;  // per head
 };
 
-int64_t row_tiles(int64_t nq, int group) { return (nq * group + kAttnRows - 1) / kAttnRows; }
+int64_t row_tiles(int64_t nq, int group, int rows) { return (nq * group + rows - 1) / rows; }
 
 // The most key tiles a row tile of the sequence goes through.
 int64_t key_tiles(int64_t nq, int64_t nk, int group, const AttnPlan& p) {
-  const int64_t queries = std::min<int64_t>(nq, kAttnRows / group + 2);
+  const int64_t queries = std::min<int64_t>(nq, p.rows / group + 2);
   const int64_t near = std::min(nk, p.window + queries), sinks = std::min(nk, p.n_sink);
   const int64_t apart = (near + kAttnTile - 1) / kAttnTile + (sinks + kAttnTile - 1) / kAttnTile;
   return std::min(apart, (nk + kAttnTile - 1) / kAttnTile) + 1;
@@ -181,22 +182,36 @@ int64_t splits_of(int64_t tiles, int split_tiles) {
 // two tiles a wave.
 constexpr int64_t kItems = 1024;
 
-int attn_plan(int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
+// Rows that a sequence has in the mean from which the kernel for many of them is taken.
+constexpr int64_t kManyRows = 64;
+
+// many: whether there is a kernel for many rows.
+int attn_plan(bool many, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
               int64_t n_sink, AttnPlan& p) {
   p.window = std::min<int64_t>(window, kAttnMaxKeys);
   p.n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
+  if (many) {
+    int64_t live = 0;
+    for (int s = 0; s < n_seqs; ++s) live += cu_q[s + 1] > cu_q[s];
+    if (cu_q[n_seqs] * group >= kManyRows * live) {
+      p.rows = kAttnBigRows;
+      p.split_tiles = kAttnMaxKeys / 64;
+      for (int s = 0; s < n_seqs; ++s) p.items += row_tiles(cu_q[s + 1] - cu_q[s], group, p.rows);
+      return grid_ok(p.items * n_heads, 256) ? TWINKV_OK : TWINKV_E_ARG;
+    }
+  }
   int64_t work = 0;  // key tiles, over all heads
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t nq = cu_q[s + 1] - cu_q[s];
-    work += n_heads * row_tiles(nq, group) * key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p);
+    work += n_heads * row_tiles(nq, group, p.rows) * key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p);
   }
   const int64_t each = std::max<int64_t>(8, (work + kItems - 1) / kItems);
   p.split_tiles = (int)std::min<int64_t>((each + 3) / 4 * 4, kAttnMaxKeys / 64);
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t nq = cu_q[s + 1] - cu_q[s];
     const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
-    p.items += row_tiles(nq, group) * splits;
-    if (splits > 1) p.parts += row_tiles(nq, group) * splits;
+    p.items += row_tiles(nq, group, p.rows) * splits;
+    if (splits > 1) p.parts += row_tiles(nq, group, p.rows) * splits;
   }
   return grid_ok(p.items, 256) ? TWINKV_OK : TWINKV_E_ARG;
 }
@@ -229,12 +244,12 @@ int check_queries(int n_seqs, const int64_t* cu_q, int group) {
 }
 
 // The queries' and outputs' side of a call, the plan, the words and the parts.
-int attn_args(const void* q, int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q,
+int attn_args(bool many, const void* q, int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q,
               const int64_t* cu_k, int64_t q_head_stride, int64_t q_token_stride, int64_t window, int64_t n_sink,
               float scale, void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse,
               void* workspace, int64_t workspace_bytes, void* stream, AttnArgs& a) {
   AttnPlan p;
-  int rc = attn_plan(n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+  const int rc = attn_plan(many, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
   if (rc != TWINKV_OK) return rc;
   const AttnLayout L = attn_layout(p, d, n_heads, n_seqs);
   if (L.total > 0 && (workspace == nullptr || workspace_bytes < (int64_t)L.total)) return TWINKV_E_WORKSPACE;
@@ -262,6 +277,7 @@ int attn_args(const void* q, int dtype, int d, int n_heads, int group, int n_seq
   a.items = (int)p.items;
   a.parts = (int)p.parts;
   a.split_tiles = p.split_tiles;
+  a.rows = p.rows;
   a.part_o = reinterpret_cast<float*>(ws + L.part_o);
   a.part_ml = reinterpret_cast<float*>(ws + L.part_ml);
   WordWriter w(a.seq, ((int64_t)n_seqs + 1) * kAttnSeqWords, ws, stream);
@@ -270,8 +286,8 @@ int attn_args(const void* q, int dtype, int d, int n_heads, int group, int n_seq
     int64_t splits = 1, tiles = 0;
     if (s < n_seqs) {
       const int64_t nq = cu_q[s + 1] - cu_q[s];
-      tiles = row_tiles(nq, group);
-      splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
+      tiles = row_tiles(nq, group, p.rows);
+      if (p.rows == kAttnRows) splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
     }
     w.put((int32_t)cu_q[s]);
     w.put((int32_t)cu_k[s]);
@@ -344,9 +360,14 @@ int64_t twinkv_attention_workspace_bytes(int dtype, int d, int n_heads, int grou
   if (rc == TWINKV_OK) rc = check_queries(n_seqs, cu_q, group);
   if (rc == TWINKV_OK && (window < 0 || n_sink < 0)) rc = TWINKV_E_ARG;
   if (rc != TWINKV_OK) return -rc;
-  AttnPlan p;
-  rc = attn_plan(n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
-  return rc != TWINKV_OK ? -rc : (int64_t)attn_layout(p, d, n_heads, n_seqs).total;
+  int64_t most = 0;  // of the plans that the two calls may make
+  for (const bool many : {false, true}) {
+    AttnPlan p;
+    rc = attn_plan(many && dtype == TWINKV_BF16, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+    if (rc != TWINKV_OK) return -rc;
+    most = std::max(most, (int64_t)attn_layout(p, d, n_heads, n_seqs).total);
+  }
+  return most;
 }
 
 int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype, int d, int n_heads, int group,
@@ -369,8 +390,8 @@ int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype
   if ((rc = check_rows(v, dtype, d, v_head_stride, v_token_stride, no_k)) != TWINKV_OK) return rc;
   if (no_q) return TWINKV_OK;
   AttnArgs a;
-  rc = attn_args(q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride, window, n_sink, scale,
-                 out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
+  rc = attn_args(dtype == TWINKV_BF16, q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride,
+                 window, n_sink, scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
   a.k = static_cast<const char*>(k);
@@ -379,6 +400,7 @@ int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype
   a.k_token = k_token_stride * esz;
   a.v_head = v_head_stride * esz;
   a.v_token = v_token_stride * esz;
+  if (a.rows == kAttnBigRows) return hip_status(launch_attn_rows(a, d, stream));
   const int e = launch_attn(a, dtype, d, stream);
   if (e != 0 || a.parts == 0) return hip_status(e);
   return hip_status(launch_attn_join(a, dtype, d, stream));
@@ -478,7 +500,7 @@ int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* 
   if (len == nullptr) return TWINKV_E_NULL;
   if (no_q) return TWINKV_OK;
   AttnArgs a;
-  rc = attn_args(q, dtype, d, cache->n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride,
+  rc = attn_args(false, q, dtype, d, cache->n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride,
                  INT64_MAX, 0, scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   a.cache = device_cache(cache);

@@ -79,6 +79,7 @@ int launch_cache4_read(const Cache4Args& a, int dtype, int d, void* stream);
 constexpr int kAttnSeqWords = 5;
 constexpr int kAttnTile = 32;        // keys of a tile
 constexpr int kAttnRows = 16;        // rows of a tile
+constexpr int kAttnBigRows = 128;    // of the kernel for many rows, which splits no keys
 constexpr int kAttnMaxKeys = 1 << 30;  // of all sequences: positions and windows add without overflow
 struct AttnArgs {
   SeqWords seq;
@@ -95,11 +96,14 @@ struct AttnArgs {
   int window, n_sink;    // at most kAttnMaxKeys each
   int n_heads, group, n_seqs;
   int items, parts;      // per head
+  int rows;              // of a tile: kAttnRows or kAttnBigRows
   int split_tiles;       // key tiles of a split
   float* part_o;         // [n_heads][parts][kAttnRows][d] unnormalised sums
   float* part_ml;        // [n_heads][parts][kAttnRows][2] maximum (log2 units) and sum
 };
 int launch_attn(const AttnArgs& a, int dtype, int d, void* stream);
+// bf16; items of kAttnBigRows rows, one split each
+int launch_attn_rows(const AttnArgs& a, int d, void* stream);
 int launch_attn4(const AttnArgs& a, int dtype, int d, void* stream);
 int launch_attn_join(const AttnArgs& a, int dtype, int d, void* stream);
 

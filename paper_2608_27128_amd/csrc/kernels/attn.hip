@@ -266,7 +266,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(const AttnArgs a)
       s[e] *= a.scale_log2;
       if (!all) {
         const int j = base + 8 * g + e;
-        if (!(j < end && j <= pos && (pos - j < window || j < a.n_sink))) s[e] = kNegInf;
+        if (!((j < end) & (j <= pos) & ((pos - j < window) | (j < a.n_sink)))) s[e] = kNegInf;
       }
     }
     st.update(s, acc);

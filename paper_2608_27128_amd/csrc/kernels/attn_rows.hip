@@ -1,0 +1,300 @@
+// K10: attention over the window and the sinks, bf16, many rows (prompts and chunks of prompts).
+//
+// A workgroup of 4 waves owns 128 rows (row = query * group + query head: the heads that share keys sit in one
+// tile, so it spans few queries and little of its work is masked), 32 a wave, and goes over their keys in
+// tiles of 64.
+//  * K q^T on v_mfma_f32_32x32x16_bf16: a lane holds one row (lane % 32) and half of the tile's keys, so
+//    maxima and sums need one exchange between two lanes, and that only when the maximum moves by more
+//    than kSlack (attn_split.h).
+//  * O^T = V^T P^T: the weights are the B operand as they lie; the contraction's order is chosen so that a
+//    lane's keys are its own.  V^T comes from the row-major tile by ds_read_b64_tr_b16.  The accumulators
+//    hold channels of the lane's own row, so rescaling and normalising them needs no exchange.
+//  * A tile is fetched two tiles ahead into registers and written to one of two LDS buffers while the other
+//    is read (loads straight to LDS made the compiler wait for all of them before each transposed read);
+//    16-byte pieces of the keys and 32-byte units of the values are turned by the row so that the lanes
+//    of a read lie in different banks.  One barrier a tile.
+//  * Two workgroups fit a CU (64 KB of LDS each, 256 registers): one's softmax runs beside the other's
+//    products.
+// Values that only some rows of a tile see: as in attn.hip.
+#include <hip/hip_runtime.h>
+
+#include "attn_split.h"
+
+namespace twinkv {
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kThreads = 256;
+constexpr int kWaveRows = 32;
+constexpr int kRows = kAttnBigRows;
+constexpr int kKeys = 64;  // of a tile
+static_assert(kRows == kThreads / 64 * kWaveRows, "a wave owns 32 rows");
+
+template <int D>
+struct Lds {
+  char k[2][kKeys * D * 2];
+  char v[2][kKeys * D * 2];
+  int bad;  // the last tile that held a value which is not finite
+};
+
+// Where 16-byte piece `piece` of key row `row` lies in its tile, and where 32-byte unit `unit` of value row
+// `row` does.
+template <int D>
+__device__ inline int k_place(int row, int piece) {
+  return row * (D * 2) + ((piece ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4);
+}
+template <int D>
+__device__ inline int v_unit(int row, int unit) {
+  return unit ^ (D == 128 ? 2 * (row & 3) : 2 * ((row >> 1) & 1));
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a) {
+  constexpr int kSteps = D / 16;          // of the contraction over channels
+  constexpr int kBlocks = D / 32;         // of 32 output channels
+  constexpr int kRowBytes = D * 2;
+  constexpr int kPieces = kRowBytes / 16;
+  constexpr int kCopies = kKeys * kRowBytes / (kThreads * 16);  // 16-byte pieces a thread brings of each tile
+  __shared__ __attribute__((aligned(16))) Lds<D> s;
+
+  const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // heads side by side: with 8 of them each XCD's L2 keeps one head's keys; the last rows of a sequence,
+  // which see most, first
+  const int h = (int)(blockIdx.x % (unsigned)a.n_heads);
+  const AttnItem p = attn_item(a, a.items - 1 - (int)(blockIdx.x / (unsigned)a.n_heads), h);
+  const int n_rows = p.nq * a.group, row0 = p.rt * kRows;
+  const int offset = p.nk - p.nq;         // position of query 0
+  // what the workgroup's rows see
+  const int pos_lo = offset + row0 / a.group;
+  const int pos_hi = offset + (min(row0 + kRows, n_rows) - 1) / a.group;
+  const int end = max(pos_hi + 1, 0);
+  const int sinks = min(a.n_sink, end);
+  int lo = min(max(pos_lo - a.window + 1, 0), end);
+  int sink_tiles = (sinks + kKeys - 1) / kKeys;
+  if (lo <= sink_tiles * kKeys) {         // the two meet
+    if (sinks > 0) lo = 0;
+    sink_tiles = 0;
+  }
+  const int tiles = sink_tiles + (end - lo + kKeys - 1) / kKeys;
+  // this lane's row; rows past the problem's repeat its last, and are not written
+  const int row = min(row0 + wave * kWaveRows + r32, n_rows - 1);
+  const int query = row / a.group;
+  const int pos = offset + query;
+  // and what the wave's rows see
+  const int wave_lo = offset + min(row0 + wave * kWaveRows, n_rows - 1) / a.group;
+  const int wave_hi = offset + min(row0 + wave * kWaveRows + kWaveRows - 1, n_rows - 1) / a.group;
+
+  const char* kb = a.k + (int64_t)h * a.k_head + (int64_t)p.k0 * a.k_token;
+  const char* vb = a.v + (int64_t)h * a.v_head + (int64_t)p.k0 * a.v_token;
+  // a tile's pieces in registers on their way from memory to buffer t % 2
+  u32x4 k_next[kCopies], v_next[kCopies];
+  auto fetch = [&](int t) {
+    const bool sink = t < sink_tiles;
+    const int base = sink ? t * kKeys : lo + (t - sink_tiles) * kKeys;
+    const int stop = sink ? sinks : end;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      const int at = c * kThreads + tid;   // 16-byte piece of the tile
+      const int64_t key = min(base + at / kPieces, stop - 1);
+      k_next[c] = *reinterpret_cast<const u32x4*>(kb + key * a.k_token + at % kPieces * 16);
+      v_next[c] = *reinterpret_cast<const u32x4*>(vb + key * a.v_token + at % kPieces * 16);
+    }
+  };
+  auto stage = [&](int t) {
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      const int at = c * kThreads + tid, r = at / kPieces, piece = at % kPieces;
+      *reinterpret_cast<u32x4*>(s.k[t & 1] + k_place<D>(r, piece)) = k_next[c];
+      *reinterpret_cast<u32x4*>(s.v[t & 1] + r * kRowBytes + v_unit<D>(r, piece >> 1) * 32 + (piece & 1) * 16) = v_next[c];
+    }
+  };
+
+  // scale > 0 from here on: the sign goes to q.  0 (all weights alike) becomes as good as 0, so that masked
+  // scores stay -inf.
+  const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);
+  bf16x8 q[kSteps];
+  {
+    const char* src = a.q + ((int64_t)h * a.group + (row - query * a.group)) * a.q_head +
+                      (int64_t)(p.q0 + query) * a.q_token + hi * 16;
+    const unsigned flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      u32x4 w = *reinterpret_cast<const u32x4*>(src + j * 32);
+      w ^= flip;
+      q[j] = __builtin_bit_cast(bf16x8, w);
+    }
+  }
+  if (tid == 0) s.bad = -1;
+
+  f32x16 acc[kBlocks];
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[b][e] = 0.0f;
+  float m = kNegInf, l = 0.0f;
+
+  if (tiles > 0) {
+    fetch(0);
+    stage(0);
+    if (tiles > 1) fetch(1);
+  }
+  for (int t = 0; t < tiles; ++t) {
+    __syncthreads();                       // tile t lies in LDS, and nobody reads the other buffer
+    if (t + 1 < tiles) stage(t + 1);
+    if (t + 2 < tiles) fetch(t + 2);
+    const bool sink = t < sink_tiles;
+    const int base = sink ? t * kKeys : lo + (t - sink_tiles) * kKeys;
+    const int stop = sink ? sinks : end;
+    const int top = base + kKeys - 1;
+    const char* ks = s.k[t & 1];
+    char* vs = s.v[t & 1];
+    bool bad = false;
+    if (top >= stop || top > pos_lo || (base <= pos_hi - a.window && top >= a.n_sink)) {
+      // some row does not see some key: values that are past the range or not finite become zeros
+#pragma unroll
+      for (int c = 0; c < kCopies; ++c) {
+        const int at = c * kThreads + tid;
+        s16x8 x = *reinterpret_cast<const s16x8*>(vs + at * 16);
+        const bool out = base + at / kPieces >= stop;
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool o = (x[e] & 0x7f80) == 0x7f80;
+          odd |= o;
+          if (o || out) x[e] = 0;
+        }
+        if (odd || out) *reinterpret_cast<s16x8*>(vs + at * 16) = x;
+        if (odd && !out) s.bad = t;
+      }
+      __syncthreads();
+      bad = s.bad == t;
+    }
+    // nothing for this wave: past its last row, or before its first row's window and past the sinks
+    if (base > wave_hi || (top <= wave_lo - a.window && base >= a.n_sink)) continue;
+
+    f32x16 x[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[b][e] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const bf16x8 k = *reinterpret_cast<const bf16x8*>(ks + k_place<D>(b * 32 + r32, 2 * j + hi));
+        x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[j], x[b], 0, 0, 0);
+      }
+    if (top >= stop || top > wave_lo || (base <= wave_hi - a.window && top >= a.n_sink)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = base + b * 32 + 8 * (e >> 2) + 4 * hi + (e & 3);
+          if (!((j < stop) & (j <= pos) & ((pos - j < a.window) | (j < a.n_sink)))) x[b][e] = kNegInf;
+        }
+    }
+    float most = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+    for (int e = 1; e < 16; ++e) most = fmaxf(most, fmaxf(x[0][e], x[1][e]));
+    most *= scale;
+    if (__any(most > m + kSlack)) {
+      const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+      const float next = fmaxf(m, fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])));
+      const float f = next == m ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= f;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[b][e] *= f;
+    }
+    const float from = m == kNegInf ? 0.0f : m;
+    bf16x8 w[4];                           // 16 keys each
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], scale, -from));
+        l += x[b][e];
+        w[2 * b + (e >> 3)][e & 7] = (bf16)x[b][e];
+      }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        // lane i of 16 points at key row i / 4, 4 channels at i % 4; it gets channel i of the 4 keys
+        s16x4 v[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int r = 16 * j + 8 * u + 4 * hi + ((lane & 15) >> 2);
+          const int unit = v_unit<D>(r, 2 * b + ((lane >> 4) & 1));
+          v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(vs + r * kRowBytes + unit * 32 + (lane & 3) * 8));
+        }
+        struct Two { s16x4 a, b; } two = {v[0], v[1]};
+        acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, two), w[j], acc[b], 0, 0, 0);
+      }
+    if (bad) {
+      // the values that are not finite, to the rows that see them
+      for (int y = 0; y < kKeys; ++y) {
+        const int j = base + y;
+        if (j >= stop) break;
+        const int e = 4 * ((y & 31) >> 3) + (y & 3);
+        float mine = 0.0f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int z = 0; z < 16; ++z) mine = (y >> 5) == b && e == z ? x[b][z] : mine;
+        const float weight = __shfl(mine, r32 + 32 * ((y >> 2) & 1));
+        if (!(j <= pos && (pos - j < a.window || j < a.n_sink))) continue;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int z = 0; z < 16; ++z) {
+            const int ch = 32 * b + 8 * (z >> 2) + 4 * hi + (z & 3);
+            const float v = (float)*reinterpret_cast<const bf16*>(vb + j * a.v_token + ch * 2);
+            if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) acc[b][z] += weight * v;
+          }
+      }
+    }
+  }
+
+  {
+    const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(two[0]) + __uint_as_float(two[1]);
+  }
+  const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+  if (row0 + wave * kWaveRows + r32 >= n_rows) return;
+  const int64_t head = (int64_t)h * a.group + (row - query * a.group);
+  char* out = a.out + head * a.o_head + (int64_t)(p.q0 + query) * a.o_token;
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 o;
+#pragma unroll
+      for (int z = 0; z < 4; ++z) o[z] = (bf16)(acc[b][4 * y + z] * inv);
+      *reinterpret_cast<bf16x4*>(out + (32 * b + 8 * y + 4 * hi) * 2) = o;
+    }
+  if (a.lse != nullptr && hi == 0)
+    a.lse[head * a.Tq + p.q0 + query] = l == 0.0f ? kNegInf : m * 0.69314718055994530942f + logf(l);
+}
+
+template <int D>
+int run(const AttnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((attn_rows_kernel<D>), dim3((unsigned)a.items * (unsigned)a.n_heads), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int launch_attn_rows(const AttnArgs& a, int d, void* stream) {
+  hipStream_t s = (hipStream_t)stream;
+  return d == 128 ? run<128>(a, s) : run<64>(a, s);
+}
+
+}  // namespace twinkv

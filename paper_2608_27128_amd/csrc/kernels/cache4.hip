@@ -295,10 +295,12 @@ __global__ __launch_bounds__(kMaxWaves * 64) void cache4_append_kernel(const Cac
 __global__ __launch_bounds__(kThreads) void cache4_grow_kernel(const Cache4Args a) {
   const int q = (int)(blockIdx.x * kThreads + threadIdx.x);
   if (q >= a.n_heads * a.n_seqs) return;
-  const AppendTo p = append_to(a, q % a.n_seqs);
+  const int w = q % a.n_seqs * kCacheSeqWords;  // another sequence in each lane
+  const int n = seq_word_of_lane(a.seq, w + kCacheSeqWords) - seq_word_of_lane(a.seq, w);
+  const int cap = seq_word_of_lane(a.seq, w + kCacheSeqWords + 1) - seq_word_of_lane(a.seq, w + 1);
   const int len = a.len_in[q];
-  const bool fits = len >= 0 && len <= p.cap - p.n;
-  a.len_out[q] = fits ? len + p.n : len;
+  const bool fits = len >= 0 && len <= cap - n;
+  a.len_out[q] = fits ? len + n : len;
   a.status[q] = fits ? kOk : kMismatch;
 }
 template <typename T, int D>

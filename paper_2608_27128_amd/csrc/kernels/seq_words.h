@@ -6,8 +6,12 @@
 
 namespace twinkv {
 
-__device__ inline int32_t seq_word(const SeqWords& t, int i) {
+__device__ inline int32_t seq_word_of_lane(const SeqWords& t, int i) {
   return t.far != nullptr ? t.far[i] : t.near[i];
+}
+// i is the same in all lanes, and the word scalar from here on.
+__device__ inline int32_t seq_word(const SeqWords& t, int i) {
+  return __builtin_amdgcn_readfirstlane(seq_word_of_lane(t, i));
 }
 
 // The sequence whose range of the non-decreasing words w(s) = word[s * stride + at], s in [0, n], holds
