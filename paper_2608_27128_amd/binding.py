@@ -221,8 +221,8 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream(device) -> int:
-    torch = _torch()
-    return torch.cuda.current_stream(device).cuda_stream
+    # the handle alone: building torch's stream object costs a small call more than its launch
+    return _torch()._C._cuda_getCurrentRawStream(device.index)
 
 
 def _mask(x, n_heads, T, device, name):
@@ -246,8 +246,12 @@ def _launch(dev, name: str, *args) -> None:
     """Call the library entry point ``name`` with the tensors' device current: the library
     enqueues on the given stream of the current device and keeps its per-device state there."""
     torch = _torch()
-    with torch.cuda.device(dev):
-        rc = getattr(lib(), name)(*args)
+    fn = getattr(_lib or lib(), name)
+    if torch.cuda.current_device() == dev.index:
+        rc = fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args)
     if rc != TWINKV_OK:
         raise TwinKVError(name, rc)
 
@@ -631,10 +635,15 @@ def compact(keys, retained, capacity, values=None, cu_seqlens=None, *, want_pos:
 
 # ---------------------------------------------------------------- the layer around the cache
 
-def _i64_view(values) -> ctypes.Array:
-    """Host offsets as a C array over an int64 copy of them."""
-    arr = np.array(values, dtype=np.int64)
-    return (ctypes.c_int64 * len(arr)).from_buffer(arr)
+def _offsets(cu, T: int, name: str):
+    """Host offsets as (C array over an int64 copy of them, sequences), checked to end at T: what the tensors
+    hold.  That they start at 0 and never decrease the library checks, before anything is enqueued."""
+    arr = np.array((0, T) if cu is None else cu, dtype=np.int64)
+    if arr.ndim != 1 or arr.size < 2:
+        raise ValueError(f"{name} must list n_seqs + 1 >= 2 offsets")
+    if arr[-1] != T:
+        raise ValueError(f"{name}[-1] = {int(arr[-1])} must equal T = {T}")
+    return (ctypes.c_int64 * arr.size).from_buffer(arr), arr.size - 1
 
 
 def _rows(x, name: str, dtype=None, d=None, dev=None):
@@ -669,9 +678,8 @@ def _rows(x, name: str, dtype=None, d=None, dev=None):
 
 def _out_rows(out, shape, like, name: str):
     """The caller's output rows (written in place, so they must be addressable as they are), or new ones."""
-    torch = _torch()
     if out is None:
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
+        return like.new_empty(shape)
     if tuple(out.shape) != tuple(shape) or out.dtype != like.dtype or out.device != like.device:
         raise ValueError(f"{name} must be {tuple(shape)} {like.dtype} on {like.device}, got "
                          f"{tuple(out.shape)} {out.dtype} on {out.device}")
@@ -686,10 +694,11 @@ def _small(x, shape, dtype, dev, name: str):
     """A contiguous, 16-byte aligned operand of one exact shape and type (None stays None)."""
     if x is None:
         return None
-    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or x.device != dev:
-        raise ValueError(f"{name} must be {tuple(shape)} {dtype} on {dev}, got {tuple(x.shape)} {x.dtype} on {x.device}")
-    x = x.contiguous()
-    return x if x.data_ptr() % 16 == 0 else x.clone()
+    if x.shape != shape or x.dtype != dtype or x.device != dev:
+        raise ValueError(f"{name} must be {shape} {dtype} on {dev}, got {tuple(x.shape)} {x.dtype} on {x.device}")
+    if x.is_contiguous() and x.data_ptr() % 16 == 0:
+        return x
+    return x.clone(memory_format=_torch().contiguous_format)
 
 
 def _scratch(workspace, nbytes: int, dev, fn: str):
@@ -713,7 +722,6 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, eps: float = 1e-6, rope=Non
     some = q if q is not None else k
     if some is None:
         raise ValueError("q or k is required")
-    given_q, given_k = q, k
     dt = T = d = None
     if q is not None:
         q, dt = _rows(q, "q")
@@ -734,7 +742,7 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, eps: float = 1e-6, rope=Non
         positions = _small(positions, (T,), torch.int32, dev, "positions")
     out = {}
     args = {"q": (None, 0, 0, 0, None, 0, 0), "k": (None, 0, 0, 0, None, 0, 0)}
-    for name, x, given, to in (("q", q, given_q, q_out), ("k", k, given_k, k_out)):
+    for name, x, to in (("q", q, q_out), ("k", k, k_out)):
         if x is None:
             continue
         if to is not None and to.dim() == 2:
@@ -750,9 +758,11 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, eps: float = 1e-6, rope=Non
 
 def attention_workspace_bytes(dtype: int, d: int, n_heads: int, group: int, cu_q, cu_k, window: int,
                               n_sink: int) -> int:
-    cq, ck = _i64_view(cu_q), _i64_view(cu_k)
-    n = int(lib().twinkv_attention_workspace_bytes(dtype, d, n_heads, group, len(cq) - 1, cq, ck, int(window),
-                                                   int(n_sink)))
+    cq, n_seqs = _offsets(cu_q, int(cu_q[-1]), "cu_q")
+    ck, n_k = _offsets(cu_k, int(cu_k[-1]), "cu_k")
+    if n_k != n_seqs:
+        raise ValueError("cu_q and cu_k must list the same number of sequences")
+    n = int(lib().twinkv_attention_workspace_bytes(dtype, d, n_heads, group, n_seqs, cq, ck, int(window), int(n_sink)))
     if n < 0:
         raise TwinKVError("twinkv_attention_workspace_bytes", -n)
     return n
@@ -780,9 +790,9 @@ def sink_attention(q, k, v, window: int, n_sink: int = 4, scale: Optional[float]
     if tuple(v.shape) != (H, Tk, d):
         raise ValueError("v must match k in shape")
     group = _group(Hq, H)
-    cq, ck = _i64_view(_cu(cu_q, Tq)), _i64_view(_cu(cu_k, Tk))
-    n_seqs = len(cq) - 1
-    if len(ck) - 1 != n_seqs:
+    cq, n_seqs = _offsets(cu_q, Tq, "cu_q")
+    ck, n_k = _offsets(cu_k, Tk, "cu_k")
+    if n_k != n_seqs:
         raise ValueError("cu_q and cu_k must list the same number of sequences")
     if window < 0 or n_sink < 0:
         raise ValueError("window and n_sink must not be negative")
@@ -812,9 +822,9 @@ class Cache4:
     (n_heads, n_seqs), which cache4_compact and cache4_append return."""
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales, cu_rows):
-        torch = _torch()
+        u8 = _torch().uint8
         cu = np.array(cu_rows, dtype=np.int64)
-        if cu.ndim != 1 or len(cu) < 2 or cu[0] != 0 or np.any(np.diff(cu) < 0) or np.any(cu % 32):
+        if cu.ndim != 1 or cu.size < 2 or cu[0] != 0 or (cu[1:] < cu[:-1]).any() or (cu & 31).any():
             raise ValueError("cu_rows must start at 0, never decrease, and be multiples of 32")
         if k_codes.dim() != 3:
             raise ValueError("k_codes must be (n_heads, C, d / 2)")
@@ -822,14 +832,14 @@ class Cache4:
         dev = k_codes.device
         for name, x, shape in (("k_codes", k_codes, (H, C, d // 2)), ("k_scales", k_scales, (H, C, d // 32)),
                                ("v_codes", v_codes, (H, C // 8, d, 4)), ("v_scales", v_scales, (H, C // 8, d // 32, 8))):
-            if tuple(x.shape) != shape or x.dtype != torch.uint8 or x.device != dev or not x.is_contiguous():
+            if x.shape != shape or x.dtype != u8 or x.device != dev or not x.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous uint8 {shape} tensor on {dev}, got {tuple(x.shape)} {x.dtype}")
         if not k_codes.is_cuda:
             raise ValueError("the cache must be on a GPU")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
-        self.cu_rows, self.n_heads, self.n_seqs, self.d, self.device = cu, H, len(cu) - 1, d, dev
-        self._cu = (ctypes.c_int64 * len(cu)).from_buffer(cu)
-        self._struct = _Cache4Struct(d, H, len(cu) - 1, ctypes.cast(self._cu, _PI64), k_codes.data_ptr(),
+        self.cu_rows, self.n_heads, self.n_seqs, self.d, self.device = cu, H, cu.size - 1, d, dev
+        self._cu = (ctypes.c_int64 * cu.size).from_buffer(cu)
+        self._struct = _Cache4Struct(d, H, cu.size - 1, ctypes.cast(self._cu, _PI64), k_codes.data_ptr(),
                                      k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
         self._handle = ctypes.addressof(self._struct)
 
@@ -846,10 +856,10 @@ class Cache4:
         return _small(x, (self.n_heads, self.n_seqs), _torch().int32, self.device, name)
 
     def _offsets(self, cu, T: int, name: str):
-        cu = _cu(cu, T)
-        if len(cu) - 1 != self.n_seqs:
+        arr, n = _offsets(cu, T, name)
+        if n != self.n_seqs:
             raise ValueError(f"{name} must list the cache's {self.n_seqs} sequences")
-        return _i64_view(cu)
+        return arr
 
 
 def _cache4_rows(keys, values, cache: Cache4):
@@ -918,8 +928,8 @@ def cache4_read(cache: Cache4, length, dtype, first=None, cu_out=None, *, want_k
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"unsupported dtype {dtype}")
     dev = cache.device
-    cu = np.asarray(cache.cu_rows if cu_out is None else cu_out, dtype=np.int64)
-    cu = cache._offsets(cu, int(cu[-1]) if cu.ndim == 1 and len(cu) else 0, "cu_out")
+    cu_out = cache.cu_rows if cu_out is None else cu_out
+    cu = cache._offsets(cu_out, int(cu_out[-1]), "cu_out")
     n = cache._lens(length, "length")
     f = cache._lens(first, "first")
     shape = (cache.n_heads, int(cu[-1]), cache.d)

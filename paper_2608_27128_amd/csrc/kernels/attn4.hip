@@ -46,37 +46,56 @@ __device__ inline void split8(const float (&x)[8], bf16x8 (&p)[N]) {
   }
 }
 
-// One wave's 32 rows of the cache in registers.
+// One wave's 32 rows of the cache on their way through registers.  A lane's addresses of one tile lie at fixed
+// distances, and move by whole tiles.
 template <int D>
 struct Tile4 {
+  const uint8_t *kp, *ksp, *vp, *vsp;
   u32x4 k[2];          // d 64: words 0, 1
   unsigned ks[2];
   u32x4 v[D / 64];
   u32x4 vs[D / 64];    // [d/32] groups of 8 bytes
-  __device__ void load(const Cache4& c, int64_t row, int i, int g) {  // row: of the cache, a multiple of 32
+  __device__ Tile4(const Cache4& c, int h, int64_t row, int i, int g) {  // row: in the head, a multiple of 32
+    row += (int64_t)h * c.C;
+    const int64_t r = row + 8 * (i >> 2) + (i & 3), b = row / kCacheBlock + g;
+    kp = c.k_codes + r * (D / 2) + g * (D / 8);
+    ksp = c.k_scales + r * (D / 32) + g * (D / 4) / 32;
+    vp = c.v_codes + b * (D * 4) + i * 16;
+    vsp = c.v_scales + b * (D / 4);
+  }
+  __device__ void load_keys() {
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const int64_t r = row + 8 * (i >> 2) + 4 * m + (i & 3);
       if constexpr (D == 128) {
-        k[m] = *reinterpret_cast<const u32x4*>(c.k_codes + r * 64 + g * 16);
-        ks[m] = c.k_scales[r * 4 + g];
+        k[m] = *reinterpret_cast<const u32x4*>(kp + m * 4 * (D / 2));
       } else {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(c.k_codes + r * 32 + g * 8);
+        const u32x2 w = *reinterpret_cast<const u32x2*>(kp + m * 4 * (D / 2));
         k[m] = u32x4{w[0], w[1], 0u, 0u};
-        ks[m] = c.k_scales[r * 2 + (g >> 1)];
       }
+      ks[m] = ksp[m * 4 * (D / 32)];
     }
-    const int64_t b = row / kCacheBlock + g;
+  }
+  __device__ void load_values() {
 #pragma unroll
     for (int a = 0; a < D / 64; ++a) {
-      v[a] = *reinterpret_cast<const u32x4*>(c.v_codes + (b * D + a * 64 + i * 4) * 4);
-      vs[a] = *reinterpret_cast<const u32x4*>(c.v_scales + b * (D / 4) + a * 16);
+      v[a] = *reinterpret_cast<const u32x4*>(vp + a * 256);
+      vs[a] = *reinterpret_cast<const u32x4*>(vsp + a * 16);
     }
+  }
+  __device__ void next_keys(int rows) {
+    kp += rows * (D / 2);
+    ksp += rows * (D / 32);
+    load_keys();
+  }
+  __device__ void next_values(int rows) {
+    vp += rows * (D / 2);
+    vsp += rows * (D / 32);
+    load_values();
   }
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kAttnWaves) void attn4_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4_kernel(const AttnArgs a) {
   constexpr int kSteps = D / 32;
   constexpr int N = kParts<T>;
   __shared__ float s_join[join_floats<D>()];
@@ -109,24 +128,18 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn4_kernel(const AttnArgs a
       for (int n = 0; n < N; ++n) q[n][j] = parts[n];
     }
   }
-  Cache4 c = a.cache;
-  c.k_codes += (int64_t)p.h * c.C * (D / 2);
-  c.k_scales += (int64_t)p.h * c.C * (D / 32);
-  c.v_codes += (int64_t)p.h * c.C * (D / 2);
-  c.v_scales += (int64_t)p.h * c.C * (D / 32);
-
   RowStats st;
   f32x4 acc[D / 16];
 #pragma unroll
   for (int n = 0; n < D / 16; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   constexpr int kStep = kAttnTile * kAttnWaves;
-  Tile4<D> next;
   const int first = t0 + wave * kAttnTile;
-  if (first < t1) next.load(c, p.k0 + first, i, g);
+  Tile4<D> now(a.cache, p.h, (int64_t)p.k0 + first, i, g);
+  if (first < t1) {
+    now.load_keys();
+    now.load_values();
+  }
   for (int t = first; t < t1; t += kStep) {
-    Tile4<D> now = next;
-    if (t + kStep < t1) next.load(c, p.k0 + t + kStep, i, g);
-
     float s[8];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -141,6 +154,8 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn4_kernel(const AttnArgs a
 #pragma unroll
       for (int r = 0; r < 4; ++r) s[4 * m + r] = d[r] * a.scale_log2;
     }
+    const bool more = t + kStep < t1;
+    if (more) now.next_keys(kStep);
     if (t + kAttnTile > lim_all) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -171,43 +186,72 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn4_kernel(const AttnArgs a
         for (int n = N - 1; n >= 0; --n) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], v, acc[b], 0, 0, 0);
       }
     }
+    if (more) now.next_values(kStep);
   }
   join_waves<T, D>(a, p, row0, st, acc, s_join, [](int n, int lane16) { return n * 16 + lane16; });
 }
 
-// The join: for each row tile with splits, the parts' sums brought to one maximum.
+// The join: a row tile's parts brought to one maximum.  The tile's items share its rows out among them (item
+// `split` takes rows split, split + splits, ...); the threads of a workgroup take 8 channels and every kLanes-th
+// part each, and add up through LDS.
+constexpr int kJoinThreads = 256;
 template <typename T, int D>
-__global__ __launch_bounds__(kAttnRows* D / 8) void attn_join_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(const AttnArgs a) {
+  constexpr int kPieces = D / 8, kLanes = kJoinThreads / kPieces;
+  __shared__ float s_o[kLanes][D];
+  __shared__ float s_ml[kLanes][2];
   const AttnItem p = attn_item(a, (int)blockIdx.x, (int)blockIdx.y);
-  const int splits = p.splits;
-  if (p.split != 0 || splits <= 1) return;
-  const int r = threadIdx.x / (D / 8), c = threadIdx.x % (D / 8) * 8;
-  const int row = p.rt * kAttnRows + r;
-  if (row >= p.nq * a.group) return;
-  const int64_t part = p.part * kAttnRows + r;
-  const float* ml = a.part_ml + part * 2;
-  const float* o = a.part_o + part * D + c;
-  float top = kNegInf;
-  for (int k = 0; k < splits; ++k) top = fmaxf(top, ml[(int64_t)k * kAttnRows * 2]);
-  float sum = 0.0f, f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int k = 0; k < splits; ++k) {
-    const float m = ml[(int64_t)k * kAttnRows * 2];
-    const float w = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-    sum += w * ml[(int64_t)k * kAttnRows * 2 + 1];
-    float x[8];
-    load8(o + (int64_t)k * kAttnRows * D, x);
+  if (p.splits <= 1) return;
+  const int c = threadIdx.x % kPieces * 8, sl = threadIdx.x / kPieces;
+  for (int r = p.split; r < kAttnRows; r += p.splits) {
+    const int row = p.rt * kAttnRows + r;
+    if (row >= p.nq * a.group) break;
+    const int64_t part = (p.part - p.split) * kAttnRows + r;  // of split 0
+    const float* ml = a.part_ml + part * 2;
+    const float* o = a.part_o + part * D + c;
+    float top = kNegInf, sum = 0.0f, f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = sl; k < p.splits; k += kLanes) {
+      const float m = ml[(int64_t)k * kAttnRows * 2], l = ml[(int64_t)k * kAttnRows * 2 + 1];
+      float x[8];
+      load8(o + (int64_t)k * kAttnRows * D, x);
+      const float next = fmaxf(top, m);
+      const float u = next == top ? 1.0f : __builtin_amdgcn_exp2f(top - next);
+      const float w = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+      top = next;
+      sum = sum * u + l * w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] += w * x[e];
+      for (int e = 0; e < 8; ++e) f[e] = f[e] * u + x[e] * w;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s_o[sl][c + e] = f[e];
+    if (c == 0) {
+      s_ml[sl][0] = top;
+      s_ml[sl][1] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x < kPieces) {
+      const int lanes = min(kLanes, p.splits);
+      for (int k = 1; k < lanes; ++k) {  // f, top and sum are lane 0's so far
+        const float m = s_ml[k][0], l = s_ml[k][1];
+        const float next = fmaxf(top, m);
+        const float u = next == top ? 1.0f : __builtin_amdgcn_exp2f(top - next);
+        const float w = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+        top = next;
+        sum = sum * u + l * w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = f[e] * u + s_o[k][c + e] * w;
+      }
+      const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= inv;
+      const int i = row / a.group, g = row - i * a.group;
+      const int64_t head = (int64_t)p.h * a.group + g;
+      Vec8<T>::from(f).store(a.out + head * a.o_head + (int64_t)(p.q0 + i) * a.o_token + c * (int)sizeof(T));
+      if (a.lse != nullptr && c == 0)
+        a.lse[head * a.Tq + p.q0 + i] = sum == 0.0f ? kNegInf : top * 0.69314718055994530942f + logf(sum);
+    }
+    __syncthreads();
   }
-  const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] *= inv;
-  const int i = row / a.group, g = row - i * a.group;
-  const int64_t head = (int64_t)p.h * a.group + g;
-  Vec8<T>::from(f).store(a.out + head * a.o_head + (int64_t)(p.q0 + i) * a.o_token + c * (int)sizeof(T));
-  if (a.lse != nullptr && c == 0)
-    a.lse[head * a.Tq + p.q0 + i] = sum == 0.0f ? kNegInf : top * 0.69314718055994530942f + logf(sum);
 }
 
 template <typename T, int D>
@@ -217,7 +261,7 @@ int run4(const AttnArgs& a, hipStream_t s) {
 }
 template <typename T, int D>
 int run_join(const AttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attn_join_kernel<T, D>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(kAttnRows * D / 8), 0, s, a);
+  hipLaunchKernelGGL((attn_join_kernel<T, D>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 
