@@ -160,7 +160,7 @@ void set_rows(Cache4Args& a, const void* keys, const void* values, int dtype, in
 struct AttnPlan {
   int64_t window = 0, n_sink = 0;
   int rows = kAttnRows;          // of a tile
-  int split_tiles = 0;
+  int split_tiles = 0;           // the most of a split
   int64_t items = 0, parts = 0;  // per head
 };
 
@@ -174,13 +174,19 @@ int64_t key_tiles(int64_t nq, int64_t nk, int group, const AttnPlan& p) {
   return std::min(apart, (nk + kAttnTile - 1) / kAttnTile) + 1;
 }
 
-int64_t splits_of(int64_t tiles, int split_tiles) {
-  return std::max<int64_t>(1, (tiles + split_tiles - 1) / split_tiles);
+// A sequence's splits, of at most `most` tiles each, as equal as whole rounds of the 4 waves make them.
+struct Splits {
+  int64_t n, tiles;
+};
+Splits splits_of(int64_t tiles, int most) {
+  int64_t n = std::max<int64_t>(1, (tiles + most - 1) / most);
+  const int64_t each = ((tiles + n - 1) / n + 3) / 4 * 4;
+  return Splits{std::max<int64_t>(1, (tiles + each - 1) / each), each};
 }
 
 // Items go to workgroups of 4 waves; the whole work is cut into about kItems of them, a split no shorter than
 // two tiles a wave.
-constexpr int64_t kItems = 1024;
+constexpr int64_t kItems = 512;
 
 // Rows that a sequence has in the mean from which the kernel for many of them is taken.
 constexpr int64_t kManyRows = 64;
@@ -209,7 +215,7 @@ int attn_plan(bool many, int n_heads, int group, int n_seqs, const int64_t* cu_q
   p.split_tiles = (int)std::min<int64_t>((each + 3) / 4 * 4, kAttnMaxKeys / 64);
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t nq = cu_q[s + 1] - cu_q[s];
-    const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
+    const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles).n;
     p.items += row_tiles(nq, group, p.rows) * splits;
     if (splits > 1) p.parts += row_tiles(nq, group, p.rows) * splits;
   }
@@ -276,14 +282,14 @@ int attn_args(bool many, const void* q, int dtype, int d, int n_heads, int group
   a.n_seqs = n_seqs;
   a.items = (int)p.items;
   a.parts = (int)p.parts;
-  a.split_tiles = p.split_tiles;
   a.rows = p.rows;
   a.part_o = reinterpret_cast<float*>(ws + L.part_o);
   a.part_ml = reinterpret_cast<float*>(ws + L.part_ml);
   WordWriter w(a.seq, ((int64_t)n_seqs + 1) * kAttnSeqWords, ws, stream);
   int64_t item = 0, part = 0;
   for (int s = 0; s <= n_seqs; ++s) {
-    int64_t splits = 1, tiles = 0;
+    Splits splits{1, 0};
+    int64_t tiles = 0;
     if (s < n_seqs) {
       const int64_t nq = cu_q[s + 1] - cu_q[s];
       tiles = row_tiles(nq, group, p.rows);
@@ -292,10 +298,11 @@ int attn_args(bool many, const void* q, int dtype, int d, int n_heads, int group
     w.put((int32_t)cu_q[s]);
     w.put((int32_t)cu_k[s]);
     w.put((int32_t)item);
-    w.put((int32_t)splits);
+    w.put((int32_t)splits.n);
+    w.put((int32_t)splits.tiles);
     w.put((int32_t)part);
-    item += tiles * splits;
-    if (splits > 1) part += tiles * splits;
+    item += tiles * splits.n;
+    if (splits.n > 1) part += tiles * splits.n;
   }
   return hip_status(w.finish());
 }

@@ -74,9 +74,9 @@ int launch_cache4_read(const Cache4Args& a, int dtype, int d, void* stream);
 
 // Attention.  Rows of a problem (KV head, sequence) are its queries times its query heads: row
 // r = i * group + g.  An item is a tile of rows and a range of key tiles; a problem's items are
-// row tiles times splits.  Words per sequence: first query, first key, first item, splits, first part
-// (the items of sequences with more than one split leave parts, numbered apart).
-constexpr int kAttnSeqWords = 5;
+// row tiles times splits.  Words per sequence: first query, first key, first item, splits, key tiles of a
+// split, first part (the items of sequences with more than one split leave parts, numbered apart).
+constexpr int kAttnSeqWords = 6;
 constexpr int kAttnTile = 32;        // keys of a tile
 constexpr int kAttnRows = 16;        // rows of a tile
 constexpr int kAttnBigRows = 128;    // of the kernel for many rows, which splits no keys
@@ -97,7 +97,6 @@ struct AttnArgs {
   int n_heads, group, n_seqs;
   int items, parts;      // per head
   int rows;              // of a tile: kAttnRows or kAttnBigRows
-  int split_tiles;       // key tiles of a split
   float* part_o;         // [n_heads][parts][kAttnRows][d] unnormalised sums
   float* part_ml;        // [n_heads][parts][kAttnRows][2] maximum (log2 units) and sum
 };

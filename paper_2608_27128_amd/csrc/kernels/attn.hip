@@ -234,8 +234,8 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(const AttnArgs a)
   const int query = row / a.group;
   const int pos = p.nk - p.nq + query;
   const Span sp = span_of(a, p, row0, last);
-  const int first = p.split * a.split_tiles + wave;
-  const int stop = min(sp.tiles, (p.split + 1) * a.split_tiles);
+  const int first = p.split * p.tiles + wave;
+  const int stop = min(sp.tiles, (p.split + 1) * p.tiles);
   const int window = a.window;
 
   typename Keys::Query q;

@@ -111,8 +111,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4
   const int lim = len - (p.nq - 1 - query);
   const int lim_all = len - (p.nq - 1 - row0 / a.group);      // every row sees so many
   const int lim_any = len - (p.nq - 1 - last / a.group);      // no row sees more
-  const int t0 = p.split * a.split_tiles * kAttnTile;
-  const int t1 = min(lim_any, t0 + a.split_tiles * kAttnTile);
+  const int t0 = p.split * p.tiles * kAttnTile;
+  const int t1 = min(lim_any, t0 + p.tiles * kAttnTile);
 
   bf16x8 q[N][kSteps];
   {
@@ -154,8 +154,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4
 #pragma unroll
       for (int r = 0; r < 4; ++r) s[4 * m + r] = d[r] * a.scale_log2;
     }
-    const bool more = t + kStep < t1;
-    if (more) now.next_keys(kStep);
+    // the next tile, or this one once more: a load on one path only would make the waits of both longer
+    const int ahead = t + kStep < t1 ? kStep : 0;
+    now.next_keys(ahead);
     if (t + kAttnTile > lim_all) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -186,7 +187,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4
         for (int n = N - 1; n >= 0; --n) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], v, acc[b], 0, 0, 0);
       }
     }
-    if (more) now.next_values(kStep);
+    now.next_values(ahead);
+    asm volatile("" ::: "memory");  // here, and not where the next tile begins: the scores cover the way
   }
   join_waves<T, D>(a, p, row0, st, acc, s_join, [](int n, int lane16) { return n * 16 + lane16; });
 }

@@ -76,7 +76,7 @@ struct AttnItem {
   int rt, split;       // row tile, split of its keys
   int nq;              // query tokens of the sequence
   int q0, k0, nk;      // its first query token, first key (or cache row), keys (rows)
-  int splits;
+  int splits, tiles;   // splits of its keys, and key tiles of each
   int64_t part;        // among the parts of all heads, where splits > 1
 };
 __device__ inline AttnItem attn_item(const AttnArgs& a, int item, int h) {
@@ -88,7 +88,8 @@ __device__ inline AttnItem attn_item(const AttnArgs& a, int item, int h) {
   p.k0 = seq_word(a.seq, w + 1);
   const int i = item - seq_word(a.seq, w + 2);
   p.splits = seq_word(a.seq, w + 3);
-  p.part = (int64_t)h * a.parts + seq_word(a.seq, w + 4) + i;
+  p.tiles = seq_word(a.seq, w + 4);
+  p.part = (int64_t)h * a.parts + seq_word(a.seq, w + 5) + i;
   p.rt = i / p.splits;
   p.split = i - p.rt * p.splits;
   p.nq = seq_word(a.seq, w + kAttnSeqWords) - p.q0;
