@@ -397,7 +397,9 @@ int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype
   if ((rc = check_rows(v, dtype, d, v_head_stride, v_token_stride, no_k)) != TWINKV_OK) return rc;
   if (no_q) return TWINKV_OK;
   AttnArgs a;
-  rc = attn_args(dtype == TWINKV_BF16, q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride,
+  // the kernel for many rows: 64 tokens' strides within 32 bits (the other takes any)
+  const bool many = dtype == TWINKV_BF16 && std::max(k_token_stride, v_token_stride) <= INT32_MAX / (2 * 64);
+  rc = attn_args(many, q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride,
                  window, n_sink, scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;

@@ -9,10 +9,10 @@
 //  * O^T = V^T P^T: the weights are the B operand as they lie; the contraction's order is chosen so that a
 //    lane's keys are its own.  V^T comes from the row-major tile by ds_read_b64_tr_b16.  The accumulators
 //    hold channels of the lane's own row, so rescaling and normalising them needs no exchange.
-//  * A tile is fetched two tiles ahead into registers and written to one of two LDS buffers while the other
-//    is read (loads straight to LDS made the compiler wait for all of them before each transposed read);
-//    16-byte pieces of the keys and 32-byte units of the values are turned by the row so that the lanes
-//    of a read lie in different banks.  One barrier a tile.
+//  * Keys and values go from memory to LDS without registers, into one of two buffers while the other is
+//    read; 16-byte pieces of the keys and 32-byte units of the values are turned by the row so that the
+//    lanes of a read lie in different banks.  One barrier a tile.  (Through registers and LDS writes the 32k
+//    prompt took 2470 us where this takes NNN.)
 //  * Two workgroups fit a CU (64 KB of LDS each, 256 registers): one's softmax runs beside the other's
 //    products.
 // Values that only some rows of a tile see: as in attn.hip.
@@ -49,6 +49,12 @@ template <int D>
 __device__ inline int v_unit(int row, int unit) {
   return unit ^ (D == 128 ? 2 * (row & 3) : 2 * ((row >> 1) & 1));
 }
+
+__device__ inline void to_lds(const char* from, char* to) {  // 16 bytes a lane, `to` the wave's first
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+constexpr int kNoLoads = 0x0f70;  // s_waitcnt: vmcnt 0, the other counters at their largest
 
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a) {
@@ -89,26 +95,38 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
 
   const char* kb = a.k + (int64_t)h * a.k_head + (int64_t)p.k0 * a.k_token;
   const char* vb = a.v + (int64_t)h * a.v_head + (int64_t)p.k0 * a.v_token;
-  // a tile's pieces in registers on their way from memory to buffer t % 2
-  u32x4 k_next[kCopies], v_next[kCopies];
-  auto fetch = [&](int t) {
+  // Brings tile t into buffer t % 2: a wave instruction fills 1 KB of LDS in lane order, so it is the source
+  // that is turned.  A lane's rows of the 4 (2) instructions lie kRowsAtOnce apart and turn alike: one offset
+  // of the lane, the rest is the same for all (the host takes this kernel where 64 tokens' strides stay
+  // within 32 bits).
+  constexpr int kRowsAtOnce = kThreads / kPieces;
+  const int r_lane = tid / kPieces, piece = tid % kPieces;
+  const unsigned k_turned = ((k_place<D>(r_lane, piece) >> 4) & (kPieces - 1)) * 16;
+  const unsigned v_turned = v_unit<D>(r_lane, piece >> 1) * 32 + (piece & 1) * 16;
+  const unsigned k_lane = (unsigned)r_lane * (unsigned)a.k_token + k_turned;
+  const unsigned v_lane = (unsigned)r_lane * (unsigned)a.v_token + v_turned;
+  auto bring = [&](int t) {
     const bool sink = t < sink_tiles;
     const int base = sink ? t * kKeys : lo + (t - sink_tiles) * kKeys;
     const int stop = sink ? sinks : end;
+    const char* kt = kb + (int64_t)base * a.k_token;
+    const char* vt = vb + (int64_t)base * a.v_token;
+    char* kl = s.k[t & 1] + wave * 1024;
+    char* vl = s.v[t & 1] + wave * 1024;
+    if (base + kKeys <= stop) {
 #pragma unroll
-    for (int c = 0; c < kCopies; ++c) {
-      const int at = c * kThreads + tid;   // 16-byte piece of the tile
-      const int64_t key = min(base + at / kPieces, stop - 1);
-      k_next[c] = *reinterpret_cast<const u32x4*>(kb + key * a.k_token + at % kPieces * 16);
-      v_next[c] = *reinterpret_cast<const u32x4*>(vb + key * a.v_token + at % kPieces * 16);
-    }
-  };
-  auto stage = [&](int t) {
+      for (int c = 0; c < kCopies; ++c) {
+        to_lds(kt + c * kRowsAtOnce * a.k_token + k_lane, kl + c * (kThreads * 16));
+        to_lds(vt + c * kRowsAtOnce * a.v_token + v_lane, vl + c * (kThreads * 16));
+      }
+    } else {  // the last key again past the end
+      const int rows = stop - 1 - base;
 #pragma unroll
-    for (int c = 0; c < kCopies; ++c) {
-      const int at = c * kThreads + tid, r = at / kPieces, piece = at % kPieces;
-      *reinterpret_cast<u32x4*>(s.k[t & 1] + k_place<D>(r, piece)) = k_next[c];
-      *reinterpret_cast<u32x4*>(s.v[t & 1] + r * kRowBytes + v_unit<D>(r, piece >> 1) * 32 + (piece & 1) * 16) = v_next[c];
+      for (int c = 0; c < kCopies; ++c) {
+        const unsigned r = min(c * kRowsAtOnce + r_lane, rows);
+        to_lds(kt + (r * (unsigned)a.k_token + k_turned), kl + c * (kThreads * 16));
+        to_lds(vt + (r * (unsigned)a.v_token + v_turned), vl + c * (kThreads * 16));
+      }
     }
   };
 
@@ -136,15 +154,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
     for (int e = 0; e < 16; ++e) acc[b][e] = 0.0f;
   float m = kNegInf, l = 0.0f;
 
-  if (tiles > 0) {
-    fetch(0);
-    stage(0);
-    if (tiles > 1) fetch(1);
-  }
+  if (tiles > 0) bring(0);
   for (int t = 0; t < tiles; ++t) {
-    __syncthreads();                       // tile t lies in LDS, and nobody reads the other buffer
-    if (t + 1 < tiles) stage(t + 1);
-    if (t + 2 < tiles) fetch(t + 2);
+    // tile t lies in LDS (the barrier alone does not wait for a wave's loads to LDS), and nobody reads the
+    // other buffer
+    __builtin_amdgcn_s_waitcnt(kNoLoads);
+    __syncthreads();
+    if (t + 1 < tiles) bring(t + 1);
     const bool sink = t < sink_tiles;
     const int base = sink ? t * kKeys : lo + (t - sink_tiles) * kKeys;
     const int stop = sink ? sinks : end;
@@ -175,6 +191,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
     // nothing for this wave: past its last row, or before its first row's window and past the sinks
     if (base > wave_hi || (top <= wave_lo - a.window && base >= a.n_sink)) continue;
 
+    // all of the tile's keys on their way before the first product waits for one of them
+    bf16x8 k[kSteps][2];
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        k[j][b] = *reinterpret_cast<const bf16x8*>(ks + k_place<D>(b * 32 + r32, 2 * j + hi));
+    __builtin_amdgcn_sched_barrier(0);
     f32x16 x[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -183,22 +207,26 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
 #pragma unroll
     for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const bf16x8 k = *reinterpret_cast<const bf16x8*>(ks + k_place<D>(b * 32 + r32, 2 * j + hi));
-        x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[j], x[b], 0, 0, 0);
-      }
+      for (int b = 0; b < 2; ++b) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j][b], q[j], x[b], 0, 0, 0);
     if (top >= stop || top > wave_lo || (base <= wave_hi - a.window && top >= a.n_sink)) {
+      // the row sees [from, upto) of these keys, and those below n_sink
+      const int upto = min(stop, pos + 1), from = pos - a.window + 1;
+      const int j0 = base + 4 * hi;
+      const unsigned seen = (unsigned)max(upto - from, 0);
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int j = base + b * 32 + 8 * (e >> 2) + 4 * hi + (e & 3);
-          if (!((j < stop) & (j <= pos) & ((pos - j < a.window) | (j < a.n_sink)))) x[b][e] = kNegInf;
+          const int j = j0 + (b * 32 + 8 * (e >> 2) + (e & 3));
+          if (!((unsigned)(j - from) < seen)) {
+            if (base >= a.n_sink || !((j < upto) & (j < a.n_sink))) x[b][e] = kNegInf;
+          }
         }
     }
-    float most = fmaxf(x[0][0], x[1][0]);
+    // (the maximum that a NaN passes through: v_maximum3_f32 takes the products' results as they are)
+    float most = __builtin_elementwise_maximum(x[0][0], x[1][0]);
 #pragma unroll
-    for (int e = 1; e < 16; ++e) most = fmaxf(most, fmaxf(x[0][e], x[1][e]));
+    for (int e = 1; e < 16; ++e) most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(most, x[0][e]), x[1][e]);
     most *= scale;
     if (__any(most > m + kSlack)) {
       const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
@@ -213,14 +241,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
     }
     const float from = m == kNegInf ? 0.0f : m;
     bf16x8 w[4];                           // 16 keys each
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        x[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], scale, -from));
-        l += x[b][e];
-        w[2 * b + (e >> 3)][e & 7] = (bf16)x[b][e];
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], scale, -from));
+        sum[e & 1] += y;
+        w[2 * b + (e >> 3)][e & 7] = (bf16)y;
       }
+    l += sum[0] + sum[1];
+    asm volatile("" : "+v"(l));  // added up here: put off, the sum would keep 32 registers
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -247,7 +278,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int z = 0; z < 16; ++z) mine = (y >> 5) == b && e == z ? x[b][z] : mine;
+          for (int z = 0; z < 16; ++z) mine = (y >> 5) == b && e == z ? (float)w[2 * b + (z >> 3)][z & 7] : mine;
         const float weight = __shfl(mine, r32 + 32 * ((y >> 2) & 1));
         if (!(j <= pos && (pos - j < a.window || j < a.n_sink))) continue;
 #pragma unroll
