@@ -12,7 +12,7 @@
 //  * Keys and values go from memory to LDS without registers, into one of two buffers while the other is
 //    read; 16-byte pieces of the keys and 32-byte units of the values are turned by the row so that the
 //    lanes of a read lie in different banks.  One barrier a tile.  (Through registers and LDS writes the 32k
-//    prompt took 2470 us where this takes NNN.)
+//    prompt took 2470 us where this takes 2240 us.)
 //  * Two workgroups fit a CU (64 KB of LDS each, 256 registers): one's softmax runs beside the other's
 //    products.
 // Values that only some rows of a tile see: as in attn.hip.
@@ -105,30 +105,48 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
   const unsigned v_turned = v_unit<D>(r_lane, piece >> 1) * 32 + (piece & 1) * 16;
   const unsigned k_lane = (unsigned)r_lane * (unsigned)a.k_token + k_turned;
   const unsigned v_lane = (unsigned)r_lane * (unsigned)a.v_token + v_turned;
+  // Where the next tile to bring lies; what is the same for all lanes stays out of the loop, whose scalar
+  // instructions are a good part of a wave's own time.
+  const int64_t k_tile = (int64_t)kKeys * a.k_token, v_tile = (int64_t)kKeys * a.v_token;
+  const int64_t k_step = (int64_t)kRowsAtOnce * a.k_token, v_step = (int64_t)kRowsAtOnce * a.v_token;
+  const char* k_from = sink_tiles > 0 ? kb : kb + (int64_t)lo * a.k_token;
+  const char* v_from = sink_tiles > 0 ? vb : vb + (int64_t)lo * a.v_token;
   auto bring = [&](int t) {
-    const bool sink = t < sink_tiles;
-    const int base = sink ? t * kKeys : lo + (t - sink_tiles) * kKeys;
-    const int stop = sink ? sinks : end;
-    const char* kt = kb + (int64_t)base * a.k_token;
-    const char* vt = vb + (int64_t)base * a.v_token;
     char* kl = s.k[t & 1] + wave * 1024;
     char* vl = s.v[t & 1] + wave * 1024;
-    if (base + kKeys <= stop) {
+    const bool sink_end = t == sink_tiles - 1;
+    if (t != tiles - 1 && !sink_end) {
 #pragma unroll
       for (int c = 0; c < kCopies; ++c) {
-        to_lds(kt + c * kRowsAtOnce * a.k_token + k_lane, kl + c * (kThreads * 16));
-        to_lds(vt + c * kRowsAtOnce * a.v_token + v_lane, vl + c * (kThreads * 16));
+        to_lds(k_from + c * k_step + k_lane, kl + c * (kThreads * 16));
+        to_lds(v_from + c * v_step + v_lane, vl + c * (kThreads * 16));
       }
     } else {  // the last key again past the end
-      const int rows = stop - 1 - base;
+      const int rows = (sink_end ? sinks - 1 : end - 1 - lo) % kKeys;
 #pragma unroll
       for (int c = 0; c < kCopies; ++c) {
         const unsigned r = min(c * kRowsAtOnce + r_lane, rows);
-        to_lds(kt + (r * (unsigned)a.k_token + k_turned), kl + c * (kThreads * 16));
-        to_lds(vt + (r * (unsigned)a.v_token + v_turned), vl + c * (kThreads * 16));
+        to_lds(k_from + (r * (unsigned)a.k_token + k_turned), kl + c * (kThreads * 16));
+        to_lds(v_from + (r * (unsigned)a.v_token + v_turned), vl + c * (kThreads * 16));
       }
     }
+    k_from = sink_end ? kb + (int64_t)lo * a.k_token : k_from + k_tile;
+    v_from = sink_end ? vb + (int64_t)lo * a.v_token : v_from + v_tile;
   };
+  // The window's tiles that rows at positions first .. last all see whole are a run, and so are the ones of
+  // which some of them sees anything (from key 0 there may be sinks: no tile is left out before it).
+  struct Run {
+    int from, to;
+  };
+  auto whole_of = [&](int first, int last) {
+    return Run{sink_tiles + max(last - a.window + 1 - lo + kKeys - 1, 0) / kKeys,
+               sink_tiles + max(first + 1 - lo, 0) / kKeys};
+  };
+  const Run all_see = whole_of(pos_lo, pos_hi), all = whole_of(wave_lo, wave_hi);
+  const Run some{lo == 0 ? 0 : sink_tiles + max(wave_lo - a.window + 1 - lo, 0) / kKeys,
+                 sink_tiles + max(wave_hi - lo + kKeys, 0) / kKeys};
+  auto base_of = [&](int t) { return t < sink_tiles ? t * kKeys : lo + (t - sink_tiles) * kKeys; };
+  auto stop_of = [&](int t) { return t < sink_tiles ? sinks : end; };
 
   // scale > 0 from here on: the sign goes to q.  0 (all weights alike) becomes as good as 0, so that masked
   // scores stay -inf.
@@ -161,20 +179,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
     __builtin_amdgcn_s_waitcnt(kNoLoads);
     __syncthreads();
     if (t + 1 < tiles) bring(t + 1);
-    const bool sink = t < sink_tiles;
-    const int base = sink ? t * kKeys : lo + (t - sink_tiles) * kKeys;
-    const int stop = sink ? sinks : end;
-    const int top = base + kKeys - 1;
     const char* ks = s.k[t & 1];
     char* vs = s.v[t & 1];
     bool bad = false;
-    if (top >= stop || top > pos_lo || (base <= pos_hi - a.window && top >= a.n_sink)) {
+    if (t < all_see.from || t >= all_see.to) {
       // some row does not see some key: values that are past the range or not finite become zeros
+      const int rows = stop_of(t) - base_of(t);
 #pragma unroll
       for (int c = 0; c < kCopies; ++c) {
         const int at = c * kThreads + tid;
         s16x8 x = *reinterpret_cast<const s16x8*>(vs + at * 16);
-        const bool out = base + at / kPieces >= stop;
+        const bool out = at / kPieces >= rows;
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -188,8 +203,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
       __syncthreads();
       bad = s.bad == t;
     }
-    // nothing for this wave: past its last row, or before its first row's window and past the sinks
-    if (base > wave_hi || (top <= wave_lo - a.window && base >= a.n_sink)) continue;
+    if (t >= sink_tiles && (t < some.from || t >= some.to)) continue;  // nothing for this wave's rows
 
     // all of the tile's keys on their way before the first product waits for one of them
     bf16x8 k[kSteps][2];
@@ -208,7 +222,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
     for (int j = 0; j < kSteps; ++j)
 #pragma unroll
       for (int b = 0; b < 2; ++b) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j][b], q[j], x[b], 0, 0, 0);
-    if (top >= stop || top > wave_lo || (base <= wave_hi - a.window && top >= a.n_sink)) {
+    if (t < all.from || t >= all.to) {
+      const int base = base_of(t), stop = stop_of(t);
       // the row sees [from, upto) of these keys, and those below n_sink
       const int upto = min(stop, pos + 1), from = pos - a.window + 1;
       const int j0 = base + 4 * hi;
@@ -270,6 +285,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
       }
     if (bad) {
       // the values that are not finite, to the rows that see them
+      const int base = base_of(t), stop = stop_of(t);
       for (int y = 0; y < kKeys; ++y) {
         const int j = base + y;
         if (j >= stop) break;
