@@ -156,70 +156,92 @@ void set_rows(Cache4Args& a, const void* keys, const void* values, int dtype, in
 
 // ---- attention ----
 
-// How a call's rows and keys are cut into items (attn.hip, attn4.hip).
+// How a call's rows and keys are cut into items (attn.hip, attn4.hip, attn_rows.hip).
 struct AttnPlan {
   int64_t window = 0, n_sink = 0;
-  int rows = kAttnRows;          // of a tile
-  int split_tiles = 0;           // the most of a split
-  int64_t items = 0, parts = 0;  // per head
+  int rows = kAttnRows, keys = kAttnTile;  // of a tile
+  int64_t split_tiles = 0;                 // the most key tiles of a split
+  int64_t items = 0, parts = 0;            // per head
 };
 
-int64_t row_tiles(int64_t nq, int group, int rows) { return (nq * group + rows - 1) / rows; }
+int64_t row_tiles(int64_t nq, int group, const AttnPlan& p) { return (nq * group + p.rows - 1) / p.rows; }
 
 // The most key tiles a row tile of the sequence goes through.
 int64_t key_tiles(int64_t nq, int64_t nk, int group, const AttnPlan& p) {
   const int64_t queries = std::min<int64_t>(nq, p.rows / group + 2);
   const int64_t near = std::min(nk, p.window + queries), sinks = std::min(nk, p.n_sink);
-  const int64_t apart = (near + kAttnTile - 1) / kAttnTile + (sinks + kAttnTile - 1) / kAttnTile;
-  return std::min(apart, (nk + kAttnTile - 1) / kAttnTile) + 1;
+  const int64_t apart = (near + p.keys - 1) / p.keys + (sinks + p.keys - 1) / p.keys;
+  return std::min(apart, (nk + p.keys - 1) / p.keys) + 1;
 }
 
-// A sequence's splits, of at most `most` tiles each, as equal as whole rounds of the 4 waves make them.
+// A sequence's splits, of at most `most` tiles each, as equal as whole rounds of 4 tiles (the waves of
+// the kernels for few rows) make them.
 struct Splits {
   int64_t n, tiles;
 };
-Splits splits_of(int64_t tiles, int most) {
-  int64_t n = std::max<int64_t>(1, (tiles + most - 1) / most);
+Splits splits_of(int64_t tiles, int64_t most) {
+  const int64_t n = std::max<int64_t>(1, (tiles + most - 1) / most);
   const int64_t each = ((tiles + n - 1) / n + 3) / 4 * 4;
   return Splits{std::max<int64_t>(1, (tiles + each - 1) / each), each};
 }
 
-// Items go to workgroups of 4 waves; the whole work is cut into about kItems of them, a split no shorter than
-// two tiles a wave.
-constexpr int64_t kItems = 512;
+// Row tiles of all heads, key tiles that they go through, and the most that one does.
+struct AttnWork {
+  int64_t rows = 0, tiles = 0, longest = 0;
+};
+AttnWork work_of(int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, const AttnPlan& p) {
+  AttnWork w;
+  for (int s = 0; s < n_seqs; ++s) {
+    const int64_t nq = cu_q[s + 1] - cu_q[s];
+    if (nq == 0) continue;
+    const int64_t rows = n_heads * row_tiles(nq, group, p), keys = key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p);
+    w.rows += rows;
+    w.tiles += rows * keys;
+    w.longest = std::max(w.longest, keys);
+  }
+  return w;
+}
 
-// Rows that a sequence has in the mean from which the kernel for many of them is taken.
-constexpr int64_t kManyRows = 64;
+// The whole work is cut into about kItems workgroups, two a CU: decoding over 64 caches of 1k to 4k rows is at the
+// copy rate so, and 20% slower with twice as many and their join.
+constexpr int64_t kItems = 512;
+// A split has at least two tiles a wave; in the kernel for many rows, whose parts are larger, 1024 keys (a prompt
+// of 512 tokens, 8 heads of 4: 18 us unsplit, 34 in splits of 512 keys), and only where it would leave CUs
+// without work.
+constexpr int64_t kLeast = 8, kLeastBig = 16, kCus = 256;
+// The kernel for many rows is taken for more rows than one tile of the other has, if it need not split the
+// keys or there is enough work (in 16 rows x 32 keys).  Few rows / many, us, 8 heads, d 128: 64 rows over 4k keys 25 /
+// 42, 256 38 / 56, 512 60 / 58, 2048 155 / 67; 64 over 32k 57 / 40, 2048 1145 / 298; 16 sequences of 32 rows over
+// 4k keys 96 / 57; prompts of 512 tokens, 4 rows a token, 30 / 18, of 64 tokens 8.7 / 8.5.
+constexpr int64_t kMuchWork = 20480;
 
 // many: whether there is a kernel for many rows.
 int attn_plan(bool many, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
               int64_t n_sink, AttnPlan& p) {
   p.window = std::min<int64_t>(window, kAttnMaxKeys);
   p.n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
+  const AttnWork few = work_of(n_heads, group, n_seqs, cu_q, cu_k, p);
+  int64_t each = std::max(kLeast, (few.tiles + kItems - 1) / kItems);
   if (many) {
+    AttnPlan big = p;
+    big.rows = kAttnBigRows;
+    big.keys = kAttnBigTile;
+    const AttnWork w = work_of(n_heads, group, n_seqs, cu_q, cu_k, big);
     int64_t live = 0;
     for (int s = 0; s < n_seqs; ++s) live += cu_q[s + 1] > cu_q[s];
-    if (cu_q[n_seqs] * group >= kManyRows * live) {
-      p.rows = kAttnBigRows;
-      p.split_tiles = kAttnMaxKeys / 64;
-      for (int s = 0; s < n_seqs; ++s) p.items += row_tiles(cu_q[s + 1] - cu_q[s], group, p.rows);
-      return grid_ok(p.items * n_heads, 256) ? TWINKV_OK : TWINKV_E_ARG;
+    if (cu_q[n_seqs] * group > kAttnRows * live && (few.tiles >= kMuchWork || w.longest <= kLeastBig)) {
+      p = big;
+      each = w.rows >= kCus ? kAttnMaxKeys : std::max(kLeastBig, (w.tiles + kItems - 1) / kItems);
     }
   }
-  int64_t work = 0;  // key tiles, over all heads
-  for (int s = 0; s < n_seqs; ++s) {
-    const int64_t nq = cu_q[s + 1] - cu_q[s];
-    work += n_heads * row_tiles(nq, group, p.rows) * key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p);
-  }
-  const int64_t each = std::max<int64_t>(8, (work + kItems - 1) / kItems);
-  p.split_tiles = (int)std::min<int64_t>((each + 3) / 4 * 4, kAttnMaxKeys / 64);
+  p.split_tiles = (std::min<int64_t>(each, kAttnMaxKeys / 64) + 3) / 4 * 4;
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t nq = cu_q[s + 1] - cu_q[s];
     const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles).n;
-    p.items += row_tiles(nq, group, p.rows) * splits;
-    if (splits > 1) p.parts += row_tiles(nq, group, p.rows) * splits;
+    p.items += row_tiles(nq, group, p) * splits;
+    if (splits > 1) p.parts += row_tiles(nq, group, p) * splits;
   }
-  return grid_ok(p.items, 256) ? TWINKV_OK : TWINKV_E_ARG;
+  return grid_ok(p.items * (p.rows == kAttnRows ? 1 : n_heads), 256) ? TWINKV_OK : TWINKV_E_ARG;
 }
 
 struct AttnLayout {
@@ -228,7 +250,7 @@ struct AttnLayout {
 AttnLayout attn_layout(const AttnPlan& p, int d, int n_heads, int n_seqs) {
   AttnLayout L;
   size_t off = words_bytes(n_seqs, kAttnSeqWords);
-  const size_t rows = (size_t)n_heads * (size_t)p.parts * kAttnRows;
+  const size_t rows = (size_t)n_heads * (size_t)p.parts * (size_t)p.rows;
   L.part_o = off;
   off = align_up(off + 4 * rows * (size_t)d);
   L.part_ml = off;
@@ -292,8 +314,8 @@ int attn_args(bool many, const void* q, int dtype, int d, int n_heads, int group
     int64_t tiles = 0;
     if (s < n_seqs) {
       const int64_t nq = cu_q[s + 1] - cu_q[s];
-      tiles = row_tiles(nq, group, p.rows);
-      if (p.rows == kAttnRows) splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
+      tiles = row_tiles(nq, group, p);
+      splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
     }
     w.put((int32_t)cu_q[s]);
     w.put((int32_t)cu_k[s]);
@@ -409,8 +431,7 @@ int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype
   a.k_token = k_token_stride * esz;
   a.v_head = v_head_stride * esz;
   a.v_token = v_token_stride * esz;
-  if (a.rows == kAttnBigRows) return hip_status(launch_attn_rows(a, d, stream));
-  const int e = launch_attn(a, dtype, d, stream);
+  const int e = a.rows == kAttnBigRows ? launch_attn_rows(a, d, stream) : launch_attn(a, dtype, d, stream);
   if (e != 0 || a.parts == 0) return hip_status(e);
   return hip_status(launch_attn_join(a, dtype, d, stream));
 }

@@ -79,7 +79,8 @@ int launch_cache4_read(const Cache4Args& a, int dtype, int d, void* stream);
 constexpr int kAttnSeqWords = 6;
 constexpr int kAttnTile = 32;        // keys of a tile
 constexpr int kAttnRows = 16;        // rows of a tile
-constexpr int kAttnBigRows = 128;    // of the kernel for many rows, which splits no keys
+constexpr int kAttnBigRows = 128;    // rows and keys of the kernel for many rows
+constexpr int kAttnBigTile = 64;
 constexpr int kAttnMaxKeys = 1 << 30;  // of all sequences: positions and windows add without overflow
 struct AttnArgs {
   SeqWords seq;
@@ -97,11 +98,11 @@ struct AttnArgs {
   int n_heads, group, n_seqs;
   int items, parts;      // per head
   int rows;              // of a tile: kAttnRows or kAttnBigRows
-  float* part_o;         // [n_heads][parts][kAttnRows][d] unnormalised sums
-  float* part_ml;        // [n_heads][parts][kAttnRows][2] maximum (log2 units) and sum
+  float* part_o;         // [n_heads][parts][rows][d] unnormalised sums
+  float* part_ml;        // [n_heads][parts][rows][2] maximum (log2 units) and sum
 };
 int launch_attn(const AttnArgs& a, int dtype, int d, void* stream);
-// bf16; items of kAttnBigRows rows, one split each
+// bf16
 int launch_attn_rows(const AttnArgs& a, int d, void* stream);
 int launch_attn4(const AttnArgs& a, int dtype, int d, void* stream);
 int launch_attn_join(const AttnArgs& a, int dtype, int d, void* stream);

@@ -194,28 +194,27 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4
 }
 
 // The join: a row tile's parts brought to one maximum.  The tile's items share its rows out among them (item
-// `split` takes rows split, split + splits, ...); the threads of a workgroup take 8 channels and every kLanes-th
-// part each, and add up through LDS.
+// `split` takes rows split, split + splits, ...).  Of a workgroup, D / 8 threads make a team that holds a row's
+// channels; as many teams as there are parts (a power of two, at most all of them) work on one row and add up
+// through LDS, the others on the next rows.
 constexpr int kJoinThreads = 256;
 template <typename T, int D>
 __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(const AttnArgs a) {
-  constexpr int kPieces = D / 8, kLanes = kJoinThreads / kPieces;
-  __shared__ float s_o[kLanes][D];
-  __shared__ float s_ml[kLanes][2];
+  constexpr int kPieces = D / 8, kTeams = kJoinThreads / kPieces;
+  __shared__ float s_o[kTeams][D];
+  __shared__ float s_ml[kTeams][2];
   const AttnItem p = attn_item(a, (int)blockIdx.x, (int)blockIdx.y);
   if (p.splits <= 1) return;
-  const int c = threadIdx.x % kPieces * 8, sl = threadIdx.x / kPieces;
-  for (int r = p.split; r < kAttnRows; r += p.splits) {
-    const int row = p.rt * kAttnRows + r;
-    if (row >= p.nq * a.group) break;
-    const int64_t part = (p.part - p.split) * kAttnRows + r;  // of split 0
-    const float* ml = a.part_ml + part * 2;
-    const float* o = a.part_o + part * D + c;
+  const int c = threadIdx.x % kPieces * 8, team = threadIdx.x / kPieces;
+  int per_row = 1;
+  while (per_row < kTeams && per_row < p.splits) per_row *= 2;
+  const int first = team & (per_row - 1), slot = team / per_row;  // part to begin with, row of those at hand
+  const int rows = a.rows, n_rows = p.nq * a.group, at_once = kTeams / per_row;
+  for (int r0 = p.split; r0 < rows && p.rt * rows + r0 < n_rows; r0 += at_once * p.splits) {
+    const int r = r0 + slot * p.splits, row = p.rt * rows + r;
+    const bool live = r < rows && row < n_rows;
     float top = kNegInf, sum = 0.0f, f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = sl; k < p.splits; k += kLanes) {
-      const float m = ml[(int64_t)k * kAttnRows * 2], l = ml[(int64_t)k * kAttnRows * 2 + 1];
-      float x[8];
-      load8(o + (int64_t)k * kAttnRows * D, x);
+    auto add = [&](float m, float l, const float (&x)[8]) {
       const float next = fmaxf(top, m);
       const float u = next == top ? 1.0f : __builtin_amdgcn_exp2f(top - next);
       const float w = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
@@ -223,36 +222,44 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(const AttnArgs 
       sum = sum * u + l * w;
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = f[e] * u + x[e] * w;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s_o[sl][c + e] = f[e];
-    if (c == 0) {
-      s_ml[sl][0] = top;
-      s_ml[sl][1] = sum;
-    }
-    __syncthreads();
-    if (threadIdx.x < kPieces) {
-      const int lanes = min(kLanes, p.splits);
-      for (int k = 1; k < lanes; ++k) {  // f, top and sum are lane 0's so far
-        const float m = s_ml[k][0], l = s_ml[k][1];
-        const float next = fmaxf(top, m);
-        const float u = next == top ? 1.0f : __builtin_amdgcn_exp2f(top - next);
-        const float w = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
-        top = next;
-        sum = sum * u + l * w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = f[e] * u + s_o[k][c + e] * w;
+    };
+    if (live) {
+      const int64_t part = (p.part - p.split) * rows + r;  // of split 0
+      const float* ml = a.part_ml + part * 2;
+      const float* o = a.part_o + part * D + c;
+      for (int k = first; k < p.splits; k += per_row) {
+        float x[8];
+        load8(o + (int64_t)k * rows * D, x);
+        add(ml[(int64_t)k * rows * 2], ml[(int64_t)k * rows * 2 + 1], x);
       }
-      const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] *= inv;
-      const int i = row / a.group, g = row - i * a.group;
-      const int64_t head = (int64_t)p.h * a.group + g;
-      Vec8<T>::from(f).store(a.out + head * a.o_head + (int64_t)(p.q0 + i) * a.o_token + c * (int)sizeof(T));
-      if (a.lse != nullptr && c == 0)
-        a.lse[head * a.Tq + p.q0 + i] = sum == 0.0f ? kNegInf : top * 0.69314718055994530942f + logf(sum);
     }
-    __syncthreads();
+    if (per_row > 1) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s_o[team][c + e] = f[e];
+      if (c == 0) {
+        s_ml[team][0] = top;
+        s_ml[team][1] = sum;
+      }
+      __syncthreads();
+      if (first == 0) {
+        for (int k = 1; k < per_row; ++k) {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = s_o[team + k][c + e];
+          add(s_ml[team + k][0], s_ml[team + k][1], x);
+        }
+      }
+      __syncthreads();
+    }
+    if (!live || first != 0) continue;
+    const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= inv;
+    const int i = row / a.group, g = row - i * a.group;
+    const int64_t head = (int64_t)p.h * a.group + g;
+    Vec8<T>::from(f).store(a.out + head * a.o_head + (int64_t)(p.q0 + i) * a.o_token + c * (int)sizeof(T));
+    if (a.lse != nullptr && c == 0)
+      a.lse[head * a.Tq + p.q0 + i] = sum == 0.0f ? kNegInf : top * 0.69314718055994530942f + logf(sum);
   }
 }
 

@@ -13,6 +13,7 @@
 //    read; 16-byte pieces of the keys and 32-byte units of the values are turned by the row so that the
 //    lanes of a read lie in different banks.  One barrier a tile.  (Through registers and LDS writes the 32k
 //    prompt took 2470 us where this takes 2240 us.)
+//  * With too few row tiles for the machine a tile's keys are split over workgroups and joined (attn4.hip).
 //  * Two workgroups fit a CU (64 KB of LDS each, 256 registers): one's softmax runs beside the other's
 //    products.
 // Values that only some rows of a tile see: as in attn.hip.
@@ -29,7 +30,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 constexpr int kThreads = 256;
 constexpr int kWaveRows = 32;
 constexpr int kRows = kAttnBigRows;
-constexpr int kKeys = 64;  // of a tile
+constexpr int kKeys = kAttnBigTile;
 static_assert(kRows == kThreads / 64 * kWaveRows, "a wave owns 32 rows");
 
 template <int D>
@@ -84,7 +85,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
     if (sinks > 0) lo = 0;
     sink_tiles = 0;
   }
-  const int tiles = sink_tiles + (end - lo + kKeys - 1) / kKeys;
+  // this item's tiles of them
+  const int all_tiles = sink_tiles + (end - lo + kKeys - 1) / kKeys;
+  const int first = p.split * p.tiles, tiles = min(all_tiles, first + p.tiles);
   // this lane's row; rows past the problem's repeat its last, and are not written
   const int row = min(row0 + wave * kWaveRows + r32, n_rows - 1);
   const int query = row / a.group;
@@ -109,13 +112,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
   // instructions are a good part of a wave's own time.
   const int64_t k_tile = (int64_t)kKeys * a.k_token, v_tile = (int64_t)kKeys * a.v_token;
   const int64_t k_step = (int64_t)kRowsAtOnce * a.k_token, v_step = (int64_t)kRowsAtOnce * a.v_token;
-  const char* k_from = sink_tiles > 0 ? kb : kb + (int64_t)lo * a.k_token;
-  const char* v_from = sink_tiles > 0 ? vb : vb + (int64_t)lo * a.v_token;
+  auto base_of = [&](int t) { return t < sink_tiles ? t * kKeys : lo + (t - sink_tiles) * kKeys; };
+  auto stop_of = [&](int t) { return t < sink_tiles ? sinks : end; };
+  const char* k_from = kb + (int64_t)base_of(first) * a.k_token;
+  const char* v_from = vb + (int64_t)base_of(first) * a.v_token;
   auto bring = [&](int t) {
     char* kl = s.k[t & 1] + wave * 1024;
     char* vl = s.v[t & 1] + wave * 1024;
     const bool sink_end = t == sink_tiles - 1;
-    if (t != tiles - 1 && !sink_end) {
+    if (t != all_tiles - 1 && !sink_end) {
 #pragma unroll
       for (int c = 0; c < kCopies; ++c) {
         to_lds(k_from + c * k_step + k_lane, kl + c * (kThreads * 16));
@@ -145,8 +150,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
   const Run all_see = whole_of(pos_lo, pos_hi), all = whole_of(wave_lo, wave_hi);
   const Run some{lo == 0 ? 0 : sink_tiles + max(wave_lo - a.window + 1 - lo, 0) / kKeys,
                  sink_tiles + max(wave_hi - lo + kKeys, 0) / kKeys};
-  auto base_of = [&](int t) { return t < sink_tiles ? t * kKeys : lo + (t - sink_tiles) * kKeys; };
-  auto stop_of = [&](int t) { return t < sink_tiles ? sinks : end; };
 
   // scale > 0 from here on: the sign goes to q.  0 (all weights alike) becomes as good as 0, so that masked
   // scores stay -inf.
@@ -172,8 +175,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
     for (int e = 0; e < 16; ++e) acc[b][e] = 0.0f;
   float m = kNegInf, l = 0.0f;
 
-  if (tiles > 0) bring(0);
-  for (int t = 0; t < tiles; ++t) {
+  if (first < tiles) bring(first);
+  for (int t = first; t < tiles; ++t) {
     // tile t lies in LDS (the barrier alone does not wait for a wave's loads to LDS), and nobody reads the
     // other buffer
     __builtin_amdgcn_s_waitcnt(kNoLoads);
@@ -313,8 +316,23 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
     const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(two[0]) + __uint_as_float(two[1]);
   }
-  const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
   if (row0 + wave * kWaveRows + r32 >= n_rows) return;
+  if (p.splits > 1) {
+    const int64_t part = p.part * kRows + wave * kWaveRows + r32;
+    float* to = a.part_o + part * D;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        *reinterpret_cast<f32x4*>(to + 32 * b + 8 * y + 4 * hi) =
+            f32x4{acc[b][4 * y], acc[b][4 * y + 1], acc[b][4 * y + 2], acc[b][4 * y + 3]};
+    if (hi == 0) {
+      a.part_ml[part * 2] = m;
+      a.part_ml[part * 2 + 1] = l;
+    }
+    return;
+  }
+  const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
   const int64_t head = (int64_t)h * a.group + (row - query * a.group);
   char* out = a.out + head * a.o_head + (int64_t)(p.q0 + query) * a.o_token;
 #pragma unroll
