@@ -161,6 +161,7 @@ struct AttnPlan {
   int64_t window = 0, n_sink = 0;
   int rows = kAttnRows, keys = kAttnTile;  // of a tile
   int64_t split_tiles = 0;                 // the most key tiles of a split
+  int64_t whole_tiles = 0;                 // up to so many are not split
   int64_t items = 0, parts = 0;            // per head
 };
 
@@ -174,13 +175,13 @@ int64_t key_tiles(int64_t nq, int64_t nk, int group, const AttnPlan& p) {
   return std::min(apart, (nk + p.keys - 1) / p.keys) + 1;
 }
 
-// A sequence's splits, of at most `most` tiles each, as equal as whole rounds of 4 tiles (the waves of
+// A sequence's splits, of at most split_tiles tiles each, as equal as whole rounds of 4 tiles (the waves of
 // the kernels for few rows) make them.
 struct Splits {
   int64_t n, tiles;
 };
-Splits splits_of(int64_t tiles, int64_t most) {
-  const int64_t n = std::max<int64_t>(1, (tiles + most - 1) / most);
+Splits splits_of(int64_t tiles, const AttnPlan& p) {
+  const int64_t n = tiles <= p.whole_tiles ? 1 : (tiles + p.split_tiles - 1) / p.split_tiles;
   const int64_t each = ((tiles + n - 1) / n + 3) / 4 * 4;
   return Splits{std::max<int64_t>(1, (tiles + each - 1) / each), each};
 }
@@ -205,43 +206,66 @@ AttnWork work_of(int n_heads, int group, int n_seqs, const int64_t* cu_q, const 
 // The whole work is cut into about kItems workgroups, two a CU: decoding over 64 caches of 1k to 4k rows is at the
 // copy rate so, and 20% slower with twice as many and their join.
 constexpr int64_t kItems = 512;
-// A split has at least two tiles a wave; in the kernel for many rows, whose parts are larger, 1024 keys (a prompt
-// of 512 tokens, 8 heads of 4: 18 us unsplit, 34 in splits of 512 keys), and only where it would leave CUs
-// without work.
-constexpr int64_t kLeast = 8, kLeastBig = 16, kCus = 256;
+// A split has at least two tiles a wave (8 heads of 4, one query over 4k keys 15.6 us, with twice that 18.5).  The
+// 4-bit kernel takes a tile in less time than its join does: 4 a wave, and up to 8 a wave are not split
+// (512 cached rows 8.1 us, split 10.3; 8k rows 13.3 / 14.7).  In the kernel for many rows, whose parts are larger, a
+// split has 1024 keys (a prompt of 512 tokens: 18 us unsplit, 34 in splits of 512 keys), and there is one
+// only where tiles of rows would leave CUs without work.
+constexpr int64_t kLeast = 8, kLeastCached = 16, kWholeCached = 32, kLeastBig = 16, kCus = 256;
 // The kernel for many rows is taken for more rows than one tile of the other has, if it need not split the
 // keys or there is enough work (in 16 rows x 32 keys).  Few rows / many, us, 8 heads, d 128: 64 rows over 4k keys 25 /
 // 42, 256 38 / 56, 512 60 / 58, 2048 155 / 67; 64 over 32k 57 / 40, 2048 1145 / 298; 16 sequences of 32 rows over
 // 4k keys 96 / 57; prompts of 512 tokens, 4 rows a token, 30 / 18, of 64 tokens 8.7 / 8.5.
 constexpr int64_t kMuchWork = 20480;
 
-// many: whether there is a kernel for many rows.
-int attn_plan(bool many, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
+// What a call's keys are: rows of any kind, rows that the kernel for many rows takes too, fp32 rows, a 4-bit
+// cache.
+enum class KeysAre { kRows, kRowsOfMany, kRowsFp32, kCached };
+
+int64_t live_of(int n_seqs, const int64_t* cu_q) {  // sequences with queries
+  int64_t n = 0;
+  for (int s = 0; s < n_seqs; ++s) n += cu_q[s + 1] > cu_q[s];
+  return n;
+}
+
+// fp32: with so many row tiles (of all heads) and at most so many key tiles the waves of a workgroup take a row
+// tile each, and their join falls away.  Shared / own, us, 8 heads of 4, d 128, window 128: 256 tokens (512 row tiles)
+// 20 / 27, 512 40 / 30, 2048 143 / 86; plain causal, 512 tokens (17 key tiles) 60 / 50, 1024 (33) 155 / 207.
+constexpr int64_t kWideRows = 768, kWideTiles = 20;
+
+int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
               int64_t n_sink, AttnPlan& p) {
   p.window = std::min<int64_t>(window, kAttnMaxKeys);
   p.n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
   const AttnWork few = work_of(n_heads, group, n_seqs, cu_q, cu_k, p);
-  int64_t each = std::max(kLeast, (few.tiles + kItems - 1) / kItems);
-  if (many) {
+  const bool cached = keys == KeysAre::kCached;
+  int64_t each = std::max(cached ? kLeastCached : kLeast, (few.tiles + kItems - 1) / kItems);
+  p.whole_tiles = cached ? kWholeCached : kLeast;
+  if (keys == KeysAre::kRowsOfMany) {
     AttnPlan big = p;
     big.rows = kAttnBigRows;
     big.keys = kAttnBigTile;
     const AttnWork w = work_of(n_heads, group, n_seqs, cu_q, cu_k, big);
-    int64_t live = 0;
-    for (int s = 0; s < n_seqs; ++s) live += cu_q[s + 1] > cu_q[s];
-    if (cu_q[n_seqs] * group > kAttnRows * live && (few.tiles >= kMuchWork || w.longest <= kLeastBig)) {
+    if (cu_q[n_seqs] * group > kAttnRows * live_of(n_seqs, cu_q) && (few.tiles >= kMuchWork || w.longest <= kLeastBig)) {
       p = big;
+      p.whole_tiles = kLeastBig;
       each = w.rows >= kCus ? kAttnMaxKeys : std::max(kLeastBig, (w.tiles + kItems - 1) / kItems);
     }
+  }
+  if (keys == KeysAre::kRowsFp32 && few.rows >= kWideRows && few.longest <= kWideTiles &&
+      cu_q[n_seqs] * group > kAttnRows * live_of(n_seqs, cu_q)) {
+    p.rows = kAttnWideRows;
+    each = kAttnMaxKeys;
+    p.whole_tiles = kAttnMaxKeys;
   }
   p.split_tiles = (std::min<int64_t>(each, kAttnMaxKeys / 64) + 3) / 4 * 4;
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t nq = cu_q[s + 1] - cu_q[s];
-    const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles).n;
+    const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p).n;
     p.items += row_tiles(nq, group, p) * splits;
     if (splits > 1) p.parts += row_tiles(nq, group, p) * splits;
   }
-  return grid_ok(p.items * (p.rows == kAttnRows ? 1 : n_heads), 256) ? TWINKV_OK : TWINKV_E_ARG;
+  return grid_ok(p.items * (p.rows == kAttnBigRows ? n_heads : 1), 256) ? TWINKV_OK : TWINKV_E_ARG;
 }
 
 struct AttnLayout {
@@ -272,12 +296,12 @@ int check_queries(int n_seqs, const int64_t* cu_q, int group) {
 }
 
 // The queries' and outputs' side of a call, the plan, the words and the parts.
-int attn_args(bool many, const void* q, int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q,
+int attn_args(KeysAre keys, const void* q, int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q,
               const int64_t* cu_k, int64_t q_head_stride, int64_t q_token_stride, int64_t window, int64_t n_sink,
               float scale, void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse,
               void* workspace, int64_t workspace_bytes, void* stream, AttnArgs& a) {
   AttnPlan p;
-  const int rc = attn_plan(many, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+  const int rc = attn_plan(keys, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
   if (rc != TWINKV_OK) return rc;
   const AttnLayout L = attn_layout(p, d, n_heads, n_seqs);
   if (L.total > 0 && (workspace == nullptr || workspace_bytes < (int64_t)L.total)) return TWINKV_E_WORKSPACE;
@@ -315,7 +339,7 @@ int attn_args(bool many, const void* q, int dtype, int d, int n_heads, int group
     if (s < n_seqs) {
       const int64_t nq = cu_q[s + 1] - cu_q[s];
       tiles = row_tiles(nq, group, p);
-      splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p.split_tiles);
+      splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p);
     }
     w.put((int32_t)cu_q[s]);
     w.put((int32_t)cu_k[s]);
@@ -390,9 +414,9 @@ int64_t twinkv_attention_workspace_bytes(int dtype, int d, int n_heads, int grou
   if (rc == TWINKV_OK && (window < 0 || n_sink < 0)) rc = TWINKV_E_ARG;
   if (rc != TWINKV_OK) return -rc;
   int64_t most = 0;  // of the plans that the two calls may make
-  for (const bool many : {false, true}) {
+  for (const KeysAre keys : {KeysAre::kRows, KeysAre::kCached, dtype == TWINKV_BF16 ? KeysAre::kRowsOfMany : KeysAre::kRowsFp32}) {
     AttnPlan p;
-    rc = attn_plan(many && dtype == TWINKV_BF16, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+    rc = attn_plan(keys, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
     if (rc != TWINKV_OK) return -rc;
     most = std::max(most, (int64_t)attn_layout(p, d, n_heads, n_seqs).total);
   }
@@ -420,9 +444,11 @@ int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype
   if (no_q) return TWINKV_OK;
   AttnArgs a;
   // the kernel for many rows: 64 tokens' strides within 32 bits (the other takes any)
-  const bool many = dtype == TWINKV_BF16 && std::max(k_token_stride, v_token_stride) <= INT32_MAX / (2 * 64);
-  rc = attn_args(many, q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride,
-                 window, n_sink, scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
+  const KeysAre keys = dtype != TWINKV_BF16 ? KeysAre::kRowsFp32
+                       : std::max(k_token_stride, v_token_stride) <= INT32_MAX / (2 * 64) ? KeysAre::kRowsOfMany
+                                                                                         : KeysAre::kRows;
+  rc = attn_args(keys, q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride, window, n_sink,
+                 scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
   a.k = static_cast<const char*>(k);
@@ -530,7 +556,7 @@ int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* 
   if (len == nullptr) return TWINKV_E_NULL;
   if (no_q) return TWINKV_OK;
   AttnArgs a;
-  rc = attn_args(false, q, dtype, d, cache->n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride,
+  rc = attn_args(KeysAre::kCached, q, dtype, d, cache->n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride,
                  INT64_MAX, 0, scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   a.cache = device_cache(cache);

@@ -6,7 +6,8 @@
 // wave's own LDS and comes back transposed (ds_read_b64_tr_b16: 4 tokens of a channel to a lane); units of
 // 32 bytes are rotated by the row so that the 4 rows such a read touches lie in different banks.
 // Nothing of it is shared between waves, so there is no barrier in the loop.  HBM- or L2-bound.
-// fp32: v_mfma_f32_16x16x4_f32, whose operands are single values a lane: keys and values both come
+// fp32: with many rows and few keys the waves take a row tile each instead (no join).
+// v_mfma_f32_16x16x4_f32, whose operands are single values a lane: keys and values both come
 // straight from memory, 16 bytes a lane, the contraction's and the channels' order chosen to fit.  Bound
 // by that instruction's rate with many rows.
 //
@@ -220,21 +221,24 @@ struct Tile<float, D> {
   }
 };
 
-template <typename T, int D>
+// kOnRows: the four waves take four row tiles, each over all of its keys, instead of sharing one tile's keys.
+template <typename T, int D, bool kOnRows>
 __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(const AttnArgs a) {
   typedef Tile<T, D> Keys;
   __shared__ __attribute__((aligned(16))) char s_values[kAttnWaves][Keys::kLds];
-  __shared__ float s_join[join_floats<D>()];
+  __shared__ float s_join[kOnRows ? kAttnWaves * own_floats<D>() : join_floats<D>()];
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const AttnItem p = attn_item(a, (int)blockIdx.x, (int)blockIdx.y);
-  const int n_rows = p.nq * a.group, row0 = p.rt * kAttnRows;
+  const int n_rows = p.nq * a.group, row0 = kOnRows ? (p.rt * kAttnWaves + wave) * kAttnRows : p.rt * kAttnRows;
+  if (kOnRows && row0 >= n_rows) return;
   const int last = min(row0 + kAttnRows, n_rows) - 1;
   const int row = min(row0 + i, n_rows - 1);  // rows past the problem's repeat its last, and are not written
   const int query = row / a.group;
   const int pos = p.nk - p.nq + query;
   const Span sp = span_of(a, p, row0, last);
-  const int first = p.split * p.tiles + wave;
+  constexpr int kStep = kOnRows ? 1 : kAttnWaves;
+  const int first = p.split * p.tiles + (kOnRows ? 0 : wave);
   const int stop = min(sp.tiles, (p.split + 1) * p.tiles);
   const int window = a.window;
 
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(const AttnArgs a)
 #pragma unroll
   for (int n = 0; n < D / 16; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   Keys now;
-  for (int x = first; x < stop; x += kAttnWaves) {
+  for (int x = first; x < stop; x += kStep) {
     const bool sink = x < sp.sink_tiles;
     const int base = sink ? x * kAttnTile : sp.lo + (x - sp.sink_tiles) * kAttnTile;
     const int end = sink ? sp.sinks : sp.end;
@@ -296,12 +300,14 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(const AttnArgs a)
       }
     }
   }
-  join_waves<T, D>(a, p, row0, st, acc, s_join, [](int n, int lane16) { return Keys::channel(n, lane16); });
+  const auto channel = [](int n, int lane16) { return Keys::channel(n, lane16); };
+  if constexpr (kOnRows) write_own<T, D>(a, p, row0, st, acc, s_join + wave * own_floats<D>(), channel);
+  else join_waves<T, D>(a, p, row0, st, acc, s_join, channel);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kOnRows>
 int run(const AttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attn_kernel<T, D>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
+  hipLaunchKernelGGL((attn_kernel<T, D, kOnRows>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
   return hipGetLastError();
 }
 
@@ -309,8 +315,9 @@ int run(const AttnArgs& a, hipStream_t s) {
 
 int launch_attn(const AttnArgs& a, int dtype, int d, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == 0) return d == 128 ? run<bf16, 128>(a, s) : run<bf16, 64>(a, s);
-  return d == 128 ? run<float, 128>(a, s) : run<float, 64>(a, s);
+  if (dtype == 0) return d == 128 ? run<bf16, 128, false>(a, s) : run<bf16, 64, false>(a, s);
+  if (a.rows == kAttnWideRows) return d == 128 ? run<float, 128, true>(a, s) : run<float, 64, true>(a, s);
+  return d == 128 ? run<float, 128, false>(a, s) : run<float, 64, false>(a, s);
 }
 
 }  // namespace twinkv

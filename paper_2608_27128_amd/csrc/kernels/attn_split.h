@@ -191,4 +191,31 @@ constexpr int join_floats() {
   return kAttnWaves * 2 * kAttnRows + kAttnRows * (D + 4);
 }
 
+// One wave's own 16 rows, complete, through its own LDS.
+template <typename T, int D, typename Channel>
+__device__ inline void write_own(const AttnArgs& a, const AttnItem& p, int row0, const RowStats& st,
+                                 const f32x4 (&acc)[D / 16], float* lds, const Channel& channel) {
+  constexpr int kStride = D + 4;
+  float* s_ml = lds;               // [2][16]
+  float* s_o = lds + 2 * kAttnRows;
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const float l = group_sum(st.l);
+  if (g == 0) {
+    s_ml[i] = st.m;
+    s_ml[kAttnRows + i] = l;
+  }
+#pragma unroll
+  for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s_o[(4 * g + r) * kStride + channel(n, i)] = acc[n][r];
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  write_rows<T, D, kStride>(a, p, row0, s_o, s_ml, s_ml + kAttnRows, lane, 64);
+}
+template <int D>
+constexpr int own_floats() {
+  return 2 * kAttnRows + kAttnRows * (D + 4);
+}
+
 }  // namespace twinkv

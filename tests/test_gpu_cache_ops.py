@@ -505,3 +505,67 @@ def test_streams_and_graph():
         torch.cuda.synchronize()
         for n in ("out", "lse"):
             assert torch.equal(replayed[n], eager[n]), (t, n)
+
+
+# shapes that take each of the attention's ways: keys split or not, fp32 waves on row tiles of their own,
+# many bf16 rows whole and split, chunks of a prompt over long keys
+WAYS = [((700,), (0,), 40, 4, 4, 8), ((2500,), (40,), 1 << 20, 0, 4, 8), ((5000,), (64,), 1 << 20, 4, 2, 8),
+        ((9000,), (300,), 3000, 4, 4, 2), ((300,) * 16, (33,) * 16, 1 << 20, 0, 1, 8), ((4200,), (513,), 70, 10, 8, 4),
+        ((1300, 40, 3000), (1300, 1, 200), 500, 16, 4, 2)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", range(len(WAYS)))
+def test_sink_attention_every_way(case, dtype, d):
+    import torch
+    lens, nq, window, sink, G, H = WAYS[case]
+    nq = [m if m else n for m, n in zip(nq, lens)]
+    g = gen(300 + case)
+    cu_q, cu_k = cum(nq), cum(lens)
+    q = randn(g, sum(nq), H * G, d, dtype=dtype).transpose(0, 1)
+    k, v = randn(g, H, sum(lens), d, dtype=dtype), randn(g, H, sum(lens), d, dtype=dtype)
+    got = binding.sink_attention(q, k, v, window, sink, None, cu_q, cu_k, want_lse=True)
+    # some rows of some heads: the first and the last of every sequence, and a spread between
+    for s, (m, n) in enumerate(zip(nq, lens)):
+        rows = torch.tensor(sorted({0, m - 1, *(int(x) for x in np.linspace(0, m - 1, 23))}), device="cuda")
+        seen = ref.seen_by(m, n, window, sink).cuda()[rows]
+        a, x = int(cu_q[s]), int(cu_k[s])
+        for h in (0, H * G - 1):
+            o, e, mass, size = ref.softmax_rows(q[h, a + rows].double(), k[h // G, x:x + n].double(),
+                                                v[h // G, x:x + n].double(), seen, d ** -0.5)
+            tol, tol_e = ref.attention_bounds(o, e, mass, size, n, d, dtype == "bf16")
+            assert bool(((got["out"][h, a + rows].double() - o).abs() <= tol).all()), (s, h)
+            assert bool(((got["lse"][h, a + rows].double() - e).abs() <= tol_e).all()), (s, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sink_attention_negative_and_zero_scale(dtype):
+    """Any finite scale, on the kernels for few and for many rows."""
+    g = gen(41)
+    H, G, d, n = 2, 4, 64, 200
+    q, k, v = randn(g, H * G, n, d, dtype=dtype), randn(g, H, n, d, dtype=dtype), randn(g, H, n, d, dtype=dtype)
+    for m in (2, n):
+        for scale in (-0.2, 0.0):
+            got = binding.sink_attention(q[:, :m], k, v, 50, 3, scale, [0, m], [0, n], want_lse=True)
+            check_attention(got["out"], q[:, :m], k, v, [0, m], [0, n], lambda s, h, i, j: ref.seen_by(i, j, 50, 3), scale,
+                            dtype, got["lse"], heads=[0, 7])
+
+
+def test_sink_attention_split_unseen_values_do_not_matter():
+    """As above where a chunk's keys are split over workgroups (bf16, many rows; fp32, few)."""
+    import torch
+    for dtype, m in (("bf16", 130), ("f32", 3)):
+        g = gen(43)
+        H, G, d, n, W, sink = 1, 4, 128, 6000, 4000, 4
+        q, k, v = randn(g, H * G, m, d, dtype=dtype), randn(g, H, n, d, dtype=dtype), randn(g, H, n, d, dtype=dtype)
+        clean = binding.sink_attention(q, k, v, W, sink, None, [0, m], [0, n])["out"]
+        seen = ref.seen_by(m, n, W, sink).cuda()
+        for j in (2, 900, n - m - W + 1, n - m + 1, n - 1):
+            v2 = v.clone()
+            v2[:, j, 77] = math.inf
+            got = binding.sink_attention(q, k, v2, W, sink, None, [0, m], [0, n])["out"]
+            hit = torch.zeros((H * G, m, d), dtype=torch.bool, device="cuda")
+            hit[:, seen[:, j], 77] = True
+            assert torch.equal(got[~hit], clean[~hit]), (dtype, j)
+            assert not bool(torch.isfinite(got[hit]).any()), (dtype, j)
