@@ -569,3 +569,81 @@ def test_sink_attention_split_unseen_values_do_not_matter():
             hit[:, seen[:, j], 77] = True
             assert torch.equal(got[~hit], clean[~hit]), (dtype, j)
             assert not bool(torch.isfinite(got[hit]).any()), (dtype, j)
+
+
+# ---------------------------------------------------------------- together, and far into memory
+
+def test_example_layer():
+    """The example's calls in a row: the steps attend over exactly the rows that were kept, then the new ones."""
+    import torch
+    from paper_2608_27128_amd.examples import serve_layer
+    g = gen(47)
+    layer = serve_layer.Layer([900, 333], steps=5, n_heads=2, group=4, d=128, window=128)
+    T = int(layer.cu[-1])
+    q, k, v = serve_layer.projections(T, layer, g)
+    got = layer.prompt(q, k, v, torch.rand((2, T), generator=g, device="cuda"))
+    assert bool((got["status"] == OK).all()) and layer.length.tolist() == [layer.budget.tolist()] * 2
+    want_k = ref.norm_rope(k.transpose(0, 1).double(), layer.k_weight, serve_layer.EPS, layer.rope, layer.positions)
+    check_rope(got["keys"], want_k, 128, "bf16")
+    qr = binding.qk_norm_rope(q.transpose(0, 1), None, layer.q_weight, None, serve_layer.EPS, layer.rope,
+                              layer.positions)["q"]
+    check_attention(got["out"].transpose(0, 1), qr, got["keys"], v.transpose(0, 1), layer.cu, layer.cu,
+                    lambda s, h, m, n: ref.seen_by(m, n, 128, 4), layer.scale, "bf16", heads=[0, 7])
+    for t in range(5):
+        q1, k1, v1 = serve_layer.projections(2, layer, g)
+        out = layer.step(q1, k1, v1)
+        n = layer.length
+        assert bool((out["status"] == OK).all()) and n.tolist() == [(layer.budget + t + 1).tolist()] * 2
+        kv = binding.cache4_read(layer.cache, n, torch.float32)
+        for s in range(2):
+            r0 = int(layer.cache.cu_rows[s])
+            for h in range(2):
+                a = int(layer.cu[s])
+                pos = got["s1"][h, a:int(layer.cu[s + 1])].nonzero().squeeze(1)
+                kept = ref.quantise(got["keys"][h, a + pos].double())[0]
+                assert torch.equal(kv["keys"][h, r0:r0 + len(pos)].double(), kept)
+                last = r0 + int(n[h, s]) - 1
+                assert torch.equal(kv["values"][h, last].double(), ref.quantise(v1[s, h].double())[0])
+        check_attention(out["out"].transpose(0, 1), out["q"], kv["keys"], kv["values"], [0, 1, 2], layer.cache.cu_rows,
+                        lambda s, h, m, c: (torch.arange(c)[None, :] < int(n[h // 4, s])).expand(m, c), layer.scale, "bf16")
+
+
+def test_rows_beyond_32_bits():
+    """Byte offsets past 2^32 in keys, values and the 4-bit cache: the last rows of a long buffer."""
+    import torch
+    g = gen(53)
+    H, d, far, n = 2, 128, 9_000_000, 700
+    big = torch.empty((H, far + n, d), dtype=torch.bfloat16, device="cuda")   # 2.3 GB a head
+    k, v = randn(g, H, n, d), randn(g, H, n, d)
+    cu = [0, far, far + n]
+    q = randn(g, H * 4, 3, d)
+    big[:, far:] = k
+    vals = torch.empty_like(big)
+    vals[:, far:] = v
+    for m in (3, 300):
+        q = randn(g, H * 4, m, d)
+        got = binding.sink_attention(q, big, vals, 1 << 20, 0, None, [0, 0, m], cu)["out"]
+        assert torch.equal(got, binding.sink_attention(q, k, v, 1 << 20, 0, None, [0, m], [0, n])["out"])
+    out = binding.qk_norm_rope(None, big[:, far:], None, torch.ones(d, device="cuda"), 1e-6, table(n, d),
+                               torch.arange(n, dtype=torch.int32, device="cuda"))["k"]
+    check_rope(out, ref.norm_rope(k.double(), torch.ones(d, device="cuda"), 1e-6, table(n, d), torch.arange(n, device="cuda")), d, "bf16")
+    ret = torch.zeros((H, far + n), dtype=torch.uint8, device="cuda")
+    ret[:, far:] = 1
+    rows = 40_000_000                                                        # 2.6 GB of codes a head
+    cache = binding.Cache4.empty(H, [rows, n + 1], d)
+    kept = binding.cache4_compact(big, vals, ret, cache, cu)
+    del big, vals, ret
+    assert kept["len"].tolist() == [[0, n]] * H
+    small = binding.Cache4.empty(H, [n + 1], d)
+    ones = torch.ones((H, n), dtype=torch.uint8, device="cuda")
+    near = binding.cache4_compact(k, v, ones, small)
+    k1, v1, q1 = randn(g, H, 1, d), randn(g, H, 1, d), randn(g, H * 4, 1, d)
+    length = binding.cache4_append(k1, v1, cache, kept["len"], [0, 0, 1])["len"]
+    length1 = binding.cache4_append(k1, v1, small, near["len"], [0, 1])["len"]
+    a = binding.cache4_attention(q1, cache, length, None, [0, 0, 1])["out"]
+    b = binding.cache4_attention(q1, small, length1, None, [0, 1])["out"]
+    assert torch.equal(a, b)
+    x = binding.cache4_read(cache, length, torch.bfloat16, cu_out=[0, 0, n + 1])
+    y = binding.cache4_read(small, length1, torch.bfloat16, cu_out=[0, n + 1])
+    for name in ("keys", "values"):
+        assert torch.equal(x[name], y[name])
