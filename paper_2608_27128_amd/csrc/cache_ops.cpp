@@ -386,7 +386,7 @@ int twinkv_qk_norm_rope(const void* q, const void* k, int dtype, int d, int n_q_
   const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
   NormRopeArgs a;
   // heads a unit of lanes goes through with its token's cos and sin: as many as leave units for every
-  // SIMD of the machine (about 16000 rows of lanes)
+  // SIMD of the machine (about 16000 rows of lanes; both ends measured in norm_rope.hip)
   const int64_t rows = T * ((int64_t)n_q_heads + n_k_heads);
   a.per_unit = (int)std::min<int64_t>(std::max<int64_t>(rows / 16384, 1), 8);
   auto side = [&](const void* in, void* out, int64_t ih, int64_t it, int64_t oh, int64_t ot, const float* weight,

@@ -7,7 +7,10 @@
 //    the mean takes 2 or 3 exchanges between the row's lanes.
 //  * A unit of lanes goes through several heads of its token with the token's cos and sin in registers:
 //    they are fp32 and as long as the row, so reading them per row would double the traffic of bf16
-//    rows.  Few tokens take one head a unit instead, so that there are units for the whole machine.
+//    rows.  Few tokens take one head a unit instead, so that there are units for the whole machine
+//    (32 + 8 heads of 128, bf16, 1 head / 8 heads a unit: 64 tokens 3.7 / 6.4 us, 1024 7.2 / 8.7, 4096 17.2 / 15.7,
+//    32k 182 / 131).
+// 32k tokens, 40 heads of 128, bf16: 139 us a call, 4.9 TB/s where a large copy runs at 5.15.
 #include <hip/hip_runtime.h>
 
 #include "../cache_ops.h"
