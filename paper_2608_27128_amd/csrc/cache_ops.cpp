@@ -219,14 +219,19 @@ constexpr int64_t kLeast = 8, kLeastCached = 16, kWholeCached = 32, kLeastBig = 
 constexpr int64_t kMuchWork = 20480;
 
 // What a call's keys are: rows of any kind, rows that the kernel for many rows takes too, fp32 rows, a 4-bit
-// cache.
-enum class KeysAre { kRows, kRowsOfMany, kRowsFp32, kCached };
+// cache under bf16 or fp32 queries.
+enum class KeysAre { kRows, kRowsOfMany, kRowsFp32, kCached, kCachedFp32 };
 
 int64_t live_of(int n_seqs, const int64_t* cu_q) {  // sequences with queries
   int64_t n = 0;
   for (int s = 0; s < n_seqs; ++s) n += cu_q[s + 1] > cu_q[s];
   return n;
 }
+
+// 4 bits, bf16: with so much work (as above) and more than a row tile in the mean a wave takes two row tiles at
+// once.  One / two, us, 8 heads of 8, d 128: 3 queries over 32k rows 25 / 28, over 128k 58 / 50, over 64 caches of 4k 94 /
+// 72; 7 queries over 32k 34 / 36, over 64 caches of 4k 182 / 143.
+constexpr int64_t kPairWork = 49152;
 
 // fp32: with so many row tiles (of all heads) and at most so many key tiles the waves of a workgroup take a row
 // tile each, and their join falls away.  Shared / own, us, 8 heads of 4, d 128, window 128: 256 tokens (512 row tiles)
@@ -237,8 +242,12 @@ int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* c
               int64_t n_sink, AttnPlan& p) {
   p.window = std::min<int64_t>(window, kAttnMaxKeys);
   p.n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
-  const AttnWork few = work_of(n_heads, group, n_seqs, cu_q, cu_k, p);
-  const bool cached = keys == KeysAre::kCached;
+  const bool cached = keys == KeysAre::kCached || keys == KeysAre::kCachedFp32;
+  AttnWork few = work_of(n_heads, group, n_seqs, cu_q, cu_k, p);
+  if (keys == KeysAre::kCached && few.tiles >= kPairWork && cu_q[n_seqs] * group > kAttnRows * live_of(n_seqs, cu_q)) {
+    p.rows = kAttnPairRows;
+    few = work_of(n_heads, group, n_seqs, cu_q, cu_k, p);
+  }
   int64_t each = std::max(cached ? kLeastCached : kLeast, (few.tiles + kItems - 1) / kItems);
   p.whole_tiles = cached ? kWholeCached : kLeast;
   if (keys == KeysAre::kRowsOfMany) {
@@ -414,7 +423,8 @@ int64_t twinkv_attention_workspace_bytes(int dtype, int d, int n_heads, int grou
   if (rc == TWINKV_OK && (window < 0 || n_sink < 0)) rc = TWINKV_E_ARG;
   if (rc != TWINKV_OK) return -rc;
   int64_t most = 0;  // of the plans that the two calls may make
-  for (const KeysAre keys : {KeysAre::kRows, KeysAre::kCached, dtype == TWINKV_BF16 ? KeysAre::kRowsOfMany : KeysAre::kRowsFp32}) {
+  for (const KeysAre keys : {KeysAre::kRows, dtype == TWINKV_BF16 ? KeysAre::kCached : KeysAre::kCachedFp32,
+                             dtype == TWINKV_BF16 ? KeysAre::kRowsOfMany : KeysAre::kRowsFp32}) {
     AttnPlan p;
     rc = attn_plan(keys, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
     if (rc != TWINKV_OK) return -rc;
@@ -556,8 +566,9 @@ int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* 
   if (len == nullptr) return TWINKV_E_NULL;
   if (no_q) return TWINKV_OK;
   AttnArgs a;
-  rc = attn_args(KeysAre::kCached, q, dtype, d, cache->n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride,
-                 INT64_MAX, 0, scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
+  rc = attn_args(dtype == TWINKV_BF16 ? KeysAre::kCached : KeysAre::kCachedFp32, q, dtype, d, cache->n_heads, group, n_seqs,
+                 cu_q, cache->cu_rows, q_head_stride, q_token_stride, INT64_MAX, 0, scale, out, out_head_stride,
+                 out_token_stride, lse, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   a.cache = device_cache(cache);
   a.len = len;

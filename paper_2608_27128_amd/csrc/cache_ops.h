@@ -79,6 +79,7 @@ int launch_cache4_read(const Cache4Args& a, int dtype, int d, void* stream);
 constexpr int kAttnSeqWords = 6;
 constexpr int kAttnTile = 32;        // keys of a tile
 constexpr int kAttnRows = 16;        // rows of a tile
+constexpr int kAttnPairRows = 32;    // of an item whose waves take two row tiles at once (4 bits)
 constexpr int kAttnWideRows = 64;    // of an item whose four waves take a tile each
 constexpr int kAttnBigRows = 128;    // rows and keys of the kernel for many rows
 constexpr int kAttnBigTile = 64;
@@ -98,7 +99,7 @@ struct AttnArgs {
   int window, n_sink;    // at most kAttnMaxKeys each
   int n_heads, group, n_seqs;
   int items, parts;      // per head
-  int rows;              // of an item: kAttnRows, kAttnWideRows or kAttnBigRows
+  int rows;              // of an item: kAttnRows, kAttnPairRows, kAttnWideRows or kAttnBigRows
   float* part_o;         // [n_heads][parts][rows][d] unnormalised sums
   float* part_ml;        // [n_heads][parts][rows][2] maximum (log2 units) and sum
 };

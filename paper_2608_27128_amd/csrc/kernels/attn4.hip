@@ -14,8 +14,8 @@
 // The keys are split over workgroups when there are too few problems for the machine (attn_split.h).
 // A tile costs about 250 vector instructions a wave, which at 4 waves a SIMD is under half of the time its bytes
 // take: 256 sequences of 2k rows, 8 heads of 4, d 128 120 us (4.8 TB/s; copy rate 111 us), 64 of 1k to 4k 42 us, one of
-// 128k rows 32 us and 6.5 us for its join, one of 512 rows 8 us (launch and latency).  56 rows a problem (8 heads of
-// 8, 7 tokens) read it 4 times, mostly from the last cache: 345 us for the first of these.
+// 128k rows 32 us and 6.5 us for its join, one of 512 rows 8 us (launch and latency).  More rows than 16 a problem
+// (8 heads of 8, 7 tokens: 56) unpack the cache once per tile, or pair of tiles: 288 us for the first of these.
 #include <hip/hip_runtime.h>
 
 #include "attn_split.h"
@@ -98,8 +98,9 @@ struct Tile4 {
   }
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4_kernel(const AttnArgs a) {
+// R: row tiles of 16 that a wave takes at once; what it unpacks serves them all.
+template <typename T, int D, int R>
+__global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 && R == 1 ? 4 : 2) void attn4_kernel(const AttnArgs a) {
   constexpr int kSteps = D / 32;
   constexpr int N = kParts<T>;
   __shared__ float s_join[join_floats<D>()];
@@ -107,19 +108,21 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const AttnItem p = attn_item(a, (int)blockIdx.x, (int)blockIdx.y);
   const int len = min(max(a.len[(int64_t)p.h * a.n_seqs + p.s], 0), p.nk);
-  const int n_rows = p.nq * a.group, row0 = p.rt * kAttnRows;
-  const int last = min(row0 + kAttnRows, n_rows) - 1;
-  // rows past the problem's are computed as if they saw everything, and not written
-  const int row = min(row0 + i, n_rows - 1);
-  const int query = row / a.group;
-  const int lim = len - (p.nq - 1 - query);
+  const int n_rows = p.nq * a.group, row0 = p.rt * R * kAttnRows;
+  const int last = min(row0 + R * kAttnRows, n_rows) - 1;
   const int lim_all = len - (p.nq - 1 - row0 / a.group);      // every row sees so many
   const int lim_any = len - (p.nq - 1 - last / a.group);      // no row sees more
   const int t0 = p.split * p.tiles * kAttnTile;
   const int t1 = min(lim_any, t0 + p.tiles * kAttnTile);
 
-  bf16x8 q[N][kSteps];
-  {
+  int lim[R];
+  bf16x8 q[R][N][kSteps];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    // rows past the problem's repeat its last, and are not written
+    const int row = min(row0 + r * kAttnRows + i, n_rows - 1);
+    const int query = row / a.group;
+    lim[r] = len - (p.nq - 1 - query);
     const int64_t head = (int64_t)p.h * a.group + (row - query * a.group);
     const char* src = a.q + head * a.q_head + (int64_t)(p.q0 + query) * a.q_token;
 #pragma unroll
@@ -129,13 +132,16 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4
       bf16x8 parts[N];
       split8<N>(x, parts);
 #pragma unroll
-      for (int n = 0; n < N; ++n) q[n][j] = parts[n];
+      for (int n = 0; n < N; ++n) q[r][n][j] = parts[n];
     }
   }
-  RowStats st;
-  f32x4 acc[D / 16];
+
+  RowStats st[R];
+  f32x4 acc[R][D / 16];
 #pragma unroll
-  for (int n = 0; n < D / 16; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) acc[r][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   constexpr int kStep = kAttnTile * kAttnWaves;
   const int first = t0 + wave * kAttnTile;
   Tile4<D> now(a.cache, p.h, (int64_t)p.k0 + first, i, g);
@@ -144,27 +150,35 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4
     now.load_values();
   }
   for (int t = first; t < t1; t += kStep) {
-    float s[8];
+    float s[R][8];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const float scale = __uint_as_float(now.ks[m] << 23);
-      f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
+      f32x4 d[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) d[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) {
         const bf16x8 k = codes8(now.k[m][j], scale);
 #pragma unroll
-        for (int n = N - 1; n >= 0; --n) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[n][j], d, 0, 0, 0);
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int n = N - 1; n >= 0; --n) d[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[r][n][j], d[r], 0, 0, 0);
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[4 * m + r] = d[r] * a.scale_log2;
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[r][4 * m + e] = d[r][e] * a.scale_log2;
     }
     // the next tile, or this one once more: a load on one path only would make the waits of both longer
     const int ahead = t + kStep < t1 ? kStep : 0;
     now.next_keys(ahead);
     if (t + kAttnTile > lim_all) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (t + 8 * g + e >= lim) s[e] = kNegInf;
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (t + 8 * g + e >= lim[r]) s[r][e] = kNegInf;
       if (t + kAttnTile > len) {  // rows not in use: their scales may be anything
         const int use = min(max(len - (t + 8 * g), 0), 8);
         const unsigned lo = use >= 4 ? ~0u : (1u << (8 * use)) - 1u;
@@ -173,28 +187,44 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 ? 4 : 2) void attn4
         for (int x = 0; x < D / 64; ++x) now.vs[x] = u32x4{now.vs[x][0] & lo, now.vs[x][1] & hi, now.vs[x][2] & lo, now.vs[x][3] & hi};
       }
     }
-    st.update(s, acc);
+#pragma unroll
+    for (int r = 0; r < R; ++r) st[r].update(s[r], acc[r]);
 #pragma unroll
     for (int grp = 0; grp < D / 32; ++grp) {
-      float x[8];
+      bf16x8 w[R][N];
+      float scale[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const unsigned w = now.vs[grp >> 1][(grp & 1) * 2 + (e >> 2)];
-        x[e] = s[e] * __uint_as_float(((w >> (8 * (e & 3))) & 255u) << 23);
+        const unsigned b = now.vs[grp >> 1][(grp & 1) * 2 + (e >> 2)];
+        scale[e] = __uint_as_float(((b >> (8 * (e & 3))) & 255u) << 23);
       }
-      bf16x8 w[N];
-      split8<N>(x, w);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[r][e] * scale[e];
+        split8<N>(x, w[r]);
+      }
 #pragma unroll
       for (int b = 2 * grp; b < 2 * grp + 2; ++b) {
         const bf16x8 v = codes8(now.v[b >> 2][b & 3], 1.0f);
 #pragma unroll
-        for (int n = N - 1; n >= 0; --n) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], v, acc[b], 0, 0, 0);
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int n = N - 1; n >= 0; --n) acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[r][n], v, acc[r][b], 0, 0, 0);
       }
     }
     now.next_values(ahead);
     asm volatile("" ::: "memory");  // here, and not where the next tile begins: the scores cover the way
   }
-  join_waves<T, D>(a, p, row0, st, acc, s_join, [](int n, int lane16) { return n * 16 + lane16; });
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (r > 0) {
+      if (row0 + r * kAttnRows >= n_rows) break;  // the same for the workgroup
+      __syncthreads();                            // the tile before has been written
+    }
+    join_waves<T, D>(a, p, row0 + r * kAttnRows, st[r], acc[r], s_join, [](int n, int lane16) { return n * 16 + lane16; });
+  }
 }
 
 // The join: a row tile's parts brought to one maximum.  The tile's items share its rows out among them (item
@@ -267,9 +297,9 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(const AttnArgs 
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, int R>
 int run4(const AttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attn4_kernel<T, D>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
+  hipLaunchKernelGGL((attn4_kernel<T, D, R>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
   return hipGetLastError();
 }
 template <typename T, int D>
@@ -282,8 +312,9 @@ int run_join(const AttnArgs& a, hipStream_t s) {
 
 int launch_attn4(const AttnArgs& a, int dtype, int d, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == 0) return d == 128 ? run4<bf16, 128>(a, s) : run4<bf16, 64>(a, s);
-  return d == 128 ? run4<float, 128>(a, s) : run4<float, 64>(a, s);
+  if (dtype != 0) return d == 128 ? run4<float, 128, 1>(a, s) : run4<float, 64, 1>(a, s);
+  if (a.rows == kAttnPairRows) return d == 128 ? run4<bf16, 128, 2>(a, s) : run4<bf16, 64, 2>(a, s);
+  return d == 128 ? run4<bf16, 128, 1>(a, s) : run4<bf16, 64, 1>(a, s);
 }
 
 int launch_attn_join(const AttnArgs& a, int dtype, int d, void* stream) {

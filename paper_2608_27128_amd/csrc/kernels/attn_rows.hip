@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int j = j0 + (b * 32 + 8 * (e >> 2) + (e & 3));
-          if (!((unsigned)(j - from) < seen)) {
+          if (!((unsigned)j - (unsigned)from < seen)) {
             if (base >= a.n_sink || !((j < upto) & (j < a.n_sink))) x[b][e] = kNegInf;
           }
         }

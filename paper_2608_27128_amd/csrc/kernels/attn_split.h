@@ -103,17 +103,18 @@ template <typename T, int D, int kStride>
 __device__ inline void write_rows(const AttnArgs& a, const AttnItem& p, int row0, const float* o, const float* m,
                                   const float* l, int tid, int threads) {
   const int n_rows = p.nq * a.group;
+  const int64_t part = p.part * a.rows + (row0 - p.rt * a.rows);
   constexpr int kPieces = D / 8;
   for (int x = tid; x < kAttnRows * kPieces; x += threads) {
     const int r = x / kPieces, c = x % kPieces * 8;
     if (row0 + r >= n_rows) continue;
     float f[8];
     if (p.splits > 1) {
-      float* to = a.part_o + (p.part * kAttnRows + r) * D + c;
+      float* to = a.part_o + (part + r) * D + c;
 #pragma unroll
       for (int e = 0; e < 8; ++e) to[e] = o[r * kStride + c + e];
       if (c == 0) {
-        float* ml = a.part_ml + (p.part * kAttnRows + r) * 2;
+        float* ml = a.part_ml + (part + r) * 2;
         ml[0] = m[r];
         ml[1] = l[r];
       }

@@ -105,7 +105,7 @@ int launch_attn_rows(const AttnArgs& a, int d, void*) {
   return 0;
 }
 int launch_attn4(const AttnArgs& a, int, int d, void*) {
-  CHECK(a.rows == kAttnRows);
+  CHECK(a.rows == kAttnRows || a.rows == kAttnPairRows);
   check_items(a, d, kAttnTile, true);
   return 0;
 }

@@ -391,7 +391,7 @@ ATTN4 = [  # capacities, lengths per head, queries per sequence, group
     ((32,), [[1]], (1,), 1), ((32,), [[0]], (2,), 4), ((64,), [[33]], (1,), 4), ((96,), [[90]], (5,), 3),
     ((256, 32, 160), [[256, 31, 100], [200, 0, 129]], (1, 1, 1), 4), ((512,), [[500], [3]], (7,), 4),
     ((640, 64), [[640, 1], [65, 64]], (0, 9), 2), ((4096,), [[4001]], (1,), 16), ((1024,), [[1000]], (33,), 1),
-    ((8192,), [[8190]], (2,), 20)]
+    ((8192,), [[8190]], (2,), 20), ((64000, 4096), [[63000, 4000]] * 8, (5, 3), 10)]
 
 
 def fill_cache(g, H, caps, d, dtype):
