@@ -685,8 +685,8 @@ def _out_rows(out, shape, like, name: str):
                          f"{tuple(out.shape)} {out.dtype} on {out.device}")
     h, t, c = out.stride()
     lanes = 16 // out.element_size()
-    if c != 1 or t % lanes or h % lanes or t < shape[2] or out.data_ptr() % 16:
-        raise ValueError(f"{name} must have contiguous channels and strides of multiples of 16 bytes")
+    if c != 1 or t % lanes or h % lanes or t < shape[2] or out.data_ptr() % 16 or (h < shape[2] and shape[0] > 1):
+        raise ValueError(f"{name} must have contiguous channels, strides of multiples of 16 bytes and no overlap")
     return out
 
 

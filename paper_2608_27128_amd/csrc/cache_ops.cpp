@@ -49,6 +49,12 @@ int check_rows(const void* p, int dtype, int d, int64_t head_stride, int64_t tok
   return token_stride * esz % 16 != 0 || head_stride * esz % 16 != 0 ? TWINKV_E_ARG : TWINKV_OK;
 }
 
+// Rows that are written: heads that share a place (a stride of 0, say) would overwrite each other.
+int check_out(const void* p, int dtype, int d, int64_t head_stride, int64_t token_stride, int64_t heads, bool empty) {
+  const int rc = check_rows(p, dtype, d, head_stride, token_stride, empty);
+  return rc == TWINKV_OK && !empty && heads > 1 && head_stride < d ? TWINKV_E_ARG : rc;
+}
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 // Collects a call's per-sequence words: into the kernel arguments, or piece by piece into the workspace.
@@ -382,9 +388,9 @@ int twinkv_qk_norm_rope(const void* q, const void* k, int dtype, int d, int n_q_
   if (!std::isfinite(eps) || eps < 0.0f) return TWINKV_E_ARG;
   const bool no_q = n_q_heads == 0 || T == 0, no_k = n_k_heads == 0 || T == 0;
   if ((rc = check_rows(q, dtype, d, q_head_stride, q_token_stride, no_q)) != TWINKV_OK) return rc;
-  if ((rc = check_rows(q_out, dtype, d, qo_head_stride, qo_token_stride, no_q)) != TWINKV_OK) return rc;
+  if ((rc = check_out(q_out, dtype, d, qo_head_stride, qo_token_stride, n_q_heads, no_q)) != TWINKV_OK) return rc;
   if ((rc = check_rows(k, dtype, d, k_head_stride, k_token_stride, no_k)) != TWINKV_OK) return rc;
-  if ((rc = check_rows(k_out, dtype, d, ko_head_stride, ko_token_stride, no_k)) != TWINKV_OK) return rc;
+  if ((rc = check_out(k_out, dtype, d, ko_head_stride, ko_token_stride, n_k_heads, no_k)) != TWINKV_OK) return rc;
   if (!aligned16(q_weight) || !aligned16(k_weight) || !aligned16(rope)) return TWINKV_E_ARG;
   if (rope != nullptr) {
     if (n_pos < 0) return TWINKV_E_ARG;
@@ -448,7 +454,8 @@ int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype
   if (window < 0 || n_sink < 0 || !std::isfinite(scale)) return TWINKV_E_ARG;
   const bool no_q = cu_q[n_seqs] == 0, no_k = cu_k[n_seqs] == 0;
   if ((rc = check_rows(q, dtype, d, q_head_stride, q_token_stride, no_q)) != TWINKV_OK) return rc;
-  if ((rc = check_rows(out, dtype, d, out_head_stride, out_token_stride, no_q)) != TWINKV_OK) return rc;
+  if ((rc = check_out(out, dtype, d, out_head_stride, out_token_stride, (int64_t)n_heads * group, no_q)) != TWINKV_OK)
+    return rc;
   if ((rc = check_rows(k, dtype, d, k_head_stride, k_token_stride, no_k)) != TWINKV_OK) return rc;
   if ((rc = check_rows(v, dtype, d, v_head_stride, v_token_stride, no_k)) != TWINKV_OK) return rc;
   if (no_q) return TWINKV_OK;
@@ -562,7 +569,8 @@ int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* 
   if (!std::isfinite(scale)) return TWINKV_E_ARG;
   const bool no_q = cu_q[n_seqs] == 0;
   if ((rc = check_rows(q, dtype, d, q_head_stride, q_token_stride, no_q)) != TWINKV_OK) return rc;
-  if ((rc = check_rows(out, dtype, d, out_head_stride, out_token_stride, no_q)) != TWINKV_OK) return rc;
+  if ((rc = check_out(out, dtype, d, out_head_stride, out_token_stride, (int64_t)cache->n_heads * group, no_q)) != TWINKV_OK)
+    return rc;
   if (len == nullptr) return TWINKV_E_NULL;
   if (no_q) return TWINKV_OK;
   AttnArgs a;

@@ -176,3 +176,12 @@ def test_binding_refusals():
                  lambda: binding.Cache4(*(torch.zeros((1, 1, 1)),) * 4, [0, 33])):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("stride", [0, 8, 120])
+def test_heads_of_an_output_may_not_overlap(stride):
+    assert rope(qos=(stride, 128)) == E_ARG
+    assert rope(hk=2, kos=(stride, 128)) == E_ARG
+    assert sink(os=(stride, 128)) == E_ARG
+    assert attend(os=(stride, 128)) == E_ARG
+    assert rope(T=0, q=None, k=None, qo=None, ko=None, pos=None, qos=(stride, 128)) == 0

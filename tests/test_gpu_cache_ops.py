@@ -647,3 +647,25 @@ def test_rows_beyond_32_bits():
     y = binding.cache4_read(small, length1, torch.bfloat16, cu_out=[0, n + 1])
     for name in ("keys", "values"):
         assert torch.equal(x[name], y[name])
+
+
+def test_outputs_whose_heads_overlap_are_refused():
+    import torch
+    g = gen(900)
+    H, T, d = 2, 8, 128
+    q, k, v = randn(g, H * 2, T, d), randn(g, H, T, d), randn(g, H, T, d)
+    one = torch.zeros((1, T, d), dtype=q.dtype, device="cuda")
+    with pytest.raises(ValueError, match="overlap"):
+        binding.qk_norm_rope(q, None, q_out=one.expand(H * 2, T, d))
+    with pytest.raises(ValueError, match="overlap"):
+        binding.qk_norm_rope(None, k, k_out=one.expand(H, T, d))
+    with pytest.raises(ValueError, match="overlap"):
+        binding.sink_attention(q, k, v, 4, out=one.expand(H * 2, T, d))
+    cache = binding.Cache4.empty(H, [32], d)
+    kept = binding.cache4_compact(k, v, torch.ones((H, T), dtype=torch.uint8, device="cuda"), cache)
+    with pytest.raises(ValueError, match="overlap"):
+        binding.cache4_attention(q, cache, kept["len"], out=one.expand(H * 2, T, d))
+    # an input may repeat one head: the same answer as with the copies laid out
+    got = binding.sink_attention(q, k[:1].expand(H, T, d), v[:1].expand(H, T, d), 4)["out"]
+    want = binding.sink_attention(q, k[:1].repeat(H, 1, 1), v[:1].repeat(H, 1, 1), 4)["out"]
+    assert torch.equal(got, want)
