@@ -15,7 +15,7 @@
 // A tile costs about 250 vector instructions a wave, which at 4 waves a SIMD is under half of the time its bytes
 // take: 256 sequences of 2k rows, 8 heads of 4, d 128 120 us (4.8 TB/s; copy rate 111 us), 64 of 1k to 4k 42 us, one of
 // 128k rows 32 us and 6.5 us for its join, one of 512 rows 8 us (launch and latency).  More rows than 16 a problem
-// (8 heads of 8, 7 tokens: 56) unpack the cache once per tile, or pair of tiles: 288 us for the first of these.
+// (8 heads of 8, 7 tokens: 56) unpack the cache once per tile, or pair of tiles: 282 us for the first of these.
 #include <hip/hip_runtime.h>
 
 #include "attn_split.h"
