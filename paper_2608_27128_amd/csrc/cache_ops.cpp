@@ -239,10 +239,13 @@ int64_t live_of(int n_seqs, const int64_t* cu_q) {  // sequences with queries
 // 72; 7 queries over 32k 34 / 36, over 64 caches of 4k 182 / 143.
 constexpr int64_t kPairWork = 49152;
 
-// fp32: with so many row tiles (of all heads) and at most so many key tiles the waves of a workgroup take a row
-// tile each, and their join falls away.  Shared / own, us, 8 heads of 4, d 128, window 128: 256 tokens (512 row tiles)
-// 20 / 27, 512 40 / 30, 2048 143 / 86; plain causal, 512 tokens (17 key tiles) 60 / 50, 1024 (33) 155 / 207.
-constexpr int64_t kWideRows = 768, kWideTiles = 20;
+// fp32: the kernel for many rows takes four row tiles a workgroup and does not split their keys, so it is taken where
+// the most key tiles that a row tile has are no more than each of kItems such workgroups has in the mean, or up to
+// kWideShare times that where they are few.  Split / wide, us, 8 heads, that ratio in brackets: d 128, 4 rows a token,
+// causal, 256 tokens (4) 22 / 27, 512 (2) 60 / 49, 1024 (1) 151 / 124, 2048 (0.5) 443 / 326; window 128, 256 tokens (4)
+// 20 / 21, 512 (2) 39 / 23, 2048 (0.5) 144 / 69; a row a token, causal, 2048 tokens (2) 155 / 172, 4096 (1) 472 / 445, and
+// of d 64 73 / 101 and 233 / 243.
+constexpr int64_t kWideShare = 3, kWideTiles = 20;
 
 int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
               int64_t n_sink, AttnPlan& p) {
@@ -267,7 +270,8 @@ int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* c
       each = w.rows >= kCus ? kAttnMaxKeys : std::max(kLeastBig, (w.tiles + kItems - 1) / kItems);
     }
   }
-  if (keys == KeysAre::kRowsFp32 && few.rows >= kWideRows && few.longest <= kWideTiles &&
+  const int64_t share = few.longest <= kWideTiles ? kWideShare : 1;
+  if (keys == KeysAre::kRowsFp32 && few.longest * (kAttnWideRows / kAttnRows) * kItems <= share * few.tiles &&
       cu_q[n_seqs] * group > kAttnRows * live_of(n_seqs, cu_q)) {
     p.rows = kAttnWideRows;
     each = kAttnMaxKeys;
@@ -280,7 +284,7 @@ int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* c
     p.items += row_tiles(nq, group, p) * splits;
     if (splits > 1) p.parts += row_tiles(nq, group, p) * splits;
   }
-  return grid_ok(p.items * (p.rows == kAttnBigRows ? n_heads : 1), 256) ? TWINKV_OK : TWINKV_E_ARG;
+  return grid_ok(p.items * (p.rows == kAttnBigRows || p.rows == kAttnWideRows ? n_heads : 1), 256) ? TWINKV_OK : TWINKV_E_ARG;
 }
 
 struct AttnLayout {

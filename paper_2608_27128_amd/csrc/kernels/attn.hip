@@ -1,5 +1,5 @@
-// K9: attention over the window and the sinks, few rows or fp32: the keys split over waves and workgroups
-// (attn_split.h).
+// K9: attention over the window and the sinks, few rows or fp32.  Few rows: the keys split over waves and
+// workgroups (attn_split.h).
 //
 // bf16: 32 keys a wave at a time.  K q^T takes the key rows as they lie in memory, 16 bytes a lane,
 // without LDS.  The product with the values contracts over tokens, so the values' tile goes through the
@@ -8,12 +8,14 @@
 // Nothing of it is shared between waves, so there is no barrier in the loop.  HBM-bound: 64 sequences, 1028 keys of a
 // window each, 8 heads of 4, d 128: 52 us, 5.1 TB/s.  (Fetching a tile's keys and values before the tile in
 // front is done took 175 registers instead of 160 and 1-8% longer.)
-// fp32: with many rows and few keys the waves take a row tile each instead (no join).
-// v_mfma_f32_16x16x4_f32, whose operands are single values a lane: keys and values both come
-// straight from memory, 16 bytes a lane, the contraction's and the channels' order chosen to fit.  Bound
-// by that instruction's rate with many rows (2048 tokens, 32 heads of 128, causal: 443 us, 78 of the 153 TFLOP/s
-// of a large product), by latency with few (5 prompts of up to 1500 tokens, window 128, d 64: 31 us).
-//
+// fp32: v_mfma_f32_16x16x4_f32, whose operands are single values a lane: keys and values are read 16 bytes a lane, the
+// contraction's and the channels' order chosen to fit.
+//  * Few rows: straight from memory.
+//  * Many: four row tiles share their keys through LDS (attn_wide_kernel), which reads a quarter as much: 2048 tokens,
+//    32 heads of 128, causal, 326 us (443 in the kernel for few rows), 106 of the 153 TFLOP/s of a large product;
+//    2048 tokens over 4k keys 865 (1117), 119 TFLOP/s.  Row tiles with the most keys go first: with the heads one
+//    after the other the first of these took 461 us.  5 prompts of up to 1500 tokens, window 128, d 64 take 28 us
+//    (31 with a row tile a wave and nothing shared), at most 7 key tiles one after the other.
 // Values that no row of a tile sees are taken as zeros.  A tile that some rows see and others do not may
 // hold a NaN or infinite value, which the product would spread (0 * inf) to the rows that do not: those
 // elements are zeroed before the product and added one by one to the rows that see them.
@@ -185,6 +187,24 @@ struct Tile<float, D> {
       for (int x = 0; x < D / 64; ++x) v[e][x] = *reinterpret_cast<const f32x4*>(vb + t * v_token + x * 256 + i * 16);
     }
   }
+  // A tile in LDS: rows of D values, the 16-byte pieces of key row `row` turned by turn(row) so that the lanes of
+  // a read lie in different banks.
+  __device__ static int turn(int row) { return 4 * (row >> 3) + (row & 3); }
+  __device__ void load(const char* kl, const char* vl, int lane) {
+    const int i = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int t = 8 * (i >> 2) + 4 * m + (i & 3);
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j)
+        k[m][j] = *reinterpret_cast<const f32x4*>(kl + t * (D * 4) + ((4 * j + g) ^ turn(t)) * 16);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x)
+        v[e][x] = *reinterpret_cast<const f32x4*>(vl + (8 * g + e) * (D * 4) + x * 256 + i * 16);
+  }
   __device__ void scores(const Query& q, float (&s)[8]) const {
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -224,24 +244,49 @@ struct Tile<float, D> {
   }
 };
 
-// kOnRows: the four waves take four row tiles, each over all of its keys, instead of sharing one tile's keys.
-template <typename T, int D, bool kOnRows>
+// Adds a tile's values that are not finite to the rows that see them (accumulator rows 4g .. 4g + 3).
+template <typename T, int D>
+__device__ inline void add_odd(const AttnArgs& a, const char* vb, int base, int end, int pos, int window, int i, int g,
+                               const float (&s)[8], f32x4 (&acc)[D / 16]) {
+  int at[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) at[r] = __shfl(pos, 4 * g + r);
+  for (int o = 0; o < 4; ++o) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = base + 8 * o + e;
+      float w[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) w[r] = __shfl(s[e], 16 * o + 4 * g + r);
+      if (j >= end) continue;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) {
+        const T v = *reinterpret_cast<const T*>(vb + j * a.v_token + Tile<T, D>::channel(n, i) * (int)sizeof(T));
+        if (!not_finite(v)) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (j <= at[r] && (at[r] - j < window || j < a.n_sink)) acc[n][r] += w[r] * (float)v;
+      }
+    }
+  }
+}
+
+// Few rows: a workgroup has 16, and its four waves share their keys.
+template <typename T, int D>
 __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(const AttnArgs a) {
   typedef Tile<T, D> Keys;
   __shared__ __attribute__((aligned(16))) char s_values[kAttnWaves][Keys::kLds];
-  __shared__ float s_join[kOnRows ? kAttnWaves * own_floats<D>() : join_floats<D>()];
+  __shared__ float s_join[join_floats<D>()];
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const AttnItem p = attn_item(a, (int)blockIdx.x, (int)blockIdx.y);
-  const int n_rows = p.nq * a.group, row0 = kOnRows ? (p.rt * kAttnWaves + wave) * kAttnRows : p.rt * kAttnRows;
-  if (kOnRows && row0 >= n_rows) return;
+  const int n_rows = p.nq * a.group, row0 = p.rt * kAttnRows;
   const int last = min(row0 + kAttnRows, n_rows) - 1;
   const int row = min(row0 + i, n_rows - 1);  // rows past the problem's repeat its last, and are not written
   const int query = row / a.group;
   const int pos = p.nk - p.nq + query;
   const Span sp = span_of(a, p, row0, last);
-  constexpr int kStep = kOnRows ? 1 : kAttnWaves;
-  const int first = p.split * p.tiles + (kOnRows ? 0 : wave);
+  const int first = p.split * p.tiles + wave;
   const int stop = min(sp.tiles, (p.split + 1) * p.tiles);
   const int window = a.window;
 
@@ -256,7 +301,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(const AttnArgs a)
 #pragma unroll
   for (int n = 0; n < D / 16; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   Keys now;
-  for (int x = first; x < stop; x += kStep) {
+  for (int x = first; x < stop; x += kAttnWaves) {
     const bool sink = x < sp.sink_tiles;
     const int base = sink ? x * kAttnTile : sp.lo + (x - sp.sink_tiles) * kAttnTile;
     const int end = sink ? sp.sinks : sp.end;
@@ -278,39 +323,111 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attn_kernel(const AttnArgs a)
     }
     st.update(s, acc);
     Keys::product(s, now, lds, lane, acc);
-    if (bad) {
-      // the values that are not finite, to the rows that see them (accumulator rows 4g .. 4g + 3)
-      int at[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) at[r] = __shfl(pos, 4 * g + r);
-      for (int o = 0; o < 4; ++o) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = base + 8 * o + e;
-          float w[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) w[r] = __shfl(s[e], 16 * o + 4 * g + r);
-          if (j >= end) continue;
-#pragma unroll
-          for (int n = 0; n < D / 16; ++n) {
-            const T v = *reinterpret_cast<const T*>(vb + j * a.v_token + Keys::channel(n, i) * (int)sizeof(T));
-            if (!not_finite(v)) continue;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (j <= at[r] && (at[r] - j < window || j < a.n_sink)) acc[n][r] += w[r] * (float)v;
-          }
-        }
-      }
-    }
+    if (bad) add_odd<T, D>(a, vb, base, end, pos, window, i, g, s, acc);
   }
-  const auto channel = [](int n, int lane16) { return Keys::channel(n, lane16); };
-  if constexpr (kOnRows) write_own<T, D>(a, p, row0, st, acc, s_join + wave * own_floats<D>(), channel);
-  else join_waves<T, D>(a, p, row0, st, acc, s_join, channel);
+  join_waves<T, D>(a, p, row0, st, acc, s_join, [](int n, int lane16) { return Keys::channel(n, lane16); });
 }
 
-template <typename T, int D, bool kOnRows>
+// Many rows, fp32: a workgroup has 64, 16 a wave, and goes over their keys once.  A tile comes from memory to LDS
+// without registers, into one of two buffers while the other is read, one barrier a tile.
+template <int D>
+__global__ __launch_bounds__(64 * kAttnWaves, 2) void attn_wide_kernel(const AttnArgs a) {
+  typedef Tile<float, D> Keys;
+  constexpr int kThreads = 64 * kAttnWaves, kRowBytes = D * 4, kPieces = kRowBytes / 16, kRowsAtOnce = kThreads / kPieces;
+  struct Tiles {
+    char k[2][kAttnTile * kRowBytes];
+    char v[2][kAttnTile * kRowBytes];
+  };
+  union Lds {
+    Tiles t;
+    float own[kAttnWaves * own_floats<D>()];
+  };
+  __shared__ __attribute__((aligned(16))) Lds lds;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // heads side by side, and the last rows of a sequence, which see most, first
+  const int h = (int)(blockIdx.x % (unsigned)a.n_heads);
+  const AttnItem p = attn_item(a, a.items - 1 - (int)(blockIdx.x / (unsigned)a.n_heads), h);
+  const int n_rows = p.nq * a.group, offset = p.nk - p.nq;
+  const Span sp = span_of(a, p, p.rt * kAttnWideRows, min((p.rt + 1) * kAttnWideRows, n_rows) - 1);
+  // the wave's rows (there may be none), and this lane's; rows past the problem's repeat its last
+  const int row0 = p.rt * kAttnWideRows + wave * kAttnRows;
+  const int wave_lo = offset + min(row0, n_rows - 1) / a.group;
+  const int wave_hi = offset + min(row0 + kAttnRows - 1, n_rows - 1) / a.group;
+  const int row = min(row0 + i, n_rows - 1);
+  const int query = row / a.group;
+  const int pos = offset + query;
+  const int window = a.window;
+
+  typename Keys::Query q;
+  q.load(a.q + ((int64_t)p.h * a.group + (row - query * a.group)) * a.q_head + (int64_t)(p.q0 + query) * a.q_token, g);
+  const char* kb = a.k + (int64_t)p.h * a.k_head + (int64_t)p.k0 * a.k_token;
+  const char* vb = a.v + (int64_t)p.h * a.v_head + (int64_t)p.k0 * a.v_token;
+
+  auto base_of = [&](int x) { return x < sp.sink_tiles ? x * kAttnTile : sp.lo + (x - sp.sink_tiles) * kAttnTile; };
+  auto end_of = [&](int x) { return x < sp.sink_tiles ? sp.sinks : sp.end; };
+  // A wave instruction fills 1 KB of LDS in lane order, so it is the source that is turned.  Past the end the last
+  // key comes again.
+  auto bring = [&](int x) {
+    const int base = base_of(x), end = end_of(x);
+    char* kl = lds.t.k[x & 1] + wave * 1024;
+    char* vl = lds.t.v[x & 1] + wave * 1024;
+#pragma unroll
+    for (int c = 0; c < kAttnTile / kRowsAtOnce; ++c) {
+      const int r = c * kRowsAtOnce + tid / kPieces, piece = tid % kPieces;
+      const int64_t t = min(base + r, end - 1);
+      to_lds(kb + t * a.k_token + (piece ^ Keys::turn(r)) * 16, kl + c * (kThreads * 16));
+      to_lds(vb + t * a.v_token + piece * 16, vl + c * (kThreads * 16));
+    }
+  };
+
+  RowStats st;
+  f32x4 acc[D / 16];
+#pragma unroll
+  for (int n = 0; n < D / 16; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (sp.tiles > 0) bring(0);
+  for (int x = 0; x < sp.tiles; ++x) {
+    // tile x lies in LDS (the barrier alone does not wait for a wave's loads to LDS), and nobody reads the other
+    // buffer
+    __builtin_amdgcn_s_waitcnt(kNoLoads);
+    __syncthreads();
+    if (x + 1 < sp.tiles) bring(x + 1);
+    const int base = base_of(x), end = end_of(x);
+    if (row0 >= n_rows || base > wave_hi || (base + kAttnTile <= wave_lo - window + 1 && base >= a.n_sink))
+      continue;  // nothing for this wave's rows
+    Keys now;
+    now.load(lds.t.k[x & 1], lds.t.v[x & 1], lane);
+    const bool all = base + kAttnTile <= end && base + kAttnTile - 1 <= wave_lo &&
+                     (base > wave_hi - window || base + kAttnTile <= a.n_sink);
+    bool bad = false;
+    if (!all) bad = now.clean(base, end, lane);
+    float s[8];
+    now.scores(q, s);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s[e] *= a.scale_log2;
+      if (!all) {
+        const int j = base + 8 * g + e;
+        if (!((j < end) & (j <= pos) & ((pos - j < window) | (j < a.n_sink)))) s[e] = kNegInf;
+      }
+    }
+    st.update(s, acc);
+    Keys::product(s, now, nullptr, lane, acc);
+    if (bad) add_odd<float, D>(a, vb, base, end, pos, window, i, g, s, acc);
+  }
+  __syncthreads();  // the rows go out through the tiles' place
+  write_own<float, D>(a, p, row0, st, acc, lds.own + wave * own_floats<D>(),
+                      [](int n, int lane16) { return Keys::channel(n, lane16); });
+}
+
+template <typename T, int D>
 int run(const AttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attn_kernel<T, D, kOnRows>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
+  hipLaunchKernelGGL((attn_kernel<T, D>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
+  return hipGetLastError();
+}
+template <int D>
+int run_wide(const AttnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((attn_wide_kernel<D>), dim3((unsigned)a.items * (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
   return hipGetLastError();
 }
 
@@ -318,9 +435,9 @@ int run(const AttnArgs& a, hipStream_t s) {
 
 int launch_attn(const AttnArgs& a, int dtype, int d, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == 0) return d == 128 ? run<bf16, 128, false>(a, s) : run<bf16, 64, false>(a, s);
-  if (a.rows == kAttnWideRows) return d == 128 ? run<float, 128, true>(a, s) : run<float, 64, true>(a, s);
-  return d == 128 ? run<float, 128, false>(a, s) : run<float, 64, false>(a, s);
+  if (dtype == 0) return d == 128 ? run<bf16, 128>(a, s) : run<bf16, 64>(a, s);
+  if (a.rows == kAttnWideRows) return d == 128 ? run_wide<128>(a, s) : run_wide<64>(a, s);
+  return d == 128 ? run<float, 128>(a, s) : run<float, 64>(a, s);
 }
 
 }  // namespace twinkv

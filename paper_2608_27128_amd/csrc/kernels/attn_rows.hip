@@ -57,12 +57,6 @@ __device__ inline int v_unit(int row, int unit) {
   return unit ^ (D == 128 ? 2 * (row & 3) : 2 * ((row >> 1) & 1));
 }
 
-__device__ inline void to_lds(const char* from, char* to) {  // 16 bytes a lane, `to` the wave's first
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-}
-constexpr int kNoLoads = 0x0f70;  // s_waitcnt: vmcnt 0, the other counters at their largest
-
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a) {
   constexpr int kSteps = D / 16;          // of the contraction over channels

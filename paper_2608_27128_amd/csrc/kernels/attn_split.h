@@ -25,6 +25,12 @@ constexpr float kSlack = 8.0f;
 constexpr int kAttnWaves = 4;
 constexpr float kNegInf = -__builtin_huge_valf();
 
+__device__ inline void to_lds(const char* from, char* to) {  // 16 bytes a lane, `to` the wave's first
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+constexpr int kNoLoads = 0x0f70;  // s_waitcnt: vmcnt 0, the other counters at their largest
+
 __device__ inline float group_max(float x) {  // over the 4 lane groups
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));

@@ -669,3 +669,63 @@ def test_outputs_whose_heads_overlap_are_refused():
     got = binding.sink_attention(q, k[:1].expand(H, T, d), v[:1].expand(H, T, d), 4)["out"]
     want = binding.sink_attention(q, k[:1].repeat(H, 1, 1), v[:1].repeat(H, 1, 1), 4)["out"]
     assert torch.equal(got, want)
+
+
+# fp32 with rows enough that workgroups of four row tiles go over keys of their own: a ragged batch with sinks that
+# end inside a tile, plain causal, rows before the first key, a window of no key but the row's own, many short ones
+WIDE = [((400, 1, 0, 37, 350, 600), (400, 1, 0, 37, 100, 600), 90, 33, 3), ((1100,), (1100,), 1 << 40, 0, 4),
+        ((300,) * 6, (350,) * 6, 1 << 20, 0, 4), ((900,), (900,), 1, 0, 4), ((70, 65, 64, 63, 1) * 8,) * 2 + (1 << 20, 0, 5),
+        ((1200,), (700,), 0, 70, 4)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", range(len(WIDE)))
+def test_sink_attention_wide_fp32(case, d):
+    lens, nq, window, sink, G = WIDE[case]
+    g = gen(500 + case)
+    H = 8
+    cu_q, cu_k = cum(nq), cum(lens)
+    q = randn(g, H * G, sum(nq), d, dtype="f32")
+    k, v = randn(g, H, sum(lens), d, dtype="f32"), randn(g, H, sum(lens), d, dtype="f32")
+    got = binding.sink_attention(q, k, v, window, sink, None, cu_q, cu_k, want_lse=True)
+    check_attention(got["out"], q, k, v, cu_q, cu_k, lambda s, h, m, n: ref.seen_by(m, n, window, sink), d ** -0.5,
+                    "f32", got["lse"], heads=[0, G, H * G - 1])
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_sink_attention_wide_fp32_unseen_values_do_not_matter(bad):
+    import torch
+    g = gen(520)
+    H, G, d, n, W, sink = 8, 4, 128, 600, 64, 4
+    q, k, v = randn(g, H * G, n, d, dtype="f32"), randn(g, H, n, d, dtype="f32"), randn(g, H, n, d, dtype="f32")
+    clean = binding.sink_attention(q, k, v, W, sink)["out"]
+    seen = ref.seen_by(n, n, W, sink).cuda()
+    for j in (2, 17, 300, n - 1):
+        v2 = v.clone()
+        v2[:, j, 77] = bad
+        got = binding.sink_attention(q, k, v2, W, sink)["out"]
+        hit = torch.zeros((H * G, n, d), dtype=torch.bool, device="cuda")
+        hit[:, seen[:, j], 77] = True
+        assert torch.equal(got[~hit], clean[~hit]), j
+        assert not bool(torch.isfinite(got[hit]).any()), j
+
+
+def test_sink_attention_wide_fp32_in_a_graph():
+    """Recorded and replayed after other work, on another stream's tensors."""
+    import torch
+    g = gen(521)
+    H, G, d, n = 8, 4, 64, 500
+    q, k, v = randn(g, H * G, n, d, dtype="f32"), randn(g, H, n, d, dtype="f32"), randn(g, H, n, d, dtype="f32")
+    out = torch.empty_like(q)
+    binding.sink_attention(q, k, v, 100, 4, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.sink_attention(q, k, v, 100, 4, out=out)
+    for t in range(3):
+        q.copy_(randn(g, H * G, n, d, dtype="f32"))
+        want = binding.sink_attention(q, k, v, 100, 4)["out"]
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), t
