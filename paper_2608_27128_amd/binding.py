@@ -715,9 +715,9 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, eps: float = 1e-6, rope=Non
                  q_out=None, k_out=None) -> dict:
     """RMS norm of each head of q (Hq, T, d) and k (Hk, T, d) (a weight (d,) float32 each; None: not
     normalised) and the rotary embedding by ``rope`` (n_pos, d) float32 (cos of the d/2 pairs, then
-    sin; None: no rotation) at ``positions`` (T,) int32.  Channel c turns with c + d/2.  A projection's
-    token-major output goes in as its (H, T, d) view.  q or k may be None.  The outputs may be the
-    inputs."""
+    sin; None: no rotation) at ``positions`` (T,) int32.  Channel c turns with c + d/2; a token whose position
+    is no row of the table gets NaN.  A projection's token-major output goes in as its (H, T, d) view.  q or k
+    may be None.  The outputs may be the inputs."""
     torch = _torch()
     some = q if q is not None else k
     if some is None:
@@ -740,6 +740,9 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, eps: float = 1e-6, rope=Non
             raise ValueError("positions is required with rope")
         rope = _small(rope, (rope.shape[0], d), f32, dev, "rope")
         positions = _small(positions, (T,), torch.int32, dev, "positions")
+    n_pos = 0 if rope is None else rope.shape[0]
+    # a table without rows has no address, and none is the library's "no rotation"
+    table = torch.empty((1, d), dtype=f32, device=dev) if rope is not None and n_pos == 0 else rope
     out = {}
     args = {"q": (None, 0, 0, 0, None, 0, 0), "k": (None, 0, 0, 0, None, 0, 0)}
     for name, x, to in (("q", q, q_out), ("k", k, k_out)):
@@ -751,7 +754,7 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, eps: float = 1e-6, rope=Non
         args[name] = (x.data_ptr(), x.shape[0], x.stride(0), x.stride(1), o.data_ptr(), o.stride(0), o.stride(1))
     qa, ka = args["q"], args["k"]
     _launch(dev, "twinkv_qk_norm_rope", qa[0], ka[0], dt, d, qa[1], ka[1], T, qa[2], qa[3], ka[2], ka[3],
-            _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(rope), 0 if rope is None else rope.shape[0],
+            _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(table), n_pos,
             None if rope is None else positions.data_ptr(), qa[4], qa[5], qa[6], ka[4], ka[5], ka[6], _stream(dev))
     return out
 
