@@ -35,14 +35,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(const NormRopeArgs 
   const int c0 = (threadIdx.x % kLanes) * 8;  // first channel of this lane in either half
   if (t >= a.T) return;  // whole rows of lanes
 
-  float cs[8], sn[8], w0[8], w1[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    cs[e] = 1.0f;
-    sn[e] = 0.0f;
-    w0[e] = 1.0f;
-    w1[e] = 1.0f;
-  }
+  float cs[8] = {}, sn[8] = {}, w0[8] = {}, w1[8] = {};
   if (a.rope != nullptr) {
     const int64_t p = a.pos[t];
     const bool in = p >= 0 && p < a.n_pos;
@@ -87,15 +80,17 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(const NormRopeArgs 
           v[e] *= r * w1[e];
         }
       }
-      float x[8], y[8];
+      if (a.rope != nullptr) {  // (not a turn by 0, which would make NaN of the partner of an infinity)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = u[e] * cs[e] - v[e] * sn[e];
-        y[e] = v[e] * cs[e] + u[e] * sn[e];
+        for (int e = 0; e < 8; ++e) {
+          const float x = u[e];
+          u[e] = x * cs[e] - v[e] * sn[e];
+          v[e] = v[e] * cs[e] + x * sn[e];
+        }
       }
       char* p = out + (int64_t)(h + b) * s.out_head;
-      Vec8<T>::from(x).store(p);
-      Vec8<T>::from(y).store(p + kHalf);
+      Vec8<T>::from(u).store(p);
+      Vec8<T>::from(v).store(p + kHalf);
     }
   }
 }
