@@ -334,9 +334,11 @@ int twinkv_compact(const void* keys, const void* values, int dtype, int d, int n
  * Rows of channels.  In the calls below q, k, v and their outputs are addressed like the keys above:
  * element (head, token, c) at p[head*head_stride + token*token_stride + c], pointer and byte strides
  * multiples of 16, so a projection's token-major output (head_stride = d, token_stride = heads*d) is
- * taken as it is.  An input may repeat one head (head_stride 0), outputs may not overlap.  d is 64 or 128;
- * bf16 or fp32, one type in a call.  `group` query heads share a KV
- * head: query head h*group + g reads KV head h.  These are inference calls: none has a gradient.
+ * taken as it is.  An input may repeat one head (head_stride 0), outputs may not overlap (refused: a
+ * head_stride below d, and heads that lie at least as far apart as tokens and meet; that the heads of a
+ * token-major output end before its next token is the caller's to keep).  d is 64 or 128; bf16 or fp32, one
+ * type in a call.  `group` query heads share a KV head: query head h*group + g reads KV head h.  These are
+ * inference calls: none has a gradient.
  */
 
 /*

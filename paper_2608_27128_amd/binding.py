@@ -676,6 +676,21 @@ def _rows(x, name: str, dtype=None, d=None, dev=None):
     return x, dt
 
 
+def _rows_overlap(heads: int, T: int, h: int, t: int, d: int) -> bool:
+    """Whether two of the rows of d channels at head * h + token * t (t >= d) share a place."""
+    if heads < 2:
+        return False
+    if h < d:
+        return True
+    if T < 2 or h >= (T - 1) * t + d or t >= (heads - 1) * h + d:
+        return False
+    for at in range(h, min(heads * h, (T - 1) * t + d), h):  # the distance of two heads, against that of tokens
+        token = min(at // t, T - 1)
+        if at - token * t < d or (token < T - 1 and (token + 1) * t - at < d):
+            return True
+    return False
+
+
 def _out_rows(out, shape, like, name: str):
     """The caller's output rows (written in place, so they must be addressable as they are), or new ones."""
     if out is None:
@@ -685,7 +700,7 @@ def _out_rows(out, shape, like, name: str):
                          f"{tuple(out.shape)} {out.dtype} on {out.device}")
     h, t, c = out.stride()
     lanes = 16 // out.element_size()
-    if c != 1 or t % lanes or h % lanes or t < shape[2] or out.data_ptr() % 16 or (h < shape[2] and shape[0] > 1):
+    if c != 1 or t % lanes or h % lanes or t < shape[2] or out.data_ptr() % 16 or _rows_overlap(shape[0], shape[1], h, t, shape[2]):
         raise ValueError(f"{name} must have contiguous channels, strides of multiples of 16 bytes and no overlap")
     return out
 

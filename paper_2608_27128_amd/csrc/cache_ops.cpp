@@ -55,6 +55,21 @@ int check_out(const void* p, int dtype, int d, int64_t head_stride, int64_t toke
   return rc == TWINKV_OK && !empty && heads > 1 && head_stride < d ? TWINKV_E_ARG : rc;
 }
 
+// Whether rows (head, token) and (head', token') of an output with head_stride >= token_stride >= d share a place.
+// Heads dh apart lie dh * head_stride apart, and the nearest that a token comes to that is one of two.
+bool heads_overlap(int64_t head_stride, int64_t token_stride, int64_t heads, int64_t T, int d) {
+  typedef __int128 Wide;
+  if (T < 2 || head_stride < token_stride) return false;
+  const Wide last = (Wide)(T - 1) * token_stride;
+  for (int64_t dh = 1; dh < heads; ++dh) {
+    const Wide at = (Wide)dh * head_stride;
+    if (at >= last + d) break;
+    const Wide token = std::min(at / token_stride, (Wide)(T - 1)), below = at - token * token_stride;
+    if (below < d || (token < T - 1 && token_stride - below < d)) return true;
+  }
+  return false;
+}
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 // Collects a call's per-sequence words: into the kernel arguments, or piece by piece into the workspace.
@@ -324,6 +339,7 @@ int attn_args(KeysAre keys, const void* q, int dtype, int d, int n_heads, int gr
   if (rc != TWINKV_OK) return rc;
   const AttnLayout L = attn_layout(p, d, n_heads, n_seqs);
   if (L.total > 0 && (workspace == nullptr || workspace_bytes < (int64_t)L.total)) return TWINKV_E_WORKSPACE;
+  if (heads_overlap(out_head_stride, out_token_stride, (int64_t)n_heads * group, cu_q[n_seqs], d)) return TWINKV_E_ARG;
   char* ws = L.total > 0 ? aligned_base(workspace) : nullptr;
   const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
   a.q = static_cast<const char*>(q);
@@ -400,6 +416,9 @@ int twinkv_qk_norm_rope(const void* q, const void* k, int dtype, int d, int n_q_
     if (n_pos < 0) return TWINKV_E_ARG;
     if (positions == nullptr && T > 0) return TWINKV_E_NULL;
   }
+  if (heads_overlap(qo_head_stride, qo_token_stride, no_q ? 0 : n_q_heads, T, d) ||
+      heads_overlap(ko_head_stride, ko_token_stride, no_k ? 0 : n_k_heads, T, d))
+    return TWINKV_E_ARG;
   if (no_q && no_k) return TWINKV_OK;
   if (!grid_ok((T + 31) / 32, 256)) return TWINKV_E_ARG;
   const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;

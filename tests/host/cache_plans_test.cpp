@@ -1,0 +1,97 @@
+// More of the host layer of the operators around the cache (csrc/cache_ops.cpp) on the CPU, under sanitizers, with
+// stand-ins for the launchers: which outputs are refused because two of their rows share a place.
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <random>
+#include <vector>
+
+#include "cache_ops.h"
+#include "twinkv.h"
+
+#define CHECK(x)                                                        \
+  do {                                                                  \
+    if (!(x)) {                                                         \
+      std::fprintf(stderr, "%s:%d: %s\n", __FILE__, __LINE__, #x);      \
+      std::exit(1);                                                     \
+    }                                                                   \
+  } while (0)
+
+namespace twinkv {
+int launch_upload(const void* src, size_t bytes, void* dst, void*) {
+  std::memcpy(dst, src, bytes);
+  return 0;
+}
+int launch_norm_rope(const NormRopeArgs&, int, int, void*) { return 0; }
+int launch_attn(const AttnArgs&, int, int, void*) { return 0; }
+int launch_attn_rows(const AttnArgs&, int, void*) { return 0; }
+int launch_attn4(const AttnArgs&, int, int, void*) { return 0; }
+int launch_attn_join(const AttnArgs&, int, int, void*) { return 0; }
+int launch_cache4_positions(const Cache4Args&, void*) { return 0; }
+int launch_cache4_gather(const Cache4Args&, int, int, void*) { return 0; }
+int launch_cache4_append(const Cache4Args&, int, int, int, void*) { return 0; }
+int launch_cache4_read(const Cache4Args&, int, int, void*) { return 0; }
+}  // namespace twinkv
+
+namespace {
+void* const fake = reinterpret_cast<void*>(0x100000);
+
+bool overlap(int64_t heads, int64_t T, int64_t hs, int64_t ts, int64_t d) {
+  std::vector<int64_t> at;
+  for (int64_t h = 0; h < heads; ++h)
+    for (int64_t t = 0; t < T; ++t) at.push_back(h * hs + t * ts);
+  std::sort(at.begin(), at.end());
+  for (size_t i = 1; i < at.size(); ++i)
+    if (at[i] - at[i - 1] < d) return true;
+  return false;
+}
+
+// What each call with an output says to rows at these strides (8 elements are 16 bytes or more of both types).
+void check_output(int64_t heads, int64_t T, int64_t hs, int64_t ts, int d, int dtype, int code) {
+  CHECK(twinkv_qk_norm_rope(fake, fake, dtype, d, (int)heads, 1, T, d * T, d, d * T, d, nullptr, nullptr, 1e-6f, nullptr, 0,
+                            nullptr, fake, hs, ts, fake, d * T, d, nullptr) == code);
+  CHECK(twinkv_qk_norm_rope(nullptr, fake, dtype, d, 0, (int)heads, T, 0, 0, d * T, d, nullptr, nullptr, 1e-6f, nullptr, 0,
+                            nullptr, nullptr, 0, 0, fake, hs, ts, nullptr) == code);
+  const int64_t cq[2] = {0, T}, ck[2] = {0, 64};
+  CHECK(twinkv_sink_attention(fake, fake, fake, dtype, d, 1, (int)heads, 1, cq, ck, d * T, d, 64 * d, d, 64 * d, d, 64, 0,
+                              0.1f, fake, hs, ts, nullptr, nullptr, 0, nullptr) == code);
+  const twinkv_cache4 c{d, (int)heads, 1, ck, fake, fake, fake, fake};
+  CHECK(twinkv_cache4_attention(fake, dtype, 1, cq, d * T, d, &c, static_cast<int32_t*>(fake), 0.1f, fake, hs, ts, nullptr,
+                                nullptr, 0, nullptr) == code);
+}
+
+void outputs() {
+  std::mt19937_64 g(11);
+  auto from = [&](int64_t a, int64_t b) { return a + (int64_t)(g() % (uint64_t)(b - a + 1)); };
+  int64_t refused = 0, odd = 0;
+  for (int round = 0; round < 20000; ++round) {
+    const int d = round % 2 ? 128 : 64;
+    const int64_t heads = from(1, 9), T = from(1, 40);
+    const int64_t ts = d + 8 * from(0, round % 3 ? 2 : 60);
+    // heads apart by a few tokens and a bit, or by about all of them
+    const int64_t hs = from(0, 1) ? ts * from(1, 6) + 8 * from(0, ts / 8) : ts * T + 8 * from(-ts / 8, 4);
+    if (hs < ts) continue;
+    const bool meet = overlap(heads, T, hs, ts, d);
+    refused += meet;
+    odd += !meet && heads > 1 && T > 1 && hs < (T - 1) * ts + d;  // heads between each other's tokens
+    check_output(heads, T, hs, ts, d, (int)from(0, 1), meet ? TWINKV_E_ARG : TWINKV_OK);
+  }
+  for (const int d : {64, 128}) {
+    check_output(4, 3, d, d, d, 0, TWINKV_E_ARG);
+    check_output(2, 3, 2 * d, d, d, 0, TWINKV_E_ARG);
+    check_output(2, 2, 2 * d, d, d, 0, TWINKV_OK);
+    check_output(4, 1, d, d, d, 0, TWINKV_OK);          // one token: the heads side by side
+    check_output(4, 3, d, 4 * d, d, 0, TWINKV_OK);      // token major
+    check_output(3, 3, INT64_MAX / 16 * 8, INT64_MAX / 16 * 8, d, 0, TWINKV_E_ARG);
+  }
+  CHECK(refused > 1000 && odd > 100);
+  std::printf("outputs: %lld refused, %lld interleaved\n", (long long)refused, (long long)odd);
+}
+}  // namespace
+
+int main() {
+  outputs();
+  std::printf("cache plans ok\n");
+  return 0;
+}
