@@ -705,6 +705,13 @@ def _out_rows(out, shape, like, name: str):
     return out
 
 
+def _no_gradient(fn: str, *tensors) -> None:
+    """These calls return tensors that torch's autograd does not know of: where it would record one, the
+    gradient would be lost without a word."""
+    if _torch().is_grad_enabled() and any(x is not None and x.requires_grad for x in tensors):
+        raise ValueError(f"{fn} has no gradient: call it under torch.no_grad(), or on detached tensors")
+
+
 def _small(x, shape, dtype, dev, name: str):
     """A contiguous, 16-byte aligned operand of one exact shape and type (None stays None)."""
     if x is None:
@@ -732,11 +739,13 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, eps: float = 1e-6, rope=Non
     normalised) and the rotary embedding by ``rope`` (n_pos, d) float32 (cos of the d/2 pairs, then
     sin; None: no rotation) at ``positions`` (T,) int32.  Channel c turns with c + d/2; a token whose position
     is no row of the table gets NaN.  A projection's token-major output goes in as its (H, T, d) view.  q or k
-    may be None.  The outputs may be the inputs."""
+    may be None.  The outputs may be the inputs.  There is no gradient: inputs that require one are refused
+    (torch.no_grad() lifts that)."""
     torch = _torch()
     some = q if q is not None else k
     if some is None:
         raise ValueError("q or k is required")
+    _no_gradient("qk_norm_rope", q, k, q_weight, k_weight, rope, q_out, k_out)
     dt = T = d = None
     if q is not None:
         q, dt = _rows(q, "q")
@@ -797,8 +806,11 @@ def sink_attention(q, k, v, window: int, n_sink: int = 4, scale: Optional[float]
     """Causal attention over a sliding window and the first ``n_sink`` tokens.  q (Hq, Tq, d) are the
     last tokens of each sequence, k and v (H, Tk, d) all of its tokens; query head h reads KV head
     h // (Hq // H).  A query at position p sees j <= p with p - j < window or j < n_sink.  scale defaults to
-    1 / sqrt(d).  Returns out, and lse (Hq, Tq) float32 with ``want_lse``."""
+    1 / sqrt(d).  Returns out, and lse (Hq, Tq) float32 with ``want_lse``.  For bfloat16 the softmax weights are
+    rounded to bfloat16 for the product with v, for float32 nothing is.  There is no gradient: inputs that
+    require one are refused (torch.no_grad() lifts that)."""
     torch = _torch()
+    _no_gradient("sink_attention", q, k, v, out)
     q, dt = _rows(q, "q")
     Hq, Tq, d = q.shape
     dev = q.device
@@ -964,8 +976,11 @@ def cache4_attention(q, cache: Cache4, length, scale: Optional[float] = None, cu
                      want_lse: bool = False, out=None, workspace=None) -> dict:
     """Attention of q (Hq, Tq, d), the last tokens [cu_q[s], cu_q[s + 1]) of each cached sequence, over the
     ``length`` (n_heads, n_seqs) int32 rows in use: query i of m sees the first length - (m - 1 - i) of
-    them.  scale defaults to 1 / sqrt(d).  Returns out, and lse (Hq, Tq) float32 with ``want_lse``."""
+    them.  scale defaults to 1 / sqrt(d).  Returns out, and lse (Hq, Tq) float32 with ``want_lse``.  For bfloat16
+    the softmax weights, times the values' scales, are rounded to bfloat16; for float32 they keep 24 bits.  There
+    is no gradient: a q that requires one is refused (torch.no_grad() lifts that)."""
     torch = _torch()
+    _no_gradient("cache4_attention", q, out)
     dev = cache.device
     q, dt = _rows(q, "q", None, cache.d, dev)
     Hq, Tq, d = q.shape

@@ -52,3 +52,26 @@ def test_binding_refuses_outputs_whose_rows_overlap():
             kept += 1
             assert binding._out_rows(out, (heads, T, d), like, "out") is out
     assert refused > 500 and kept > 500
+
+
+def test_binding_refuses_inputs_that_require_a_gradient():
+    """Before anything else, so that CPU tensors show it; under no_grad the next check speaks."""
+    import torch
+    x = torch.zeros((2, 8, 128), dtype=torch.bfloat16)
+    y = x.clone().requires_grad_()
+    w = torch.ones(128, requires_grad=True)
+    rope, pos = torch.zeros((8, 128), requires_grad=True), torch.zeros(8, dtype=torch.int32)
+
+    class Cache:
+        d, n_heads, n_seqs, device = 128, 2, 1, x.device
+    calls = [lambda: binding.qk_norm_rope(y, None), lambda: binding.qk_norm_rope(x, y), lambda: binding.qk_norm_rope(x, x, w),
+             lambda: binding.qk_norm_rope(x, x, None, w), lambda: binding.qk_norm_rope(x, x, rope=rope, positions=pos),
+             lambda: binding.qk_norm_rope(x, None, q_out=y), lambda: binding.sink_attention(y, x, x, 8),
+             lambda: binding.sink_attention(x, y, x, 8), lambda: binding.sink_attention(x, x, y, 8),
+             lambda: binding.sink_attention(x, x, x, 8, out=y), lambda: binding.cache4_attention(y, Cache, pos),
+             lambda: binding.cache4_attention(x, Cache, pos, out=y)]
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+            call()
