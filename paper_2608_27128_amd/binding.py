@@ -221,8 +221,11 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream(device) -> int:
-    # the handle alone: building torch's stream object costs a small call more than its launch
-    return _torch()._C._cuda_getCurrentRawStream(device.index)
+    # the handle alone, where torch has it (the name is not of its documented interface): building its stream
+    # object costs a small call more than its launch
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream(device).cuda_stream if raw is None else raw(device.index)
 
 
 def _mask(x, n_heads, T, device, name):

@@ -5,6 +5,7 @@ import os
 import random
 import shutil
 import subprocess
+from types import SimpleNamespace
 
 import pytest
 
@@ -75,3 +76,12 @@ def test_binding_refuses_inputs_that_require_a_gradient():
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
             call()
+
+
+@pytest.mark.parametrize("raw", [None, lambda index: 100 + index])
+def test_stream_handle_with_and_without_torch_private_name(monkeypatch, raw):
+    """A torch without the undocumented function for a stream's handle gives it by its stream object."""
+    c = SimpleNamespace() if raw is None else SimpleNamespace(_cuda_getCurrentRawStream=raw)
+    cuda = SimpleNamespace(current_stream=lambda device: SimpleNamespace(cuda_stream=100 + device.index))
+    monkeypatch.setattr(binding, "_torch", lambda: SimpleNamespace(_C=c, cuda=cuda))
+    assert binding._stream(SimpleNamespace(index=3)) == 103
