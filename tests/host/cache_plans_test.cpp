@@ -1,5 +1,6 @@
 // More of the host layer of the operators around the cache (csrc/cache_ops.cpp) on the CPU, under sanitizers, with
-// stand-ins for the launchers: which outputs are refused because two of their rows share a place.
+// stand-ins for the launchers: which outputs are refused because two of their rows share a place, and which kernel and
+// splits the attention chooses where a test or a bound counts on them.
 #include <algorithm>
 #include <cstdio>
 #include <cstdlib>
@@ -18,15 +19,30 @@
     }                                                                   \
   } while (0)
 
+namespace {
+// The last attention: rows of an item, and each sequence's splits.
+int g_rows = 0;
+std::vector<int64_t> g_splits;
+int planned(const twinkv::AttnArgs& a) {
+  g_rows = a.rows;
+  g_splits.clear();
+  for (int s = 0; s < a.n_seqs; ++s) {
+    const int64_t w = (int64_t)s * twinkv::kAttnSeqWords + 3;
+    g_splits.push_back(a.seq.far ? a.seq.far[w] : a.seq.near[w]);
+  }
+  return 0;
+}
+}  // namespace
+
 namespace twinkv {
 int launch_upload(const void* src, size_t bytes, void* dst, void*) {
   std::memcpy(dst, src, bytes);
   return 0;
 }
 int launch_norm_rope(const NormRopeArgs&, int, int, void*) { return 0; }
-int launch_attn(const AttnArgs&, int, int, void*) { return 0; }
-int launch_attn_rows(const AttnArgs&, int, void*) { return 0; }
-int launch_attn4(const AttnArgs&, int, int, void*) { return 0; }
+int launch_attn(const AttnArgs& a, int, int, void*) { return planned(a); }
+int launch_attn_rows(const AttnArgs& a, int, void*) { return planned(a); }
+int launch_attn4(const AttnArgs& a, int, int, void*) { return planned(a); }
 int launch_attn_join(const AttnArgs&, int, int, void*) { return 0; }
 int launch_cache4_positions(const Cache4Args&, void*) { return 0; }
 int launch_cache4_gather(const Cache4Args&, int, int, void*) { return 0; }
@@ -88,10 +104,44 @@ void outputs() {
   CHECK(refused > 1000 && odd > 100);
   std::printf("outputs: %lld refused, %lld interleaved\n", (long long)refused, (long long)odd);
 }
+
+typedef std::vector<int64_t> Lens;
+void attend(int dtype, int d, int H, int G, const Lens& nq, const Lens& nk, int64_t window, int64_t sink) {
+  Lens cq{0}, ck{0};
+  for (size_t s = 0; s < nq.size(); ++s) {
+    cq.push_back(cq.back() + nq[s]);
+    ck.push_back(ck.back() + nk[s]);
+  }
+  const int S = (int)nq.size();
+  const int64_t need = twinkv_attention_workspace_bytes(dtype, d, H, G, S, cq.data(), ck.data(), window, sink);
+  CHECK(need >= 0 && need < (int64_t)1 << 31);
+  std::vector<char> ws((size_t)std::max<int64_t>(need, 1));
+  const int64_t t = (int64_t)d * H * G;
+  CHECK(twinkv_sink_attention(fake, fake, fake, dtype, d, H, G, S, cq.data(), ck.data(), d, t, d, (int64_t)d * H, d,
+                              (int64_t)d * H, window, sink, 0.1f, fake, d, t, nullptr, ws.data(), need, nullptr) == TWINKV_OK);
+}
+
+// The shapes of tests/test_gpu_cache_ops_edges.py that are there for split keys in the kernel for many bf16 rows.
+void many_rows_split() {
+  const int64_t all = (int64_t)1 << 40;
+  auto split = [&](int d, int H, int G, const Lens& nq, const Lens& nk, int64_t window, int64_t sink) {
+    attend(0, d, H, G, nq, nk, window, sink);
+    CHECK(g_rows == twinkv::kAttnBigRows && *std::max_element(g_splits.begin(), g_splits.end()) > 1);
+  };
+  for (const int d : {64, 128}) {
+    split(d, 4, 4, {200}, {5000}, 1 << 20, 4);
+    split(d, 4, 8, {150}, {9000}, 6000, 70);
+    split(d, 4, 4, {130, 60, 0, 301}, {7001, 90, 0, 5000}, all, 0);
+    CHECK(g_splits[1] == 1);
+    split(d, 2, 5, {513}, {6000}, 2500, 33);
+    split(d, 4, 4, {200}, {6000}, 4000, 4);
+  }
+}
 }  // namespace
 
 int main() {
   outputs();
+  many_rows_split();
   std::printf("cache plans ok\n");
   return 0;
 }

@@ -1,11 +1,12 @@
 """Edges of the operators around the cache on the GPU, against plain 64-bit forms (cache_ops_ref.py)."""
 import math
 
+import numpy as np
 import pytest
 
 import cache_ops_ref as ref
 from paper_2608_27128_amd import binding
-from test_gpu_cache_ops import check_rope, gen, randn
+from test_gpu_cache_ops import check_rope, cum, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +50,53 @@ def test_without_rotation_a_channel_is_its_own(dtype, d):
     got = binding.qk_norm_rope(q, k, w, w, 1e-6)
     for name, x in (("q", q), ("k", k)):
         check_rope(got[name], ref.norm_rope(x.double(), w, 1e-6, None, None), d, dtype)
+
+
+# bf16 with rows enough for the kernel of 128 rows and row tiles too few for the machine, so that it splits keys: a
+# chunk over long keys, a window far from sinks that end inside a tile, a batch whose sequences split and do not
+# (tests/host/cache_plans_test.cpp holds the host layer to these plans)
+BIG_SPLIT = [((5000,), (200,), 1 << 20, 4, 4, 4), ((9000,), (150,), 6000, 70, 8, 4), ((7001, 90, 0, 5000), (130, 60, 0, 301), 1 << 40, 0, 4, 4),
+             ((6000,), (513,), 2500, 33, 5, 2)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", range(len(BIG_SPLIT)))
+def test_sink_attention_many_rows_split(case, d):
+    import torch
+    lens, nq, window, sink, G, H = BIG_SPLIT[case]
+    g = gen(1100 + case)
+    cu_q, cu_k = cum(nq), cum(lens)
+    q = randn(g, sum(nq), H * G, d).transpose(0, 1)
+    k, v = randn(g, H, sum(lens), d), randn(g, H, sum(lens), d)
+    k = k + 2 * randn(g, H, 1, d)
+    got = binding.sink_attention(q, k, v, window, sink, None, cu_q, cu_k, want_lse=True)
+    for s, (m, n) in enumerate(zip(nq, lens)):
+        if m == 0:
+            continue
+        rows = torch.tensor(sorted({0, m - 1, *(int(x) for x in np.linspace(0, m - 1, 23))}), device="cuda")
+        seen = ref.seen_by(m, n, window, sink).cuda()[rows]
+        a, x = int(cu_q[s]), int(cu_k[s])
+        for h in sorted({0, G - 1, H * G - 1}):
+            o, e, mass, size = ref.softmax_rows(q[h, a + rows].double(), k[h // G, x:x + n].double(),
+                                                v[h // G, x:x + n].double(), seen, d ** -0.5)
+            tol, tol_e = ref.attention_bounds(o, e, mass, size, n, d, True)
+            assert bool(((got["out"][h, a + rows].double() - o).abs() <= tol).all()), (s, h)
+            assert bool(((got["lse"][h, a + rows].double() - e).abs() <= tol_e).all()), (s, h)
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_sink_attention_many_rows_split_unseen_values_do_not_matter(bad):
+    import torch
+    g = gen(1150)
+    H, G, d, n, m, W, sink = 4, 4, 128, 6000, 200, 4000, 4
+    q, k, v = randn(g, H * G, m, d), randn(g, H, n, d), randn(g, H, n, d)
+    clean = binding.sink_attention(q, k, v, W, sink, None, [0, m], [0, n])["out"]
+    seen = ref.seen_by(m, n, W, sink).cuda()
+    for j in (2, 900, n - m - W + 1, n - m + 1, 3000, n - 1):
+        v2 = v.clone()
+        v2[:, j, 77] = bad
+        got = binding.sink_attention(q, k, v2, W, sink, None, [0, m], [0, n])["out"]
+        hit = torch.zeros((H * G, m, d), dtype=torch.bool, device="cuda")
+        hit[:, seen[:, j], 77] = True
+        assert torch.equal(got[~hit], clean[~hit]), j
+        assert not bool(torch.isfinite(got[hit]).any()), j
