@@ -183,6 +183,9 @@ struct AttnPlan {
   int rows = kAttnRows, keys = kAttnTile;  // of a tile
   int64_t split_tiles = 0;                 // the most key tiles of a split
   int64_t whole_tiles = 0;                 // up to so many are not split
+  // a sequence with fewer row tiles than lone_rows (of all heads) and more key tiles than lone_run: its splits have
+  // about lone_tiles at most
+  int64_t lone_rows = 0, lone_run = 0, lone_tiles = 0;
   int64_t items = 0, parts = 0;            // per head
 };
 
@@ -201,8 +204,11 @@ int64_t key_tiles(int64_t nq, int64_t nk, int group, const AttnPlan& p) {
 struct Splits {
   int64_t n, tiles;
 };
-Splits splits_of(int64_t tiles, const AttnPlan& p) {
-  const int64_t n = tiles <= p.whole_tiles ? 1 : (tiles + p.split_tiles - 1) / p.split_tiles;
+Splits splits_of(int64_t tiles, int64_t rows, const AttnPlan& p) {
+  int64_t most = p.split_tiles;
+  if (rows < p.lone_rows && tiles > p.lone_run)
+    most = std::min(most, std::max(p.lone_tiles, (rows * tiles + 2 * p.lone_rows - 1) / (2 * p.lone_rows)));
+  const int64_t n = tiles <= p.whole_tiles ? 1 : (tiles + most - 1) / most;
   const int64_t each = ((tiles + n - 1) / n + 3) / 4 * 4;
   return Splits{std::max<int64_t>(1, (tiles + each - 1) / each), each};
 }
@@ -233,6 +239,15 @@ constexpr int64_t kItems = 512;
 // split has 1024 keys (a prompt of 512 tokens: 18 us unsplit, 34 in splits of 512 keys), and there is one
 // only where tiles of rows would leave CUs without work.
 constexpr int64_t kLeast = 8, kLeastCached = 16, kWholeCached = 32, kLeastBig = 16, kCus = 256;
+// What each workgroup has to do in the mean goes by the whole batch.  A sequence of few rows over far more keys than
+// the others (one token over a long cache beside a prompt) would be one run about that long, and end the call alone.
+// So a sequence with more than kLone times the mean run and too few row tiles to fill the machine is split whatever the
+// others are: into runs of at most kLoneTiles (in the kernel for many rows kLoneBig) tiles, longer only where its own
+// work fills the machine with them.  Without / with, us, 8 heads of 4, d 128: one token over 128k keys and a prompt of
+// 8k tokens (alone 120 and 600) 2770 to 3200 by their order / 780, fp32 7900 to 8400 / 5900; 512 tokens over 32k and 64
+// single ones over 4k each 1055 / 540; 8 tokens over 128k keys and 56 over 20k 1660 / 1530 (with kLoneTiles 256 1590,
+// and fp32 a loss: 3155 / 3040, with 256 3270).
+constexpr int64_t kLone = 2, kLoneTiles = 512, kLoneBig = 64;
 // The kernel for many rows is taken for more rows than one tile of the other has, if it need not split the
 // keys or there is enough work (in 16 rows x 32 keys).  Few rows / many, us, 8 heads, d 128: 64 rows over 4k keys 25 /
 // 42, 256 38 / 56, 512 60 / 58, 2048 155 / 67; 64 over 32k 57 / 40, 2048 1145 / 298; 16 sequences of 32 rows over
@@ -274,6 +289,9 @@ int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* c
   }
   int64_t each = std::max(cached ? kLeastCached : kLeast, (few.tiles + kItems - 1) / kItems);
   p.whole_tiles = cached ? kWholeCached : kLeast;
+  p.lone_rows = kItems;
+  p.lone_run = kLone * few.tiles / std::max<int64_t>(few.rows, 1);
+  p.lone_tiles = kLoneTiles;
   if (keys == KeysAre::kRowsOfMany) {
     AttnPlan big = p;
     big.rows = kAttnBigRows;
@@ -283,6 +301,9 @@ int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* c
       p = big;
       p.whole_tiles = kLeastBig;
       each = w.rows >= kCus ? kAttnMaxKeys : std::max(kLeastBig, (w.tiles + kItems - 1) / kItems);
+      p.lone_rows = kCus;
+      p.lone_run = kLone * w.tiles / std::max<int64_t>(w.rows, 1);
+      p.lone_tiles = kLoneBig;
     }
   }
   const int64_t share = few.longest <= kWideTiles ? kWideShare : 1;
@@ -290,14 +311,15 @@ int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* c
       cu_q[n_seqs] * group > kAttnRows * live_of(n_seqs, cu_q)) {
     p.rows = kAttnWideRows;
     each = kAttnMaxKeys;
-    p.whole_tiles = kAttnMaxKeys;
+    p.whole_tiles = kAttnMaxKeys;  // (nor for one sequence among others)
   }
   p.split_tiles = (std::min<int64_t>(each, kAttnMaxKeys / 64) + 3) / 4 * 4;
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t nq = cu_q[s + 1] - cu_q[s];
-    const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p).n;
-    p.items += row_tiles(nq, group, p) * splits;
-    if (splits > 1) p.parts += row_tiles(nq, group, p) * splits;
+    const int64_t rows = row_tiles(nq, group, p);
+    const int64_t splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), n_heads * rows, p).n;
+    p.items += rows * splits;
+    if (splits > 1) p.parts += rows * splits;
   }
   return grid_ok(p.items * (p.rows == kAttnBigRows || p.rows == kAttnWideRows ? n_heads : 1), 256) ? TWINKV_OK : TWINKV_E_ARG;
 }
@@ -374,7 +396,7 @@ int attn_args(KeysAre keys, const void* q, int dtype, int d, int n_heads, int gr
     if (s < n_seqs) {
       const int64_t nq = cu_q[s + 1] - cu_q[s];
       tiles = row_tiles(nq, group, p);
-      splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), p);
+      splits = splits_of(key_tiles(nq, cu_k[s + 1] - cu_k[s], group, p), n_heads * tiles, p);
     }
     w.put((int32_t)cu_q[s]);
     w.put((int32_t)cu_k[s]);

@@ -137,11 +137,37 @@ void many_rows_split() {
     split(d, 4, 4, {200}, {6000}, 4000, 4);
   }
 }
+
+// One token over a long cache beside others: its run of key tiles does not grow with what the others have to do, and
+// theirs are as without it.
+void lone_sequences() {
+  const int64_t all = (int64_t)1 << 40;
+  for (const int d : {64, 128})
+    for (const int64_t prompt : {2048, 8192, 32768}) {
+      attend(0, d, 8, 4, {1, prompt}, {131072, prompt}, all, 0);
+      CHECK(g_rows == twinkv::kAttnBigRows && g_splits[0] >= 32 && g_splits[1] == 1);
+      attend(0, d, 8, 4, {prompt, 1}, {prompt, 131072}, all, 0);
+      CHECK(g_rows == twinkv::kAttnBigRows && g_splits[0] == 1 && g_splits[1] >= 32);
+    }
+  attend(1, 128, 8, 4, {1, 8192}, {131072, 8192}, all, 0);
+  CHECK(g_rows == twinkv::kAttnRows && g_splits[0] >= 8 && g_splits[1] == 1);
+  // a chunk of few row tiles among single tokens
+  Lens nq(65, 1), nk(65, 4096);
+  nq[64] = 512, nk[64] = 32768;
+  attend(0, 128, 8, 4, nq, nk, all, 0);
+  CHECK(g_rows == twinkv::kAttnBigRows && g_splits[64] >= 4 && g_splits[0] == 1 && g_splits[63] == 1);
+  // batches alike, or nearly, are as before
+  attend(0, 128, 8, 4, Lens(16, 200), Lens(16, 8192), all, 0);
+  CHECK(*std::max_element(g_splits.begin(), g_splits.end()) == 1);
+  attend(0, 128, 8, 4, {8192}, {8192}, all, 0);
+  CHECK(g_splits[0] == 1);
+}
 }  // namespace
 
 int main() {
   outputs();
   many_rows_split();
+  lone_sequences();
   std::printf("cache plans ok\n");
   return 0;
 }

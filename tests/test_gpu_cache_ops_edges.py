@@ -6,7 +6,7 @@ import pytest
 
 import cache_ops_ref as ref
 from paper_2608_27128_amd import binding
-from test_gpu_cache_ops import check_rope, cum, gen, randn
+from test_gpu_cache_ops import check_rope, cum, fill_cache, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +100,51 @@ def test_sink_attention_many_rows_split_unseen_values_do_not_matter(bad):
         hit[:, seen[:, j], 77] = True
         assert torch.equal(got[~hit], clean[~hit]), j
         assert not bool(torch.isfinite(got[hit]).any()), j
+
+
+# One token over many keys beside a prompt, whose work alone would leave its keys in one run; both orders.
+LONE = [((1, 2048), (30000, 2048)), ((2048, 1), (2048, 30000)), ((3, 700, 0, 1500), (40000, 900, 5, 1500))]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", range(len(LONE)))
+def test_sink_attention_lone_sequence(case, dtype):
+    import torch
+    nq, lens = LONE[case]
+    g = gen(1200 + case)
+    H, G, d = 8, 4, 64
+    cu_q, cu_k = cum(nq), cum(lens)
+    q = randn(g, H * G, sum(nq), d, dtype=dtype)
+    k, v = randn(g, H, sum(lens), d, dtype=dtype), randn(g, H, sum(lens), d, dtype=dtype)
+    got = binding.sink_attention(q, k, v, 1 << 40, 0, None, cu_q, cu_k, want_lse=True)
+    check_some_rows(got, q, k, v, cu_q, cu_k, d, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_cache4_attention_lone_sequence(dtype):
+    import torch
+    g = gen(1250)
+    H, G, d, nq, rows = 4, 4, 64, (1, 6000), (40000, 6016)
+    cache, kv = fill_cache(g, H, rows, d, dtype)
+    cu_q, length = cum(nq), torch.tensor([rows] * H, dtype=torch.int32, device="cuda")
+    q = randn(g, H * G, sum(nq), d, dtype=dtype)
+    got = binding.cache4_attention(q, cache, length, None, cu_q, want_lse=True)
+    check_some_rows(got, q, kv["keys"], kv["values"], cu_q, cache.cu_rows, d, dtype)
+
+
+def check_some_rows(got, q, k, v, cu_q, cu_k, d, dtype):
+    """Plain causal attention: the first and last rows of every sequence and a spread between, of three heads."""
+    import torch
+    G = q.shape[0] // k.shape[0]
+    for s in range(len(cu_q) - 1):
+        a, m, x, n = int(cu_q[s]), int(cu_q[s + 1] - cu_q[s]), int(cu_k[s]), int(cu_k[s + 1] - cu_k[s])
+        if m == 0:
+            continue
+        rows = torch.tensor(sorted({0, m - 1, *(int(i) for i in np.linspace(0, m - 1, 9))}), device="cuda")
+        seen = torch.arange(n, device="cuda")[None, :] <= (n - m + rows)[:, None]
+        for h in (0, G + 1, q.shape[0] - 1):
+            o, e, mass, size = ref.softmax_rows(q[h, a + rows].double(), k[h // G, x:x + n].double(),
+                                                v[h // G, x:x + n].double(), seen, d ** -0.5)
+            tol, tol_e = ref.attention_bounds(o, e, mass, size, n, d, dtype == "bf16")
+            assert bool(((got["out"][h, a + rows].double() - o).abs() <= tol).all()), (s, h)
+            assert bool(((got["lse"][h, a + rows].double() - e).abs() <= tol_e).all()), (s, h)
