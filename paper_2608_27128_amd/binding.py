@@ -711,8 +711,9 @@ def _out_rows(out, shape, like, name: str):
 def _no_gradient(fn: str, *tensors) -> None:
     """These calls return tensors that torch's autograd does not know of: where it would record one, the
     gradient would be lost without a word."""
-    if _torch().is_grad_enabled() and any(x is not None and x.requires_grad for x in tensors):
-        raise ValueError(f"{fn} has no gradient: call it under torch.no_grad(), or on detached tensors")
+    for x in tensors:
+        if x is not None and x.requires_grad and _torch().is_grad_enabled():
+            raise ValueError(f"{fn} has no gradient: call it under torch.no_grad(), or on detached tensors")
 
 
 def _small(x, shape, dtype, dev, name: str):
