@@ -270,14 +270,16 @@ int64_t live_of(int n_seqs, const int64_t* cu_q) {  // sequences with queries
 constexpr int64_t kPairWork = 49152;
 
 // fp32: the kernel for many rows takes four row tiles a workgroup and does not split their keys, so it is taken where
-// the most key tiles that a row tile has are no more than each of kItems such workgroups has in the mean, or up to
-// kWideShare times that where they are few.  Split / wide, us, 8 heads, that ratio in brackets: d 128, 4 rows a token,
-// causal, 256 tokens (4) 22 / 27, 512 (2) 60 / 49, 1024 (1) 151 / 124, 2048 (0.5) 443 / 326; window 128, 256 tokens (4)
-// 20 / 21, 512 (2) 39 / 23, 2048 (0.5) 144 / 69; a row a token, causal, 2048 tokens (2) 155 / 172, 4096 (1) 472 / 445, and
-// of d 64 73 / 101 and 233 / 243.
-constexpr int64_t kWideShare = 3, kWideTiles = 20;
+// the most key tiles that a row tile has are no more than each of kItems such workgroups has in the mean, up to three
+// times that where they are few, and at most half of it where they are many and d is 64 (whose tiles are half the work
+// for the same waits).  Split / wide, us, 8 heads, that ratio in brackets: d 128, 4 rows a token, causal, 256 tokens (4)
+// 22 / 27, 512 (2) 72 / 62, 1024 (1) 164 / 132, 2048 (0.5) 456 / 333; window 128, 256 tokens (4) 20 / 21, 512 (2) 39 / 23,
+// 2048 (0.5) 144 / 69; a row a token, causal, 2048 tokens (2) 168 / 183, 4096 (1) 495 / 457.  d 64, a row a token, causal,
+// 2048 tokens (2) 86 / 113, 4096 (1) 256 / 258 (2 heads of 4 rows a token 227 / 249), 5000 (0.82) 327 / 338, 8192 (0.5)
+// 769 / 709; two rows a token, 2048 tokens (1) 136 / 136, 3000 (0.68) 240 / 224.
+constexpr int64_t kWideTiles = 20, kLongTiles64 = 96;
 
-int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
+int attn_plan(KeysAre keys, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
               int64_t n_sink, AttnPlan& p) {
   p.window = std::min<int64_t>(window, kAttnMaxKeys);
   p.n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
@@ -306,8 +308,8 @@ int attn_plan(KeysAre keys, int n_heads, int group, int n_seqs, const int64_t* c
       p.lone_tiles = kLoneBig;
     }
   }
-  const int64_t share = few.longest <= kWideTiles ? kWideShare : 1;
-  if (keys == KeysAre::kRowsFp32 && few.longest * (kAttnWideRows / kAttnRows) * kItems <= share * few.tiles &&
+  const int64_t halves = few.longest <= kWideTiles ? 6 : d == 64 && few.longest > kLongTiles64 ? 1 : 2;
+  if (keys == KeysAre::kRowsFp32 && 2 * few.longest * (kAttnWideRows / kAttnRows) * kItems <= halves * few.tiles &&
       cu_q[n_seqs] * group > kAttnRows * live_of(n_seqs, cu_q)) {
     p.rows = kAttnWideRows;
     each = kAttnMaxKeys;
@@ -357,7 +359,7 @@ int attn_args(KeysAre keys, const void* q, int dtype, int d, int n_heads, int gr
               float scale, void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse,
               void* workspace, int64_t workspace_bytes, void* stream, AttnArgs& a) {
   AttnPlan p;
-  const int rc = attn_plan(keys, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+  const int rc = attn_plan(keys, d, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
   if (rc != TWINKV_OK) return rc;
   const AttnLayout L = attn_layout(p, d, n_heads, n_seqs);
   if (L.total > 0 && (workspace == nullptr || workspace_bytes < (int64_t)L.total)) return TWINKV_E_WORKSPACE;
@@ -477,7 +479,7 @@ int64_t twinkv_attention_workspace_bytes(int dtype, int d, int n_heads, int grou
   for (const KeysAre keys : {KeysAre::kRows, dtype == TWINKV_BF16 ? KeysAre::kCached : KeysAre::kCachedFp32,
                              dtype == TWINKV_BF16 ? KeysAre::kRowsOfMany : KeysAre::kRowsFp32}) {
     AttnPlan p;
-    rc = attn_plan(keys, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+    rc = attn_plan(keys, d, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
     if (rc != TWINKV_OK) return -rc;
     most = std::max(most, (int64_t)attn_layout(p, d, n_heads, n_seqs).total);
   }

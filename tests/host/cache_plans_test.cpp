@@ -162,12 +162,28 @@ void lone_sequences() {
   attend(0, 128, 8, 4, {8192}, {8192}, all, 0);
   CHECK(g_splits[0] == 1);
 }
+
+// fp32: where the kernel of four row tiles a workgroup is no faster than split keys it is not taken.
+void wide_fp32() {
+  auto rows = [&](int d, int H, int G, int64_t n, int64_t window) {
+    attend(1, d, H, G, {n}, {n}, window, 0);
+    return g_rows;
+  };
+  const int64_t all = (int64_t)1 << 40;
+  CHECK(rows(64, 8, 1, 4096, all) == twinkv::kAttnRows && rows(64, 2, 4, 4096, all) == twinkv::kAttnRows);
+  CHECK(rows(64, 8, 1, 5000, all) == twinkv::kAttnRows);
+  CHECK(rows(64, 8, 1, 8192, all) == twinkv::kAttnWideRows && rows(64, 8, 2, 3000, all) == twinkv::kAttnWideRows);
+  CHECK(rows(64, 8, 1, 4096, 1024) == twinkv::kAttnWideRows && rows(64, 8, 4, 2048, all) == twinkv::kAttnWideRows);
+  CHECK(rows(128, 8, 1, 4096, all) == twinkv::kAttnWideRows && rows(128, 8, 1, 2048, all) == twinkv::kAttnRows);
+  CHECK(rows(128, 8, 4, 512, all) == twinkv::kAttnWideRows && rows(64, 8, 1, 1500, 128) == twinkv::kAttnWideRows);
+}
 }  // namespace
 
 int main() {
   outputs();
   many_rows_split();
   lone_sequences();
+  wide_fp32();
   std::printf("cache plans ok\n");
   return 0;
 }
