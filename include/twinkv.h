@@ -392,7 +392,8 @@ int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype
 
 /*
  * Bytes of workspace twinkv_sink_attention needs for this batch; negative (-TWINKV_E_*) on invalid
- * arguments.  For twinkv_cache4_attention: cu_k = the cache's cu_rows, window = INT64_MAX, n_sink = 0.
+ * arguments.  For twinkv_cache4_attention: cu_k = the cache's cu_rows, window = INT64_MAX, n_sink = 0.  One
+ * figure serves both calls: the larger of what they may need.
  */
 int64_t twinkv_attention_workspace_bytes(int dtype, int d, int n_heads, int group, int n_seqs,
                                          const int64_t* cu_q, const int64_t* cu_k, int64_t window,
@@ -480,7 +481,9 @@ int twinkv_cache4_read(const twinkv_cache4* cache, const int32_t* len, const int
  * sequence s being the last tokens of its cache: query i of m sees rows [0, len - (m - 1 - i)) of each
  * problem (one query: all of them).  out and lse as in twinkv_sink_attention (0 and -inf where nothing
  * is seen); q and out are `dtype`.  len is taken as at most the problem's rows.
- * The products are exact in the cached values; scores and sums are fp32.
+ * The products are exact in the cached values; scores, the running maximum and sums are fp32.  For bf16 the
+ * weights, times the scales of their values, are rounded to bf16 (to nearest) for the product; for fp32 they
+ * keep 24 bits.
  */
 int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* cu_q,
                             int64_t q_head_stride, int64_t q_token_stride, const twinkv_cache4* cache,

@@ -18,10 +18,13 @@
 //    products.
 // A prompt of 32k tokens, 32 heads of 128, window 4096: 2160 us, 956 TFLOP/s of the 1290 that a large bf16 product
 // reaches; 8k tokens of d 64, causal, 322 us, 852 TFLOP/s.  In the profiled run the matrix units are busy 47% of
-// the cycles and the vector units 51% (half of that the exponentials), at a clock of 2.0 GHz; a form of the
-// loop that took 12% more cycles took 5% more time.  Neither 256 rows a workgroup, which halves the memory
+// the cycles and the vector units 39% (a third of that the exponentials), at a clock of 2.0 GHz; d 64 40% and 60%.  A
+// form of the loop that took 12% more cycles took 5% more time.  Neither 256 rows a workgroup, which halves the memory
 // traffic, nor opposite phases for a SIMD's two waves, nor the next tile's scores between this one's
 // exponentials were faster.
+// The weights are rounded to bf16 for the product.  With them as two bf16 parts, and two products, the error against
+// 64 bits is that of the output's own rounding, 0.0016 of the result's norm instead of 0.0022, but the two prompts take
+// 2860 and 444 us.
 // Values that only some rows of a tile see: as in attn.hip.
 #include <hip/hip_runtime.h>
 

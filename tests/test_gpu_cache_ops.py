@@ -509,8 +509,6 @@ def test_streams_and_graph():
 
 # shapes that take each of the attention's ways: keys split or not, fp32 waves on row tiles of their own,
 # many bf16 rows whole and split, chunks of a prompt over long keys
-# (Not among these, nor in the test of split keys below: the kernel for many bf16 rows with its keys split, which
-# test_gpu_cache_ops_edges.py takes; fp32 waves on row tiles of their own are gone.)
 WAYS = [((700,), (0,), 40, 4, 4, 8), ((2500,), (40,), 1 << 20, 0, 4, 8), ((5000,), (64,), 1 << 20, 4, 2, 8),
         ((9000,), (300,), 3000, 4, 4, 2), ((300,) * 16, (33,) * 16, 1 << 20, 0, 1, 8), ((4200,), (513,), 70, 10, 8, 4),
         ((1300, 40, 3000), (1300, 1, 200), 500, 16, 4, 2)]

@@ -54,7 +54,8 @@ def test_without_rotation_a_channel_is_its_own(dtype, d):
 
 # bf16 with rows enough for the kernel of 128 rows and row tiles too few for the machine, so that it splits keys: a
 # chunk over long keys, a window far from sinks that end inside a tile, a batch whose sequences split and do not
-# (tests/host/cache_plans_test.cpp holds the host layer to these plans)
+# (tests/host/cache_plans_test.cpp holds the host layer to these plans; the shapes WAYS of test_gpu_cache_ops.py and its
+# test of split keys leave such keys whole or take the kernel for few rows)
 BIG_SPLIT = [((5000,), (200,), 1 << 20, 4, 4, 4), ((9000,), (150,), 6000, 70, 8, 4), ((7001, 90, 0, 5000), (130, 60, 0, 301), 1 << 40, 0, 4, 4),
              ((6000,), (513,), 2500, 33, 5, 2)]
 
