@@ -117,7 +117,7 @@ def _blocks_of(x):
 
 def _byte(amax):
     """The scale's byte for the largest magnitude of a block (fp32)."""
-    return (((amax.view(torch.int32) + 0x10000) >> 23) - 6).clamp(1, 252)
+    return (((amax.view(torch.int32) + 0x10000) >> 23) - 6).clamp(1, 248)
 
 
 def _power(e):
