@@ -492,6 +492,137 @@ int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* 
                             int64_t workspace_bytes, void* stream);
 
 /*
+ * ---- Eviction by accumulated attention weight, and a cache held in 8 bits ----
+ */
+
+/*
+ * The attention weight that every key has received:
+ *   mass[h][j] = sum over the query heads g of KV head h and the queries i that see key j of
+ *                exp(scale * q_i . k_j - lse_i),
+ * the softmax weights of twinkv_sink_attention with the same arguments, added up by key: a wrapped policy's
+ * per-token scores as twinkv_select_topk takes them.  All queries of a prompt, or only its last ones (an
+ * observation window: q, lse and cu_q of those).
+ *
+ *   q, k, window, n_sink, scale  as in twinkv_sink_attention.
+ *   lse       [n_heads*group][T_q] fp32, as that call returns it.  A query whose lse is -inf has no weights.
+ *   mass      [n_heads][T_k] fp32, added to the result (what earlier chunks gave).  Nullable.
+ *   mass_out  [n_heads][T_k] fp32.  May be `mass`.
+ *   workspace  twinkv_mass_workspace_bytes(...) bytes (may be NULL when that is 0).
+ * Scores and sums are fp32, and the order of the sums does not change from call to call.  A key that a query does
+ * not see never changes another key's sum, NaN and infinities included.
+ */
+int twinkv_attention_mass(const void* q, const void* k, int dtype, int d, int n_heads, int group, int n_seqs,
+                          const int64_t* cu_q, const int64_t* cu_k, int64_t q_head_stride,
+                          int64_t q_token_stride, int64_t k_head_stride, int64_t k_token_stride,
+                          int64_t window, int64_t n_sink, float scale, const float* lse, const float* mass,
+                          float* mass_out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace twinkv_attention_mass needs; negative (-TWINKV_E_*) on invalid arguments. */
+int64_t twinkv_mass_workspace_bytes(int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q,
+                                    const int64_t* cu_k, int64_t window, int64_t n_sink);
+
+/*
+ * A cache held in 8 bits.  32 rows of a head (a block: rows 32b .. 32b + 31 of a problem) share a scale
+ * 2^(byte - 127) for their keys and one for their values; an element is a whole number of -127 .. 127 times it:
+ * 1 + 1/(32 d) byte an element.  With a the largest magnitude of a block, the byte is the smallest in [1, 248]
+ * with a / scale < 127.5; each element goes to the nearest number, ties to the even one.  (A scale that is a power
+ * of two keeps every value exact in bf16, and a row that moves between blocks of one scale as it is.)  A row (of
+ * keys or of values) with an element that is NaN or infinite is stored as zeros and has no part in the scale, and
+ * the problem reports TWINKV_PROBLEM_NONFINITE.
+ *
+ * Sequence s has rows [cu_rows[s], cu_rows[s+1]) of every head, a multiple of 32; how many of them are in use is a
+ * count per problem (h, s), kept by the caller on the device.  C = cu_rows[n_seqs]; the four arrays are
+ * 16-byte aligned:
+ *   k_codes   [n_heads][C][d] int8
+ *   k_scales  [n_heads][C/32] bytes
+ *   v_codes   [n_heads][C/8][d][8] int8: 8 rows of a channel side by side
+ *   v_scales  [n_heads][C/32] bytes
+ * Unused rows may hold anything.
+ */
+typedef struct twinkv_cache8 {
+  int d;                   /* 64 or 128 */
+  int n_heads, n_seqs;
+  const int64_t* cu_rows;  /* (host) [n_seqs + 1], consumed before the call returns */
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+} twinkv_cache8;
+
+/* Bytes of workspace the calls below, but for the attention, need for n_seqs sequences (0 for small batches). */
+int64_t twinkv_cache8_workspace_bytes(int n_seqs);
+
+/*
+ * twinkv_cache4_compact into an 8-bit cache: the keys and values at the retained positions of every problem, in
+ * position order, as the first rows of its part of the cache.  Arguments as there, and
+ *   token_mass  [n_heads][T] fp32: the tokens' accumulated weights.  Nullable.
+ *   mass_out    [n_heads][C] fp32: those of the cached rows, 0 on rows not in use (0 everywhere without
+ *               token_mass).  Nullable; required with token_mass.
+ */
+int twinkv_cache8_compact(const void* keys, const void* values, int dtype, const int64_t* cu_seqlens,
+                          int64_t head_stride, int64_t token_stride, int64_t v_head_stride,
+                          int64_t v_token_stride, const uint8_t* retained, const twinkv_cache8* cache,
+                          const float* token_mass, int32_t* pos_out, float* mass_out, int32_t* len_out,
+                          int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * twinkv_cache4_append to an 8-bit cache; arguments and states as there.  Where a new row needs a larger scale
+ * than its block has, the block's rows in use are rounded once more, to the new one; a block's scale never shrinks.
+ */
+int twinkv_cache8_append(const void* keys, const void* values, int dtype, const int64_t* cu_new,
+                         int64_t head_stride, int64_t token_stride, int64_t v_head_stride,
+                         int64_t v_token_stride, const twinkv_cache8* cache, const int32_t* len_in,
+                         int32_t* len_out, int32_t* status, void* workspace, int64_t workspace_bytes,
+                         void* stream);
+
+/* The values that rows of an 8-bit cache stand for, exact in both types; arguments as in twinkv_cache4_read. */
+int twinkv_cache8_read(const twinkv_cache8* cache, const int32_t* len, const int32_t* first, int dtype,
+                       const int64_t* cu_out, void* keys_out, void* values_out, void* workspace,
+                       int64_t workspace_bytes, void* stream);
+
+/*
+ * Attention over an 8-bit cache; q, len, scale, out and lse as in twinkv_cache4_attention, and
+ *   mass      [n_heads][C] fp32: accumulated weights of the rows in use.  Nullable (0).
+ *   mass_out  [n_heads][C] fp32: with the weights of this call's queries added (sum over the queries that see the
+ *             row and the head's query heads); 0 on rows not in use, so that rows appended later begin with 0.
+ *             May be `mass`.  Nullable; required with mass.
+ *   workspace  twinkv_cache8_attention_workspace_bytes(...) bytes (may be NULL when that is 0).
+ * The products are exact in the cached values; scores, the running maximum and sums are fp32.  For bf16 the
+ * weights, times the scale of their values, are rounded to bf16 (to nearest) for the product; for fp32 they keep
+ * 24 bits.  mass adds weights that are not rounded.
+ */
+int twinkv_cache8_attention(const void* q, int dtype, int group, const int64_t* cu_q, int64_t q_head_stride,
+                            int64_t q_token_stride, const twinkv_cache8* cache, const int32_t* len, float scale,
+                            void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse,
+                            const float* mass, float* mass_out, void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+/* Bytes of workspace twinkv_cache8_attention needs; negative (-TWINKV_E_*) on invalid arguments. */
+int64_t twinkv_cache8_attention_workspace_bytes(int dtype, int d, int n_heads, int group, int n_seqs,
+                                                const int64_t* cu_q, const int64_t* cu_rows, int want_mass);
+
+/*
+ * Eviction by accumulated weight: of every problem's rows in use the min(len, budget) first in the order of
+ * twinkv_select_topk (the n_sink first and n_recent last rows, by row; then more weight, equal weights by row, NaN
+ * after every number), moved in row order to the front of the problem's part of another cache.
+ *
+ *   from, to  same d, n_heads and n_seqs; no array in common.  Rows that meet in a block of `to` take the smallest
+ *             scale that holds them all; their codes are rounded again only where that is larger than their own.
+ *   len       [n_heads * n_seqs] int32 rows of `from` in use (taken as at least 0 and at most the problem's rows).
+ *   mass      [n_heads][C of from] fp32, 16-byte aligned.
+ *   pos       [n_heads][C of from] int32, any number kept beside a row (its token's position).  Nullable.
+ *   budget    (host) [n_seqs] int64, 0 <= budget[s] <= rows of sequence s in `to`.
+ *   len_out   [n_heads * n_seqs] int32 rows of `to` in use.  May be `len`.
+ *   mass_out  [n_heads][C of to] fp32: their weights, 0 on rows not in use.  Nullable.
+ *   pos_out   [n_heads][C of to] int32: their pos, or without pos their rows in `from`; -1 on rows not in use.
+ * Outputs may not overlap the inputs but for len_out.
+ */
+int twinkv_cache8_evict(const twinkv_cache8* from, const int32_t* len, const float* mass, const int32_t* pos,
+                        const int64_t* budget, int n_sink, int n_recent, const twinkv_cache8* to,
+                        int32_t* len_out, float* mass_out, int32_t* pos_out, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/*
  * Profiling hook.  For calls made afterwards from the calling thread, record the given
  * hipEvent_t handles on the call's stream immediately before and immediately after the
  * launch of the call's main kernel -- the similarity kernel (the fused contraction +

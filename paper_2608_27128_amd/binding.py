@@ -71,6 +71,19 @@ SIGNATURES = {
     "twinkv_cache4_read": (_I, [_VP, _VP, _VP, _I, _PI64, _VP, _VP, _VP, _I64, _VP]),
     "twinkv_cache4_attention": (_I, [_VP, _I, _I, _PI64, _I64, _I64, _VP, _VP, _F, _VP, _I64, _I64, _VP,
                                      _VP, _I64, _VP]),
+    "twinkv_mass_workspace_bytes": (_I64, [_I, _I, _I, _I, _I, _PI64, _PI64, _I64, _I64]),
+    "twinkv_attention_mass": (_I, [_VP, _VP, _I, _I, _I, _I, _I, _PI64, _PI64, _I64, _I64, _I64, _I64, _I64,
+                                   _I64, _F, _VP, _VP, _VP, _VP, _I64, _VP]),
+    "twinkv_cache8_workspace_bytes": (_I64, [_I]),
+    "twinkv_cache8_compact": (_I, [_VP, _VP, _I, _PI64, _I64, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP, _VP,
+                                   _VP, _VP, _I64, _VP]),
+    "twinkv_cache8_append": (_I, [_VP, _VP, _I, _PI64, _I64, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP, _I64,
+                                  _VP]),
+    "twinkv_cache8_read": (_I, [_VP, _VP, _VP, _I, _PI64, _VP, _VP, _VP, _I64, _VP]),
+    "twinkv_cache8_attention": (_I, [_VP, _I, _I, _PI64, _I64, _I64, _VP, _VP, _F, _VP, _I64, _I64, _VP, _VP,
+                                     _VP, _VP, _I64, _VP]),
+    "twinkv_cache8_attention_workspace_bytes": (_I64, [_I, _I, _I, _I, _I, _PI64, _PI64, _I]),
+    "twinkv_cache8_evict": (_I, [_VP, _VP, _VP, _VP, _PI64, _I, _I, _VP, _VP, _VP, _VP, _VP, _I64, _VP]),
     "twinkv_status_string": (ctypes.c_char_p, [_I]),
     "twinkv_version": (_I, []),
     "twinkv_profile_sim_events": (None, [_VP, _VP]),
@@ -849,6 +862,9 @@ class _Cache4Struct(ctypes.Structure):
                 ("k_scales", _VP), ("v_codes", _VP), ("v_scales", _VP)]
 
 
+_Cache8Struct = _Cache4Struct  # twinkv_cache8 has the same fields
+
+
 class Cache4:
     """A cache held in 4 bits (layout in include/twinkv.h): sequence s has the rows
     [cu_rows[s], cu_rows[s + 1]) of every head, a multiple of 32.  Takes the four arrays as they are;
@@ -896,7 +912,7 @@ class Cache4:
         return arr
 
 
-def _cache4_rows(keys, values, cache: Cache4):
+def _cache_rows(keys, values, cache):
     keys, dt = _rows(keys, "keys", None, cache.d, cache.device)
     values, _ = _rows(values, "values", keys.dtype, cache.d, cache.device)
     if keys.shape[0] != cache.n_heads or values.shape != keys.shape:
@@ -915,7 +931,7 @@ def cache4_compact(keys, values, retained, cache: Cache4, cu_seqlens=None, *, wo
     (n_heads, C) int32 (-1 on rows not in use) and status (n_heads, n_seqs) int32; a problem that keeps more
     than its rows stores nothing (PROBLEM_BUDGET_MISMATCH, len 0)."""
     torch = _torch()
-    keys, values, dt = _cache4_rows(keys, values, cache)
+    keys, values, dt = _cache_rows(keys, values, cache)
     H, T, _ = keys.shape
     dev = cache.device
     cu = cache._offsets(cu_seqlens, T, "cu_seqlens")
@@ -937,7 +953,7 @@ def cache4_append(keys, values, cache: Cache4, length, cu_new=None, *, len_out=N
     rows after the ``length`` (n_heads, n_seqs) int32 ones in use.  Returns len (``len_out`` if given, which
     may be ``length`` itself) and status; a problem whose new tokens do not fit stays as it is."""
     torch = _torch()
-    keys, values, dt = _cache4_rows(keys, values, cache)
+    keys, values, dt = _cache_rows(keys, values, cache)
     dev = cache.device
     cu = cache._offsets(cu_new, keys.shape[1], "cu_new")
     n_in = cache._lens(length, "length")
@@ -1001,3 +1017,232 @@ def cache4_attention(q, cache: Cache4, length, scale: Optional[float] = None, cu
             n.data_ptr(), float(d ** -0.5 if scale is None else scale), o.data_ptr(), o.stride(0), o.stride(1),
             _ptr(res.get("lse")), wp, wn, _stream(dev))
     return res
+
+
+# ---------------------------------------------------------------- accumulated weights, and the 8-bit cache
+
+def attention_mass(q, k, lse, window: int, n_sink: int = 4, scale: Optional[float] = None, cu_q=None, cu_k=None, *,
+                   mass=None, out=None, workspace=None) -> dict:
+    """The attention weight that every key has received: for each KV head the sum over its query heads and over the
+    queries that see the key of exp(scale q . k - lse), the softmax weights of ``sink_attention`` with the same
+    arguments and its ``lse`` (Hq, Tq) float32.  q (Hq, Tq, d) may be a prompt's last tokens only (cu_q), then lse
+    is theirs.  Returns mass (H, Tk) float32, the scores that ``select_topk`` takes; ``mass`` (H, Tk) is added to it
+    (``out`` may be that tensor).  There is no gradient: inputs that require one are refused (torch.no_grad() lifts
+    that)."""
+    torch = _torch()
+    _no_gradient("attention_mass", q, k, lse, mass, out)
+    q, dt = _rows(q, "q")
+    Hq, Tq, d = q.shape
+    dev = q.device
+    k, _ = _rows(k, "k", q.dtype, d, dev)
+    H, Tk, _ = k.shape
+    group = _group(Hq, H)
+    cq, n_seqs = _offsets(cu_q, Tq, "cu_q")
+    ck, n_k = _offsets(cu_k, Tk, "cu_k")
+    if n_k != n_seqs:
+        raise ValueError("cu_q and cu_k must list the same number of sequences")
+    if window < 0 or n_sink < 0:
+        raise ValueError("window and n_sink must not be negative")
+    if lse is None:
+        raise ValueError("lse is required")
+    f32 = torch.float32
+    lse = _small(lse, (Hq, Tq), f32, dev, "lse")
+    mass = _small(mass, (H, Tk), f32, dev, "mass")
+    out = _own_place(out, (H, Tk), f32, dev, "out")
+    window, n_sink = min(int(window), 1 << 62), min(int(n_sink), 1 << 62)
+    nb = lib().twinkv_mass_workspace_bytes(dt, d, H, group, n_seqs, cq, ck, window, n_sink)
+    ws, wp, wn = _scratch(workspace, int(nb), dev, "twinkv_mass_workspace_bytes")
+    _launch(dev, "twinkv_attention_mass", q.data_ptr(), k.data_ptr(), dt, d, H, group, n_seqs, cq, ck, q.stride(0),
+            q.stride(1), k.stride(0), k.stride(1), window, n_sink, float(d ** -0.5 if scale is None else scale),
+            lse.data_ptr(), _ptr(mass), out.data_ptr(), wp, wn, _stream(dev))
+    return {"mass": out}
+
+
+def _own_place(out, shape, dtype, dev, name: str):
+    """The caller's output of an exact shape and type (written in place), or a new one."""
+    if out is None:
+        return _torch().empty(shape, dtype=dtype, device=dev)
+    if _small(out, shape, dtype, dev, name).data_ptr() != out.data_ptr():
+        raise ValueError(f"{name} must be contiguous and 16-byte aligned")
+    return out
+
+
+class Cache8:
+    """A cache held in 8 bits, a scale for 32 rows of a head (layout in include/twinkv.h): sequence s has the rows
+    [cu_rows[s], cu_rows[s + 1]) of every head, a multiple of 32.  Takes the four arrays as they are;
+    ``Cache8.empty`` reserves them.  How many rows a problem uses is a separate int32 tensor (n_heads, n_seqs),
+    which cache8_compact, cache8_append and cache8_evict return."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, cu_rows):
+        torch = _torch()
+        cu = np.array(cu_rows, dtype=np.int64)
+        if cu.ndim != 1 or cu.size < 2 or cu[0] != 0 or (cu[1:] < cu[:-1]).any() or (cu & 31).any():
+            raise ValueError("cu_rows must start at 0, never decrease, and be multiples of 32")
+        if k_codes.dim() != 3:
+            raise ValueError("k_codes must be (n_heads, C, d)")
+        H, C, d = k_codes.shape[0], int(cu[-1]), k_codes.shape[2]
+        dev = k_codes.device
+        i8, u8 = torch.int8, torch.uint8
+        for name, x, shape, dt in (("k_codes", k_codes, (H, C, d), i8), ("k_scales", k_scales, (H, C // 32), u8),
+                                   ("v_codes", v_codes, (H, C // 8, d, 8), i8), ("v_scales", v_scales, (H, C // 32), u8)):
+            if x.shape != shape or x.dtype != dt or x.device != dev or not x.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dt} {shape} tensor on {dev}, got {tuple(x.shape)} {x.dtype}")
+        if not k_codes.is_cuda:
+            raise ValueError("the cache must be on a GPU")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.cu_rows, self.n_heads, self.n_seqs, self.d, self.device = cu, H, cu.size - 1, d, dev
+        self._cu = (ctypes.c_int64 * cu.size).from_buffer(cu)
+        self._struct = _Cache8Struct(d, H, cu.size - 1, ctypes.cast(self._cu, _PI64), k_codes.data_ptr(),
+                                     k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
+        self._handle = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, n_heads: int, capacity, d: int, device="cuda"):
+        """Reserves ``capacity[s]`` rows for sequence s of every head, each rounded up to 32."""
+        torch = _torch()
+        cu = np.concatenate([[0], np.cumsum([(int(c) + 31) // 32 * 32 for c in np.atleast_1d(capacity)])])
+        C = int(cu[-1])
+        return cls(*(torch.empty(shape, dtype=dt, device=device) for shape, dt in (
+            ((n_heads, C, d), torch.int8), ((n_heads, C // 32), torch.uint8),
+            ((n_heads, C // 8, d, 8), torch.int8), ((n_heads, C // 32), torch.uint8))), cu)
+
+    _lens = Cache4._lens
+    _offsets = Cache4._offsets
+
+    def _weights(self, x, name: str):
+        return _small(x, (self.n_heads, int(self.cu_rows[-1])), _torch().float32, self.device, name)
+
+
+def _cache8_scratch(workspace, cache: Cache8):
+    return _scratch(workspace, int(lib().twinkv_cache8_workspace_bytes(cache.n_seqs)), cache.device,
+                    "twinkv_cache8_workspace_bytes")
+
+
+def cache8_compact(keys, values, retained, cache: Cache8, cu_seqlens=None, *, token_mass=None, workspace=None) -> dict:
+    """``compact`` into an 8-bit cache: the keys and values (n_heads, T, d) at the retained positions of every problem
+    become the first rows of its part of ``cache``.  Returns len (n_heads, n_seqs) int32, pos (n_heads, C) int32 (-1
+    on rows not in use) and status (n_heads, n_seqs) int32; a problem that keeps more than its rows stores nothing
+    (PROBLEM_BUDGET_MISMATCH, len 0).  With ``token_mass`` (n_heads, T) float32 also mass (n_heads, C), the cached
+    rows' weights."""
+    torch = _torch()
+    keys, values, dt = _cache_rows(keys, values, cache)
+    H, T, _ = keys.shape
+    dev, C = cache.device, int(cache.cu_rows[-1])
+    cu = cache._offsets(cu_seqlens, T, "cu_seqlens")
+    if retained is None:
+        raise ValueError("retained is required")
+    ret = _mask(retained, H, T, dev, "retained")
+    token_mass = _small(token_mass, (H, T), torch.float32, dev, "token_mass")
+    out = {"len": torch.empty((H, cache.n_seqs), dtype=torch.int32, device=dev),
+           "pos": torch.empty((H, C), dtype=torch.int32, device=dev),
+           "status": torch.empty((H, cache.n_seqs), dtype=torch.int32, device=dev)}
+    if token_mass is not None:
+        out["mass"] = torch.empty((H, C), dtype=torch.float32, device=dev)
+    ws, wp, wn = _cache8_scratch(workspace, cache)
+    _launch(dev, "twinkv_cache8_compact", keys.data_ptr(), values.data_ptr(), dt, cu, keys.stride(0), keys.stride(1),
+            values.stride(0), values.stride(1), ret.data_ptr(), cache._handle, _ptr(token_mass), out["pos"].data_ptr(),
+            _ptr(out.get("mass")), out["len"].data_ptr(), out["status"].data_ptr(), wp, wn, _stream(dev))
+    return out
+
+
+def cache8_append(keys, values, cache: Cache8, length, cu_new=None, *, len_out=None, workspace=None) -> dict:
+    """The keys and values (n_heads, T, d) of new tokens, [cu_new[s], cu_new[s + 1]) of sequence s, as the rows after
+    the ``length`` (n_heads, n_seqs) int32 ones in use.  Returns len (``len_out`` if given, which may be ``length``
+    itself) and status; a problem whose new tokens do not fit stays as it is.  Where a row needs a larger scale
+    than its block of 32 has, the block's rows are rounded once more."""
+    torch = _torch()
+    keys, values, dt = _cache_rows(keys, values, cache)
+    dev = cache.device
+    cu = cache._offsets(cu_new, keys.shape[1], "cu_new")
+    n_in = cache._lens(length, "length")
+    len_out = _own_place(len_out, (cache.n_heads, cache.n_seqs), torch.int32, dev, "len_out")
+    status = torch.empty((cache.n_heads, cache.n_seqs), dtype=torch.int32, device=dev)
+    ws, wp, wn = _cache8_scratch(workspace, cache)
+    _launch(dev, "twinkv_cache8_append", keys.data_ptr(), values.data_ptr(), dt, cu, keys.stride(0), keys.stride(1),
+            values.stride(0), values.stride(1), cache._handle, n_in.data_ptr(), len_out.data_ptr(),
+            status.data_ptr(), wp, wn, _stream(dev))
+    return {"len": len_out, "status": status}
+
+
+def cache8_read(cache: Cache8, length, dtype, first=None, cu_out=None, *, want_keys: bool = True,
+                want_values: bool = True, workspace=None) -> dict:
+    """The values that cached rows stand for, in ``dtype``: keys and values (n_heads, cu_out[-1], d), row r of
+    sequence s being cache row first + r (``first`` (n_heads, n_seqs) int32, default 0; ``cu_out`` defaults to all
+    of the cache's rows).  Rows that are not in use are zeros."""
+    torch = _torch()
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"unsupported dtype {dtype}")
+    dev = cache.device
+    cu_out = cache.cu_rows if cu_out is None else cu_out
+    cu = cache._offsets(cu_out, int(cu_out[-1]), "cu_out")
+    n = cache._lens(length, "length")
+    f = cache._lens(first, "first")
+    shape = (cache.n_heads, int(cu[-1]), cache.d)
+    out = {name: torch.empty(shape, dtype=dtype, device=dev)
+           for name, want in (("keys", want_keys), ("values", want_values)) if want}
+    ws, wp, wn = _cache8_scratch(workspace, cache)
+    _launch(dev, "twinkv_cache8_read", cache._handle, n.data_ptr(), _ptr(f),
+            TWINKV_BF16 if dtype == torch.bfloat16 else TWINKV_F32, cu, _ptr(out.get("keys")), _ptr(out.get("values")),
+            wp, wn, _stream(dev))
+    return out
+
+
+def cache8_attention(q, cache: Cache8, length, scale: Optional[float] = None, cu_q=None, *, want_lse: bool = False,
+                     want_mass: bool = False, mass=None, mass_out=None, out=None, workspace=None) -> dict:
+    """Attention of q (Hq, Tq, d), the last tokens [cu_q[s], cu_q[s + 1]) of each cached sequence, over the
+    ``length`` (n_heads, n_seqs) int32 rows in use, as ``cache4_attention`` computes it.  Returns out, with
+    ``want_lse`` lse (Hq, Tq) float32, and with ``want_mass``, ``mass`` or ``mass_out`` mass (n_heads, C) float32:
+    the rows' weights so far (``mass``; None: 0) and those of this call's queries, 0 on rows not in use.
+    ``mass_out`` may be ``mass``.  There is no gradient: a q that requires one is refused (torch.no_grad() lifts
+    that)."""
+    torch = _torch()
+    _no_gradient("cache8_attention", q, mass, mass_out, out)
+    dev = cache.device
+    q, dt = _rows(q, "q", None, cache.d, dev)
+    Hq, Tq, d = q.shape
+    group = _group(Hq, cache.n_heads)
+    cq = cache._offsets(cu_q, Tq, "cu_q")
+    n = cache._lens(length, "length")
+    want_mass = want_mass or mass is not None or mass_out is not None
+    mass = cache._weights(mass, "mass")
+    res = {"out": _out_rows(out, (Hq, Tq, d), q, "out")}
+    if want_lse:
+        res["lse"] = torch.empty((Hq, Tq), dtype=torch.float32, device=dev)
+    if want_mass:
+        res["mass"] = _own_place(mass_out, (cache.n_heads, int(cache.cu_rows[-1])), torch.float32, dev, "mass_out")
+    o = res["out"]
+    nb = lib().twinkv_cache8_attention_workspace_bytes(dt, d, cache.n_heads, group, cache.n_seqs, cq, cache._cu,
+                                                       1 if want_mass else 0)
+    ws, wp, wn = _scratch(workspace, int(nb), dev, "twinkv_cache8_attention_workspace_bytes")
+    _launch(dev, "twinkv_cache8_attention", q.data_ptr(), dt, group, cq, q.stride(0), q.stride(1), cache._handle,
+            n.data_ptr(), float(d ** -0.5 if scale is None else scale), o.data_ptr(), o.stride(0), o.stride(1),
+            _ptr(res.get("lse")), _ptr(mass), _ptr(res.get("mass")), wp, wn, _stream(dev))
+    return res
+
+
+def cache8_evict(cache: Cache8, length, mass, budget, to: Cache8, n_sink: int = 4, n_recent: int = 64, *, pos=None,
+                 len_out=None, workspace=None) -> dict:
+    """Keeps of every problem's ``length`` (n_heads, n_seqs) int32 rows the ``budget`` (an int, or one per sequence)
+    that ``select_topk`` would: the first ``n_sink`` and last ``n_recent``, then those of most ``mass`` (n_heads, C)
+    float32.  They move, in row order, to the front of another cache ``to``.  Returns len, mass and pos of ``to``:
+    pos is what ``pos`` (n_heads, C) int32 held for the rows, or their rows in ``cache``; -1, and mass 0, on rows
+    not in use.  ``len_out`` may be ``length``."""
+    torch = _torch()
+    dev = cache.device
+    if (to.n_heads, to.n_seqs, to.d, to.device) != (cache.n_heads, cache.n_seqs, cache.d, dev):
+        raise ValueError("the caches must have the same heads, sequences, channels and device")
+    n = cache._lens(length, "length")
+    if mass is None:
+        raise ValueError("mass is required")
+    mass = cache._weights(mass, "mass")
+    pos = _small(pos, (cache.n_heads, int(cache.cu_rows[-1])), torch.int32, dev, "pos")
+    keep = _i64_array(_budget(budget, cache.n_seqs))
+    C = int(to.cu_rows[-1])
+    out = {"len": _own_place(len_out, (cache.n_heads, cache.n_seqs), torch.int32, dev, "len_out"),
+           "mass": torch.empty((cache.n_heads, C), dtype=torch.float32, device=dev),
+           "pos": torch.empty((cache.n_heads, C), dtype=torch.int32, device=dev)}
+    ws, wp, wn = _cache8_scratch(workspace, cache)
+    _launch(dev, "twinkv_cache8_evict", cache._handle, n.data_ptr(), mass.data_ptr(), _ptr(pos), keep, int(n_sink),
+            int(n_recent), to._handle, out["len"].data_ptr(), out["mass"].data_ptr(), out["pos"].data_ptr(), wp, wn,
+            _stream(dev))
+    return out

@@ -3,7 +3,7 @@
     python -m paper_2608_27128_amd.build
 
 Kernels (csrc/kernels/*.hip) are compiled by hipcc for gfx950 with packed-fp32 VALU
-instructions disabled; the host layer (csrc/api.cpp, csrc/cache_ops.cpp) is plain C++ against the HIP
+instructions disabled; the host layer (csrc/*.cpp) is plain C++ against the HIP
 runtime API.  Everything is linked into paper_2608_27128_amd/libtwinkv.so.  A second copy
 built with -DTWINKV_DEBUG (kernels that poison their LDS between uses, with extra barriers)
 goes to paper_2608_27128_amd/libtwinkv_debug.so; only the tests load it.
@@ -66,7 +66,7 @@ def _build_one(lib: str, objdir: str, extra: list, verbose: bool) -> str:
         obj = os.path.join(objdir, os.path.basename(src) + ".o")
         jobs.append([hipcc, *HIP_FLAGS, *extra, "-c", src, "-o", obj])
         objs.append(obj)
-    for src in ("api.cpp", "cache_ops.cpp"):
+    for src in ("api.cpp", "cache_ops.cpp", "cache8_ops.cpp"):
         obj = os.path.join(objdir, src + ".o")
         jobs.append([cxx, *CXX_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)

@@ -1,5 +1,6 @@
-// Internal declarations of the operators around the cache (norm and rotation, windowed attention, the
-// 4-bit cache), shared by their host layer (cache_ops.cpp) and their kernels.  Not part of the ABI.
+// Internal declarations of the operators around the cache (norm and rotation, windowed attention, the caches
+// in 4 and 8 bits, accumulated attention weights), shared by their host layers (cache_ops.cpp, cache8_ops.cpp)
+// and their kernels.  Not part of the ABI.
 #pragma once
 
 #include <cstddef>
@@ -108,5 +109,64 @@ int launch_attn(const AttnArgs& a, int dtype, int d, void* stream);
 int launch_attn_rows(const AttnArgs& a, int d, void* stream);
 int launch_attn4(const AttnArgs& a, int dtype, int d, void* stream);
 int launch_attn_join(const AttnArgs& a, int dtype, int d, void* stream);
+
+// The 8-bit cache: the same four arrays (layouts in include/twinkv.h), 32 rows of which share a scale.
+using Cache8 = Cache4;
+constexpr int kCache8Block = 32;
+struct Cache8Args : Cache4Args {
+  const float* mass;     // nullable [n_heads][T] by token (compact)
+  float* mass_out;       // [n_heads][C]
+};
+int launch_cache8_gather(const Cache8Args& a, int dtype, int d, void* stream);
+int launch_cache8_append(const Cache8Args& a, int max_new, int dtype, int d, void* stream);
+int launch_cache8_read(const Cache8Args& a, int dtype, int d, void* stream);
+int launch_attn8(const AttnArgs& a, int dtype, int d, void* stream);
+
+// Eviction from one cache into another.  Words per sequence: first row of `from`, first row of `to`, rows to
+// keep, first block of `to`.
+constexpr int kEvict8SeqWords = 4;
+struct Evict8Args {
+  SeqWords seq;
+  Cache8 from, to;
+  const int32_t* len;    // [n_heads * n_seqs]
+  const float* mass;     // [n_heads][from.C]
+  const int32_t* pos;    // nullable [n_heads][from.C]
+  int32_t* len_out;
+  float* mass_out;       // nullable [n_heads][to.C]
+  int32_t* pos_out;      // [n_heads][to.C]; between the two kernels: the row of `from`, -1 where none
+  int n_heads, n_seqs;
+  int n_sink, n_recent;
+  int n_blocks;          // of `to`, per head
+  int max_rows;          // of a sequence of `from`
+};
+int launch_evict8_select(const Evict8Args& a, void* stream);
+int launch_evict8_move(const Evict8Args& a, int d, void* stream);
+
+// The weight that each key receives.  Rows are numbered as in the attention; an item is a tile of kMassKeys keys
+// and a range of row tiles, counted from the first that sees a key of the tile.  Words per sequence: first query,
+// first key, first item, items of a key tile (splits), rows of a split, first part (of sequences with more than one
+// split).
+constexpr int kMassSeqWords = 6;
+constexpr int kMassRowTile = 64;  // splits are whole numbers of so many rows
+struct MassArgs {
+  SeqWords seq;
+  const char* q;
+  const char* k;
+  int64_t q_head, q_token, k_head, k_token;  // bytes
+  Cache8 cache;            // k null: keys in 8 bits
+  const int32_t* len;      // [n_heads * n_seqs] rows in use (8 bits)
+  const float* lse;        // [n_heads * group][Tq]
+  const float* mass;       // nullable [n_heads][Tk]: what is there already
+  float* mass_out;         // [n_heads][Tk]
+  int64_t Tq, Tk;
+  float scale_log2;
+  int window, n_sink;      // at most kAttnMaxKeys each
+  int n_heads, group, n_seqs;
+  int items, parts;        // per head
+  float* part;             // [n_heads][parts][keys of a tile]
+};
+constexpr int mass_keys(int dtype) { return dtype == 0 ? 256 : 128; }  // of a tile (TWINKV_BF16, TWINKV_F32)
+int launch_mass(const MassArgs& a, int dtype, int d, void* stream);
+int launch_mass_join(const MassArgs& a, int dtype, void* stream);
 
 }  // namespace twinkv

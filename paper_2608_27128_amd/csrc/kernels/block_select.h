@@ -12,6 +12,15 @@ namespace twinkv {
 constexpr int kSelBins = 2048;
 constexpr int kSelMaxThreads = 1024;
 
+// Ascending key of an unprotected score: decreasing in the score, never 0 (the protected
+// key); -0 counts as +0, and NaN takes the largest key.
+__device__ inline uint32_t score_key(float f) {
+  if (f != f) return 0xFFFFFFFFu;
+  uint32_t u = __float_as_uint(f == 0.0f ? 0.0f : f);
+  u = (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // increasing in f
+  return ~u;
+}
+
 // Exclusive prefix sum of v over the block of NT threads; `total` receives the block sum.
 // s_wave holds NT / 64 ints.
 template <int NT>

@@ -30,15 +30,6 @@ namespace {
 
 constexpr int kEvThreads = 256;  // prevalence
 
-// Ascending key of an unprotected score: decreasing in the score, never 0 (the protected
-// key); -0 counts as +0, and NaN takes the largest key.
-__device__ inline uint32_t score_key(float f) {
-  if (f != f) return 0xFFFFFFFFu;
-  uint32_t u = __float_as_uint(f == 0.0f ? 0.0f : f);
-  u = (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // increasing in f
-  return ~u;
-}
-
 // Sequences of any length: every pass streams the counts (scores) from HBM, 8 slabs of NT
 // tokens per thread and round with the round's loads in flight together.  The first pass
 // writes the Eq. 3 scores and takes the AND and OR of the keys; the selection's digits start
