@@ -16,6 +16,7 @@ struct MassPlan {
   int64_t keys = 0;        // of a tile
   int64_t most_rows = 0;   // of a split
   int64_t items = 0, parts = 0;
+  bool few = false;
 };
 
 // The most rows that see a key of one tile.  `cached`: how many keys there are is known on the device only.
@@ -25,9 +26,12 @@ int64_t rows_seeing(int64_t nq, int64_t nk, int group, int64_t window, int64_t n
   return (n_sink > 0 ? seen : std::min(seen, window + keys - 1)) * group;
 }
 
-// About so many items, and at least so many rows in each: with fewer the keys' way into the registers and the parts
-// cost more than the products.
-constexpr int64_t kMassItems = 1024, kMassLeast = 512;
+// Items of equal work, many to a CU so that the last ones to end leave little of the machine idle, but of 1024 rows at
+// least, whose products cover the way of the item's keys to the registers; of fewer where there would not be two for
+// every CU.
+constexpr int64_t kMassItems = 16384, kMassSlots = 512, kMassLeast = 1024;
+// Up to so many rows (bf16) the keys' way to the registers is what takes the time: fewer registers, more workgroups.
+constexpr int64_t kMassFew = 256;
 
 MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_sink, bool cached, const MassPlan& p) {
   MassSeq m;
@@ -42,17 +46,23 @@ MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_si
 
 int mass_plan(int dtype, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
               int64_t n_sink, bool cached, MassPlan& p) {
-  p.keys = mass_keys(dtype);
+  p.keys = dtype == TWINKV_BF16 ? 2 * kMassKeys : kMassKeys;
   double work = 0;  // rows times tiles
+  int64_t longest = 0;
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t nq = cu_q[s + 1] - cu_q[s], nk = cu_k[s + 1] - cu_k[s];
     if (nk == 0) continue;
-    const double rows = (double)rows_seeing(nq, nk, group, window, n_sink, p.keys, cached);
+    const int64_t tiles = (nk + p.keys - 1) / p.keys, sinks = std::min(tiles, (n_sink + p.keys - 1) / p.keys);
+    const int64_t most = rows_seeing(nq, nk, group, window, 1, p.keys, cached);
+    const int64_t rest = rows_seeing(nq, nk, group, window, 0, p.keys, cached);
     // of a whole prompt the mean key is seen by half of the queries
     const double part = window >= nk && !cached ? 1.0 - 0.5 * std::min(1.0, (double)nq / (double)nk) : 1.0;
-    work += (double)n_heads * (double)((nk + p.keys - 1) / p.keys) * rows * part;
+    longest = std::max(longest, sinks > 0 ? most : rest);
+    work += (double)n_heads * part * ((double)sinks * (double)most + (double)(tiles - sinks) * (double)rest);
   }
-  p.most_rows = std::max<int64_t>(kMassLeast, (int64_t)(work / kMassItems));
+  p.few = longest <= kMassFew;
+  const int64_t even = (int64_t)(work / kMassSlots);
+  p.most_rows = std::max((int64_t)(work / kMassItems), std::min(kMassLeast, std::max<int64_t>(even, kMassRowTile)));
   for (int s = 0; s < n_seqs; ++s) {
     const MassSeq m = mass_seq(cu_q[s + 1] - cu_q[s], cu_k[s + 1] - cu_k[s], group, window, n_sink, cached, p);
     p.items += m.tiles * m.splits;
@@ -106,6 +116,8 @@ int mass_args(int dtype, const void* q, int n_heads, int group, int n_seqs, cons
   a.n_seqs = n_seqs;
   a.items = (int)p.items;
   a.parts = (int)p.parts;
+  a.keys = (int)p.keys;
+  a.few = p.few;
   a.part = reinterpret_cast<float*>(ws + L.part);
   WordWriter w(a.seq, ((int64_t)n_seqs + 1) * kMassSeqWords, ws, stream);
   int64_t item = 0, part = 0;
@@ -128,7 +140,7 @@ int run_mass(const MassArgs& a, int dtype, int d, void* stream) {
   if (a.items == 0) return TWINKV_OK;
   const int e = launch_mass(a, dtype, d, stream);
   if (e != 0 || a.parts == 0) return hip_status(e);
-  return hip_status(launch_mass_join(a, dtype, stream));
+  return hip_status(launch_mass_join(a, stream));
 }
 
 KeysAre cached_keys(int dtype) { return dtype == TWINKV_BF16 ? KeysAre::kCached : KeysAre::kCachedFp32; }

@@ -142,12 +142,13 @@ struct Evict8Args {
 int launch_evict8_select(const Evict8Args& a, void* stream);
 int launch_evict8_move(const Evict8Args& a, int d, void* stream);
 
-// The weight that each key receives.  Rows are numbered as in the attention; an item is a tile of kMassKeys keys
+// The weight that each key receives.  Rows are numbered as in the attention; an item is a tile of keys
 // and a range of row tiles, counted from the first that sees a key of the tile.  Words per sequence: first query,
 // first key, first item, items of a key tile (splits), rows of a split, first part (of sequences with more than one
 // split).
 constexpr int kMassSeqWords = 6;
-constexpr int kMassRowTile = 64;  // splits are whole numbers of so many rows
+constexpr int kMassRowTile = 128;  // splits are whole numbers of so many rows
+constexpr int kMassKeys = 128;     // of a tile; bf16: or twice as many
 struct MassArgs {
   SeqWords seq;
   const char* q;
@@ -163,10 +164,11 @@ struct MassArgs {
   int window, n_sink;      // at most kAttnMaxKeys each
   int n_heads, group, n_seqs;
   int items, parts;        // per head
-  float* part;             // [n_heads][parts][keys of a tile]
+  int keys;                // of a tile
+  bool few;                // rows see a tile (bf16)
+  float* part;             // [n_heads][parts][keys]
 };
-constexpr int mass_keys(int dtype) { return dtype == 0 ? 256 : 128; }  // of a tile (TWINKV_BF16, TWINKV_F32)
 int launch_mass(const MassArgs& a, int dtype, int d, void* stream);
-int launch_mass_join(const MassArgs& a, int dtype, void* stream);
+int launch_mass_join(const MassArgs& a, void* stream);
 
 }  // namespace twinkv

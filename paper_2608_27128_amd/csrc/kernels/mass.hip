@@ -16,6 +16,8 @@
 // adds the parts in their order; nothing is added atomically.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "attn_split.h"
 #include "codes8.h"
 
@@ -24,14 +26,15 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kFlush = 16;  // steps between additions to the total
+constexpr int kAhead = 3;   // steps of the contraction whose rows are on their way from LDS
 
 // A wave's keys, and the rows of a step.
-template <typename T, int D>
+template <typename T, int D, int B>
 struct Keys;
 
-template <int D>
-struct Keys<bf16, D> {
-  static constexpr int kBlocks = 2, kRowBlocks = 2, kSteps = D / 16;  // of 32 keys, of 32 rows, of 16 channels
+template <int D, int B>
+struct Keys<bf16, D, B> {
+  static constexpr int kBlocks = B, kRowBlocks = 4, kSteps = D / 16;  // of 32 keys, of 32 rows, of 16 channels
   bf16x8 k[kBlocks][kSteps];
   __device__ void load(int b, const char* row, int hi) {
 #pragma unroll
@@ -44,21 +47,16 @@ struct Keys<bf16, D> {
       k[b][j] = codes8_bf16(w[0], w[1]);
     }
   }
-  // rows: the lane's row in LDS, its 16-byte pieces at place(piece)
-  template <typename Place>
-  __device__ void products(const char* row, int hi, const Place& place, f32x16 (&acc)[kBlocks]) const {
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const bf16x8 q = *reinterpret_cast<const bf16x8*>(row + place(2 * j + hi));
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[b][j], acc[b], 0, 0, 0);
-    }
+  // The lane's 16 bytes of step j of its row.
+  typedef bf16x8 Row;
+  __device__ void product(int j, int b, const Row& q, f32x16& acc) const {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[b][j], acc, 0, 0, 0);
   }
 };
 
 template <int D>
-struct Keys<float, D> {
-  static constexpr int kBlocks = 1, kRowBlocks = 1, kSteps = D / 8;
+struct Keys<float, D, 1> {
+  static constexpr int kBlocks = 1, kRowBlocks = 2, kSteps = D / 8;
   f32x4 k[kBlocks][kSteps];
   __device__ void load(int b, const char* row, int hi) {
 #pragma unroll
@@ -68,14 +66,10 @@ struct Keys<float, D> {
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) k[b][j] = codes4_f32(*reinterpret_cast<const unsigned*>(row + (2 * j + hi) * 4));
   }
-  template <typename Place>
-  __device__ void products(const char* row, int hi, const Place& place, f32x16 (&acc)[kBlocks]) const {
+  typedef f32x4 Row;
+  __device__ void product(int j, int b, const Row& q, f32x16& acc) const {
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const f32x4 q = *reinterpret_cast<const f32x4*>(row + place(2 * j + hi));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[e], k[0][j][e], acc[0], 0, 0, 0);
-    }
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(q[e], k[b][j][e], acc, 0, 0, 0);
   }
 };
 
@@ -104,16 +98,21 @@ __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
   return p;
 }
 
-template <typename T, int D, bool kCodes>
-__global__ __launch_bounds__(kThreads, 2) void mass_kernel(const MassArgs a) {
-  typedef Keys<T, D> Own;
+// kMode: how a block's products and weights go together (see above).
+enum { kFused, kApart, kFew };
+template <typename T, int D, int B, int kMode, bool kCodes>
+__global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D == 128) ? 2 : kMode == kFew && D == 128 ? 3 : 4) void mass_kernel(const MassArgs a) {
+  typedef Keys<T, D, B> Own;
+  typedef typename Own::Row Row;
   constexpr int kWaveKeys = 32 * Own::kBlocks, kTileKeys = 4 * kWaveKeys, kTileRows = 32 * Own::kRowBlocks;
   constexpr int kRowBytes = D * (int)sizeof(T), kPieces = kRowBytes / 16, kAtOnce = kThreads / kPieces;
-  constexpr int kCopies = kTileRows / kAtOnce;
-  static_assert(kTileKeys == mass_keys(sizeof(T) == 4), "the host's tiles");
-  __shared__ __attribute__((aligned(16))) char s_q[2][kTileRows * kRowBytes];
-  __shared__ __attribute__((aligned(16))) float s_lse[2][kTileRows];  // in log2 units
-  __shared__ __attribute__((aligned(16))) int s_pos[2][kTileRows];    // of the rows' queries; below 0: no row
+  constexpr int kCopies = kTileRows / kAtOnce, kStats = 3;
+  // Two objects, so that the compiler sees that reading one need not wait for the loads into the other.
+  __shared__ __attribute__((aligned(16))) char s_even[kTileRows * kRowBytes];
+  __shared__ __attribute__((aligned(16))) char s_odd[kMode == kFew ? 16 : kTileRows * kRowBytes];
+  // (of three steps: a block's epilogue runs beside the next block's products, which may be the next step's)
+  __shared__ __attribute__((aligned(16))) float s_lse[kStats][kTileRows];  // in log2 units
+  __shared__ __attribute__((aligned(16))) int s_pos[kStats][kTileRows];    // of the rows' queries; below 0: no row
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = (int)(blockIdx.x % (unsigned)a.n_heads);
@@ -151,109 +150,219 @@ __global__ __launch_bounds__(kThreads, 2) void mass_kernel(const MassArgs a) {
     }
   }
 
-  // Row r of a step for this thread's 16 bytes: query and query head move along by whole steps.
+  // Of these rows some see some of the wave's keys, and in between all see all.
+  const int far_key = wave_key + kWaveKeys - 1;
+  auto row_at = [&](int64_t pos) { return __builtin_amdgcn_readfirstlane((int)min(max((int64_t)query_at(pos) * a.group, (int64_t)row0), (int64_t)max(row0, row1))); };
+  const int some0 = row_at(wave_key), some1 = wave_key >= n ? row0 : wave_key < a.n_sink ? max(row0, row1) : row_at((int64_t)far_key + a.window);
+  const int all0 = far_key < n ? row_at(far_key) : max(row0, row1);
+  const int all1 = far_key < a.n_sink ? max(row0, row1) : row_at((int64_t)wave_key + a.window);
+
+  // Rows to LDS.  Where whole runs of rows have the same query heads a thread's rows lie at fixed distances, and
+  // move by a fixed one from step to step; otherwise, and in the last step, each row's place is worked out.
   const char* q_head0 = a.q + (int64_t)h * a.group * a.q_head + (int64_t)p.q0 * a.q_token;
-  constexpr int kTurn = kRowBytes == 128 ? 1 : 0;
-  auto turn = [](int row) { return kTurn ? (row >> 1) & 7 : row & 15; };
-  const int step_q = kTileRows / a.group, step_g = kTileRows % a.group;
-  int query[kCopies], sub[kCopies];
-#pragma unroll
-  for (int c = 0; c < kCopies; ++c) {
-    const int r = row0 + c * kAtOnce + tid / kPieces;
-    query[c] = r / a.group;
-    sub[c] = r - query[c] * a.group;
-  }
-  int my_query = 0, my_sub = 0;  // of the row whose statistics this thread brings (the first wave)
-  if (tid < kTileRows) {
-    my_query = (row0 + tid) / a.group;
-    my_sub = row0 + tid - my_query * a.group;
-  }
-  auto advance = [&](int& qu, int& su) {
-    qu += step_q;
-    su += step_g;
-    if (su >= a.group) {
-      su -= a.group;
-      ++qu;
+  auto turn = [](int row) { return kRowBytes == 128 ? (row >> 1) & 7 : row & 15; };
+  const unsigned inv_group = (unsigned)((0xffffffffull + (unsigned)a.group) / (unsigned)a.group);  // 2^32 / group, up
+  auto query_of = [&](int r, int& sub) {  // r / group, r % group
+    int q = a.group == 1 ? r : (int)__umulhi((unsigned)r, inv_group);
+    sub = r - q * a.group;
+    if (sub < 0) {
+      sub += a.group;
+      --q;
     }
+    return q;
   };
+  const bool even = kAtOnce % a.group == 0 && row0 % a.group == 0;
+  const int64_t copy_bytes = even ? kAtOnce / a.group * a.q_token : 0, step_bytes = copy_bytes * kCopies;
+  const int r_lane = tid / kPieces, piece = tid % kPieces;
+  const char* from;
+  {
+    int sub;
+    const int query = query_of(row0 + r_lane, sub);
+    from = q_head0 + sub * a.q_head + (int64_t)query * a.q_token;
+  }
   float next_lse = 0.0f;
   int next_pos = -1;
-  auto bring = [&](int buf) {
-    char* to = s_q[buf] + wave * 1024;
+  auto bring = [&](auto F, int r0) {
+    char* to = (F == 0 ? s_even : s_odd) + wave * 1024;
+    if (even && r0 + kTileRows <= n_rows) {
 #pragma unroll
-    for (int c = 0; c < kCopies; ++c) {
-      const int r = c * kAtOnce + tid / kPieces;
-      const int piece = (tid % kPieces) ^ turn(r);
-      const int64_t qu = min(query[c], p.nq - 1);  // rows past the last: any
-      to_lds(q_head0 + sub[c] * a.q_head + qu * a.q_token + piece * 16, to + c * (kThreads * 16));
-      advance(query[c], sub[c]);
+      for (int c = 0; c < kCopies; ++c)
+        to_lds(from + c * copy_bytes + (piece ^ turn(c * kAtOnce + r_lane)) * 16, to + c * (kThreads * 16));
+      from += step_bytes;
+    } else {
+#pragma unroll
+      for (int c = 0; c < kCopies; ++c) {
+        const int r = c * kAtOnce + r_lane;
+        if (r0 + c * kAtOnce >= row1) break;
+        int sub;
+        const int query = query_of(min(r0 + r, n_rows - 1), sub);
+        to_lds(q_head0 + sub * a.q_head + (int64_t)query * a.q_token + (piece ^ turn(r)) * 16, to + c * (kThreads * 16));
+      }
     }
     if (tid < kTileRows) {
       next_pos = -1;
       next_lse = 0.0f;
-      if (my_query * a.group + my_sub < row1) {
-        next_pos = offset + my_query;
-        next_lse = a.lse[((int64_t)h * a.group + my_sub) * a.Tq + p.q0 + my_query];
+      if (r0 + tid < row1) {
+        int sub;
+        const int query = query_of(r0 + tid, sub);
+        next_pos = offset + query;
+        next_lse = a.lse[((int64_t)h * a.group + sub) * a.Tq + p.q0 + query];
       }
-      advance(my_query, my_sub);
     }
   };
 
   float total[Own::kBlocks], run[Own::kBlocks];
 #pragma unroll
   for (int b = 0; b < Own::kBlocks; ++b) total[b] = run[b] = 0.0f;
-  if (row0 < row1) bring(0);
-  int buf = 0, flush = 0;
-  for (int r0 = row0; r0 < row1; r0 += kTileRows, buf ^= 1) {
+  f32x16 acc[kMode == kFused ? 2 : 1][Own::kBlocks];  // the block at hand, and the one before it
+  f32x4 l[kMode == kFused ? 2 : 1][4];                // their rows' log-sum-exps
+  int before = 0, stats_at = 0;   // that one: none, every row sees every key of the wave, or some do; its step's statistics
+  const int lane_row = col * kRowBytes;
+  int place[Own::kSteps];
+#pragma unroll
+  for (int j = 0; j < Own::kSteps; ++j) place[j] = lane_row + ((2 * j + hi) ^ turn(col)) * 16;
+
+  const std::integral_constant<int, 0> zero;
+  const std::integral_constant<int, 1> one;
+  // The weights of block `rb` of a step (statistics `at`).
+  auto weigh = [&](auto all, auto H, int at, int rb) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {  // rows 8x + 4hi .. + 3 of the block
+      int pos[4];
+      if constexpr (!decltype(all)::value) __builtin_memcpy(pos, &s_pos[at][32 * rb + 8 * x + 4 * hi], 16);
+#pragma unroll
+      for (int b = 0; b < Own::kBlocks; ++b) {
+        const int j = wave_key + 32 * b + col;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[H][b][4 * x + e], scale[b], -l[H][x][e]));
+          if constexpr (decltype(all)::value) {
+            run[b] += w;
+          } else {
+            const bool seen = (j < n) & (j <= pos[e]) & ((pos[e] - j < a.window) | (j < a.n_sink));
+            run[b] += seen ? w : 0.0f;
+          }
+        }
+      }
+    }
+  };
+  Row ahead[kAhead];               // the first pieces of the next block's rows
+  auto look_ahead = [&](const char* rows) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) ahead[j] = *reinterpret_cast<const Row*>(rows + place[j]);
+  };
+  auto bring_stats = [&](auto H, int at, int rb) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) l[H][x] = *reinterpret_cast<const f32x4*>(&s_lse[at][32 * rb + 8 * x + 4 * hi]);
+  };
+  auto multiply = [&](auto H, const char* rows) {
+#pragma unroll
+    for (int b = 0; b < Own::kBlocks; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[H][b][e] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < Own::kSteps; ++j) {
+      const Row q = kMode == kFused && j < kAhead ? ahead[j] : *reinterpret_cast<const Row*>(rows + place[j]);
+#pragma unroll
+      for (int b = 0; b < Own::kBlocks; ++b) own.product(j, b, q, acc[H][b]);
+    }
+  };
+  // Block `rb` of the step in buffer F: its products, and the weights of the block before.
+  auto block = [&](auto H, auto F, auto RB, int now, int state) {
+    if constexpr (kMode != kFused) {
+      if (state == 0) return;
+      multiply(zero, (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes);
+      bring_stats(zero, now, RB);
+      if (state == 1) weigh(std::true_type(), zero, now, RB);
+      else weigh(std::false_type(), zero, now, RB);
+    } else {
+    constexpr int kBefore = (RB + Own::kRowBlocks - 1) % Own::kRowBlocks;  // that block's place in its step
+    std::integral_constant<int, 1 - H> other;
+    const char* rows = (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes;
+    if (sizeof(T) == 2 && before == 1 && state != 0) {
+      // The epilogue of the block before goes between the products, two elements (d 64: four) to each, its three
+      // steps on three elements' pairs at a time.  (The products of a whole block, then the weights, take the sum of
+      // both times, whether or not other waves are there to use the other unit.)
+      constexpr int kProducts = Own::kSteps * Own::kBlocks, kEach = 16 * Own::kBlocks / kProducts;
+      Row q[Own::kSteps];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) q[j] = ahead[j];
+#pragma unroll
+      for (int b = 0; b < Own::kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[H][b][e] = 0.0f;
+      float arg[2][kEach], w[2][kEach];
+#pragma unroll
+      for (int i = 0; i < kProducts + 2; ++i) {
+        const int j = i / Own::kBlocks;
+        __builtin_amdgcn_sched_barrier(0);
+        if (i < kProducts) {
+          if (i % Own::kBlocks == 0 && j + kAhead < Own::kSteps)
+            q[j + kAhead] = *reinterpret_cast<const Row*>(rows + place[j + kAhead]);
+          own.product(j, i % Own::kBlocks, q[j], acc[H][i % Own::kBlocks]);
+        }
+        if (i == kProducts - 3) bring_stats(H, now, RB);
+        if (RB + 1 < Own::kRowBlocks && i == kProducts - 1) look_ahead(rows + 32 * kRowBytes);
+#pragma unroll
+        for (int x = 0; x < kEach; ++x) {
+          const int e = i * kEach + x;  // element e / kBlocks of key block e % kBlocks
+          if (i >= 2) run[x % Own::kBlocks] += w[i & 1][x];
+          if (i >= 1 && i <= kProducts) w[(i - 1) & 1][x] = __builtin_amdgcn_exp2f(arg[(i - 1) & 1][x]);
+          if (i < kProducts)
+            arg[i & 1][x] = __builtin_fmaf(acc[1 - H][e % Own::kBlocks][e / Own::kBlocks], scale[e % Own::kBlocks],
+                                           -l[1 - H][e / Own::kBlocks / 4][e / Own::kBlocks % 4]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    } else {
+      if (before == 1) weigh(std::true_type(), other, stats_at, kBefore);
+      if (before == 2) weigh(std::false_type(), other, stats_at, kBefore);
+      if (state != 0) multiply(H, rows);
+      bring_stats(H, now, RB);
+      if constexpr (RB + 1 < Own::kRowBlocks) look_ahead(rows + 32 * kRowBytes);
+    }
+    before = state;
+    stats_at = now;
+    }
+  };
+  int r0 = row0, now = 0, flush = 0;
+  auto step = [&](auto F) {
     if (tid < kTileRows) {
       // a row that sees nothing has weight nowhere
-      s_lse[buf][tid] = next_lse == kNegInf ? -kNegInf : next_lse * 1.44269504088896340736f;
-      s_pos[buf][tid] = next_pos;
+      s_lse[now][tid] = next_lse == kNegInf ? -kNegInf : next_lse * 1.44269504088896340736f;
+      s_pos[now][tid] = next_pos;
     }
     // this step's rows lie in LDS (the barrier alone does not wait for a wave's loads to LDS), and nobody reads the
     // other buffer
     __builtin_amdgcn_s_waitcnt(kNoLoads);
     __syncthreads();
-    if (r0 + kTileRows < row1) bring(buf ^ 1);
-    const int last = min(r0 + kTileRows, row1) - 1;
-    const int pos_lo = offset + r0 / a.group, pos_hi = offset + last / a.group;
-    if (wave_key > pos_hi || (wave_key + kWaveKeys <= pos_lo - a.window + 1 && wave_key >= a.n_sink)) continue;
-    const bool all = r0 + kTileRows <= row1 && wave_key + kWaveKeys <= n && wave_key + kWaveKeys - 1 <= pos_lo &&
-                     (wave_key > pos_hi - a.window || wave_key + kWaveKeys <= a.n_sink);
-#pragma unroll
-    for (int rb = 0; rb < Own::kRowBlocks; ++rb) {
-      f32x16 acc[Own::kBlocks];
-#pragma unroll
-      for (int b = 0; b < Own::kBlocks; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[b][e] = 0.0f;
-      const int row = 32 * rb + col;
-      own.products(s_q[buf] + row * kRowBytes, hi, [&](int piece) { return (piece ^ turn(row)) * 16; }, acc);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {  // rows 8x + 4hi .. + 3 of the block
-        const f32x4 l = *reinterpret_cast<const f32x4*>(&s_lse[buf][32 * rb + 8 * x + 4 * hi]);
-        if (all) {
-#pragma unroll
-          for (int b = 0; b < Own::kBlocks; ++b)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) run[b] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[b][4 * x + e], scale[b], -l[e]));
-        } else {
-          int at[4];
-          __builtin_memcpy(at, &s_pos[buf][32 * rb + 8 * x + 4 * hi], 16);
-#pragma unroll
-          for (int b = 0; b < Own::kBlocks; ++b) {
-            const int j = wave_key + 32 * b + col;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[b][4 * x + e], scale[b], -l[e]));
-              const bool seen = (j < n) & (j <= at[e]) & ((at[e] - j < a.window) | (j < a.n_sink));
-              run[b] += seen ? w : 0.0f;
-            }
-          }
-        }
-      }
+    if (kMode != kFew && r0 + kTileRows < row1) bring(std::integral_constant<int, 1 - F>(), r0 + kTileRows);
+    // what block rb's rows see of the wave's keys
+    auto state_of = [&](int rb) {
+      const int first = r0 + 32 * rb;
+      if (first >= some1 || first + 32 <= some0) return 0;
+      return first >= all0 && first + 32 <= all1 ? 1 : 2;
+    };
+    if constexpr (kMode == kFused) look_ahead(F == 0 ? s_even : s_odd);
+    block(zero, F, std::integral_constant<int, 0>(), now, state_of(0));
+    block(one, F, std::integral_constant<int, 1>(), now, state_of(1));
+    if constexpr (Own::kRowBlocks == 4) {
+      block(zero, F, std::integral_constant<int, 2>(), now, state_of(2));
+      block(one, F, std::integral_constant<int, 3>(), now, state_of(3));
     }
-    if (++flush == kFlush) {
+    r0 += kTileRows;
+    now = now == kStats - 1 ? 0 : now + 1;
+  };
+  if (row0 < row1) bring(zero, row0);
+  while (r0 < row1) {
+    step(zero);
+    if constexpr (kMode == kFew) {
+      __syncthreads();  // the rows have been read
+      if (r0 < row1) bring(zero, r0);
+    } else {
+      if (r0 < row1) step(one);
+    }
+    if (++flush == kFlush / 2) {
       flush = 0;
 #pragma unroll
       for (int b = 0; b < Own::kBlocks; ++b) {
@@ -261,6 +370,10 @@ __global__ __launch_bounds__(kThreads, 2) void mass_kernel(const MassArgs a) {
         run[b] = 0.0f;
       }
     }
+  }
+  if constexpr (kMode == kFused) {
+    if (before == 1) weigh(std::true_type(), one, stats_at, Own::kRowBlocks - 1);
+    if (before == 2) weigh(std::false_type(), one, stats_at, Own::kRowBlocks - 1);
   }
 #pragma unroll
   for (int b = 0; b < Own::kBlocks; ++b) {
@@ -292,11 +405,11 @@ __global__ __launch_bounds__(kTileKeys) void mass_join_kernel(const MassArgs a) 
   a.mass_out[at] = j >= n ? 0.0f : a.mass != nullptr ? a.mass[at] + sum : sum;
 }
 
-template <typename T, int D>
+template <typename T, int D, int B, int kMode>
 int run(const MassArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.items * (unsigned)a.n_heads);
-  if (a.k == nullptr) hipLaunchKernelGGL((mass_kernel<T, D, true>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((mass_kernel<T, D, false>), grid, dim3(kThreads), 0, s, a);
+  if (a.k == nullptr) hipLaunchKernelGGL((mass_kernel<T, D, B, kMode, true>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((mass_kernel<T, D, B, kMode, false>), grid, dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -304,14 +417,15 @@ int run(const MassArgs& a, hipStream_t s) {
 
 int launch_mass(const MassArgs& a, int dtype, int d, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == 0) return d == 128 ? run<bf16, 128>(a, s) : run<bf16, 64>(a, s);
-  return d == 128 ? run<float, 128>(a, s) : run<float, 64>(a, s);
+  if (dtype != 0) return d == 128 ? run<float, 128, 1, kApart>(a, s) : run<float, 64, 1, kApart>(a, s);
+  if (a.few) return d == 128 ? run<bf16, 128, 2, kFew>(a, s) : run<bf16, 64, 2, kFew>(a, s);
+  return d == 128 ? run<bf16, 128, 2, kFused>(a, s) : run<bf16, 64, 2, kApart>(a, s);
 }
 
-int launch_mass_join(const MassArgs& a, int dtype, void* stream) {
+int launch_mass_join(const MassArgs& a, void* stream) {
   const dim3 grid((unsigned)a.items * (unsigned)a.n_heads);
-  if (dtype == 0) hipLaunchKernelGGL(mass_join_kernel<mass_keys(0)>, grid, dim3(mass_keys(0)), 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(mass_join_kernel<mass_keys(1)>, grid, dim3(mass_keys(1)), 0, (hipStream_t)stream, a);
+  if (a.keys == kMassKeys) hipLaunchKernelGGL(mass_join_kernel<kMassKeys>, grid, dim3(kMassKeys), 0, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL(mass_join_kernel<2 * kMassKeys>, grid, dim3(2 * kMassKeys), 0, (hipStream_t)stream, a);
   return hipGetLastError();
 }
 
