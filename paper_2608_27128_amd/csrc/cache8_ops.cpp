@@ -145,18 +145,50 @@ int run_mass(const MassArgs& a, int dtype, int d, void* stream) {
 
 KeysAre cached_keys(int dtype) { return dtype == TWINKV_BF16 ? KeysAre::kCached : KeysAre::kCachedFp32; }
 
-// Workspace of an attention over the cache: its own, the log-sum-exps where the caller wants none, the weights' own.
+// How the accumulated weights of an attention over the cache come about.  With at most one tile of rows a problem (and
+// at least one row: an item) the attention keeps its scores, 4 bytes a row and key, and the weights follow in the same
+// kernels; otherwise they are computed afresh from the queries' log-sum-exps.
+bool keeps_scores(int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_rows) {
+  for (int s = 0; s < n_seqs; ++s) {
+    const int64_t rows = (cu_q[s + 1] - cu_q[s]) * group;
+    if (cu_rows[s + 1] > cu_rows[s] && (rows < 1 || rows > kAttnRows)) return false;
+  }
+  return true;
+}
+
+// An attention's plan, and its workspace: its own; with weights wanted the scores, or the log-sum-exps where the caller
+// wants none and the weights' own.
 struct Attn8Layout {
+  AttnPlan plan;
   size_t attn = 0, lse = 0, mass = 0;
+  bool scores = false;
+  int score_rows = 0, score_lds = 0;
   int64_t total() const { return (int64_t)(attn + lse + mass); }
 };
 int attn8_layout(int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_rows,
                  bool want_mass, Attn8Layout& L) {
-  AttnPlan p;
-  int rc = attn_plan(cached_keys(dtype), d, n_heads, group, n_seqs, cu_q, cu_rows, INT64_MAX, 0, p);
+  L.scores = want_mass && keeps_scores(group, n_seqs, cu_q, cu_rows);
+  int64_t most_tiles = kAttnMaxKeys;  // of a split
+  if (L.scores) {
+    for (int s = 0; s < n_seqs; ++s)
+      if (cu_rows[s + 1] > cu_rows[s]) L.score_rows = std::max(L.score_rows, (int)((cu_q[s + 1] - cu_q[s]) * group));
+    most_tiles = kAttnMostLds / (4 * kAttnTile * std::max(L.score_rows, 1));
+  }
+  int rc = attn_plan(cached_keys(dtype), d, n_heads, group, n_seqs, cu_q, cu_rows, INT64_MAX, 0, L.plan, most_tiles);
   if (rc != TWINKV_OK) return rc;
-  L.attn = attn_layout(p, d, n_heads, n_seqs).total;
+  L.attn = attn_layout(L.plan, d, n_heads, n_seqs).total;
   if (!want_mass) return TWINKV_OK;
+  if (L.scores) {
+    for (int s = 0; s < n_seqs; ++s) {
+      const int64_t nk = cu_rows[s + 1] - cu_rows[s], nq = cu_q[s + 1] - cu_q[s];
+      if (nk == 0) continue;
+      const Splits splits = splits_of(key_tiles(nq, nk, group, L.plan), n_heads * row_tiles(nq, group, L.plan), L.plan);
+      L.score_lds = std::max(L.score_lds, (int)(nq * group * std::min(nk, splits.tiles * kAttnTile)));
+    }
+    if (L.plan.parts > 0)
+      L.mass = align_up(4 * (size_t)n_heads * (size_t)L.score_rows * (size_t)cu_rows[n_seqs]) + kAlign;
+    return TWINKV_OK;
+  }
   MassPlan m;
   rc = mass_plan(dtype, n_heads, group, n_seqs, cu_q, cu_rows, kAttnMaxKeys, 0, true, m);
   if (rc != TWINKV_OK) return rc;
@@ -333,26 +365,34 @@ int twinkv_cache8_attention(const void* q, int dtype, int group, const int64_t* 
   if ((rc = check_out(out, dtype, d, out_head_stride, out_token_stride, (int64_t)n_heads * group, no_q)) != TWINKV_OK)
     return rc;
   if (len == nullptr || (mass != nullptr && mass_out == nullptr)) return TWINKV_E_NULL;
+  if (!aligned16(mass) || !aligned16(mass_out)) return TWINKV_E_ARG;
   const bool want_mass = mass_out != nullptr && cache->cu_rows[n_seqs] > 0;
   if (no_q && !want_mass) return TWINKV_OK;
   Attn8Layout L;
   if ((rc = attn8_layout(dtype, d, n_heads, group, n_seqs, cu_q, cache->cu_rows, want_mass, L)) != TWINKV_OK) return rc;
   if (L.total() > 0 && (workspace == nullptr || workspace_bytes < L.total())) return TWINKV_E_WORKSPACE;
   char* ws = static_cast<char*>(workspace);
-  if (want_mass && lse == nullptr) lse = reinterpret_cast<float*>(aligned_base(ws + L.attn));
+  if (want_mass && !L.scores && lse == nullptr) lse = reinterpret_cast<float*>(aligned_base(ws + L.attn));
   if (!no_q) {
     AttnArgs a;
-    rc = attn_args(cached_keys(dtype), q, dtype, d, n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride,
-                   q_token_stride, INT64_MAX, 0, scale, out, out_head_stride, out_token_stride, lse, ws,
-                   (int64_t)L.attn, stream, a);
+    rc = attn_args(L.plan, q, dtype, d, n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride,
+                   q_token_stride, scale, out, out_head_stride, out_token_stride, lse, ws, (int64_t)L.attn, stream,
+                   a);
     if (rc != TWINKV_OK) return rc;
     a.cache = device_cache(cache);
     a.len = len;
+    if (L.scores) {
+      a.score = L.mass > 0 ? reinterpret_cast<float*>(aligned_base(ws + L.attn)) : nullptr;
+      a.score_rows = L.score_rows;
+      a.score_lds = L.score_lds;
+      a.mass = mass;
+      a.mass_out = mass_out;
+    }
     int e = launch_attn8(a, dtype, d, stream);
     if (e == 0 && a.parts > 0) e = launch_attn_join(a, dtype, d, stream);
     if (e != 0) return TWINKV_E_HIP;
   }
-  if (!want_mass) return TWINKV_OK;
+  if (!want_mass || L.scores) return TWINKV_OK;
   MassArgs a;
   rc = mass_args(dtype, q, n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride, INT64_MAX, 0, scale,
                  true, lse, mass, mass_out, ws + L.attn + L.lse, (int64_t)L.mass, stream, a);

@@ -281,8 +281,9 @@ constexpr int64_t kPairWork = 49152;
 // 769 / 709; two rows a token, 2048 tokens (1) 136 / 136, 3000 (0.68) 240 / 224.
 constexpr int64_t kWideTiles = 20, kLongTiles64 = 96;
 
-inline int attn_plan(KeysAre keys, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
-              int64_t n_sink, AttnPlan& p) {
+// most_tiles: a split has no more.
+inline int attn_plan(KeysAre keys, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k,
+                     int64_t window, int64_t n_sink, AttnPlan& p, int64_t most_tiles = kAttnMaxKeys) {
   p.window = std::min<int64_t>(window, kAttnMaxKeys);
   p.n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
   const bool cached = keys == KeysAre::kCached || keys == KeysAre::kCachedFp32;
@@ -317,7 +318,8 @@ inline int attn_plan(KeysAre keys, int d, int n_heads, int group, int n_seqs, co
     each = kAttnMaxKeys;
     p.whole_tiles = kAttnMaxKeys;  // (nor for one sequence among others)
   }
-  p.split_tiles = (std::min<int64_t>(each, kAttnMaxKeys / 64) + 3) / 4 * 4;
+  p.split_tiles = std::min((std::min<int64_t>(each, kAttnMaxKeys / 64) + 3) / 4 * 4, most_tiles / 4 * 4);
+  p.whole_tiles = std::min(p.whole_tiles, most_tiles);
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t nq = cu_q[s + 1] - cu_q[s];
     const int64_t rows = row_tiles(nq, group, p);
@@ -355,14 +357,11 @@ inline int check_queries(int n_seqs, const int64_t* cu_q, int group) {
   return TWINKV_OK;
 }
 
-// The queries' and outputs' side of a call, the plan, the words and the parts.
-inline int attn_args(KeysAre keys, const void* q, int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q,
-              const int64_t* cu_k, int64_t q_head_stride, int64_t q_token_stride, int64_t window, int64_t n_sink,
-              float scale, void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse,
-              void* workspace, int64_t workspace_bytes, void* stream, AttnArgs& a) {
-  AttnPlan p;
-  const int rc = attn_plan(keys, d, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
-  if (rc != TWINKV_OK) return rc;
+// The queries' and outputs' side of a call, the words and the parts.
+inline int attn_args(const AttnPlan& p, const void* q, int dtype, int d, int n_heads, int group, int n_seqs,
+                     const int64_t* cu_q, const int64_t* cu_k, int64_t q_head_stride, int64_t q_token_stride, float scale,
+                     void* out, int64_t out_head_stride, int64_t out_token_stride, float* lse, void* workspace,
+                     int64_t workspace_bytes, void* stream, AttnArgs& a) {
   const AttnLayout L = attn_layout(p, d, n_heads, n_seqs);
   if (L.total > 0 && (workspace == nullptr || workspace_bytes < (int64_t)L.total)) return TWINKV_E_WORKSPACE;
   if (heads_overlap(out_head_stride, out_token_stride, (int64_t)n_heads * group, cu_q[n_seqs], d)) return TWINKV_E_ARG;
@@ -392,6 +391,11 @@ inline int attn_args(KeysAre keys, const void* q, int dtype, int d, int n_heads,
   a.rows = p.rows;
   a.part_o = reinterpret_cast<float*>(ws + L.part_o);
   a.part_ml = reinterpret_cast<float*>(ws + L.part_ml);
+  a.score = nullptr;
+  a.score_rows = 0;
+  a.score_lds = 0;
+  a.mass = nullptr;
+  a.mass_out = nullptr;
   WordWriter w(a.seq, ((int64_t)n_seqs + 1) * kAttnSeqWords, ws, stream);
   int64_t item = 0, part = 0;
   for (int s = 0; s <= n_seqs; ++s) {

@@ -98,8 +98,11 @@ int twinkv_sink_attention(const void* q, const void* k, const void* v, int dtype
   const KeysAre keys = dtype != TWINKV_BF16 ? KeysAre::kRowsFp32
                        : std::max(k_token_stride, v_token_stride) <= INT32_MAX / (2 * 64) ? KeysAre::kRowsOfMany
                                                                                          : KeysAre::kRows;
-  rc = attn_args(keys, q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride, window, n_sink,
-                 scale, out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
+  AttnPlan p;
+  rc = attn_plan(keys, d, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, p);
+  if (rc != TWINKV_OK) return rc;
+  rc = attn_args(p, q, dtype, d, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride, scale, out,
+                 out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
   a.k = static_cast<const char*>(k);
@@ -208,9 +211,12 @@ int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* 
   if (len == nullptr) return TWINKV_E_NULL;
   if (no_q) return TWINKV_OK;
   AttnArgs a;
-  rc = attn_args(dtype == TWINKV_BF16 ? KeysAre::kCached : KeysAre::kCachedFp32, q, dtype, d, cache->n_heads, group, n_seqs,
-                 cu_q, cache->cu_rows, q_head_stride, q_token_stride, INT64_MAX, 0, scale, out, out_head_stride,
-                 out_token_stride, lse, workspace, workspace_bytes, stream, a);
+  AttnPlan p;
+  rc = attn_plan(dtype == TWINKV_BF16 ? KeysAre::kCached : KeysAre::kCachedFp32, d, cache->n_heads, group, n_seqs, cu_q,
+                 cache->cu_rows, INT64_MAX, 0, p);
+  if (rc != TWINKV_OK) return rc;
+  rc = attn_args(p, q, dtype, d, cache->n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride, scale,
+                 out, out_head_stride, out_token_stride, lse, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   a.cache = device_cache(cache);
   a.len = len;

@@ -73,6 +73,8 @@ int launch_cache4_gather(const Cache4Args& a, int dtype, int d, void* stream);
 int launch_cache4_append(const Cache4Args& a, int max_new, int dtype, int d, void* stream);
 int launch_cache4_read(const Cache4Args& a, int dtype, int d, void* stream);
 
+// Attention over 8 bits with accumulated weights: bytes of an item's scores.  Two workgroups' fill a CU's LDS.
+constexpr int kAttnMostLds = 70 * 1024;
 // Attention.  Rows of a problem (KV head, sequence) are its queries times its query heads: row
 // r = i * group + g.  An item is a tile of rows and a range of key tiles; a problem's items are
 // row tiles times splits.  Words per sequence: first query, first key, first item, splits, key tiles of a
@@ -103,6 +105,12 @@ struct AttnArgs {
   int rows;              // of an item: kAttnRows, kAttnPairRows, kAttnWideRows or kAttnBigRows
   float* part_o;         // [n_heads][parts][rows][d] unnormalised sums
   float* part_ml;        // [n_heads][parts][rows][2] maximum (log2 units) and sum
+  // 8 bits, one row tile a problem: accumulated weights wanted (else all null)
+  float* score;          // [n_heads][score_rows][cache.C] scores in log2 units
+  int score_rows;
+  int score_lds;         // scores of an item that a workgroup's LDS holds
+  const float* mass;     // nullable [n_heads][cache.C]
+  float* mass_out;       // [n_heads][cache.C]
 };
 int launch_attn(const AttnArgs& a, int dtype, int d, void* stream);
 // bf16

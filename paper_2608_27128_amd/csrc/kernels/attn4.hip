@@ -296,6 +296,31 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(const AttnArgs 
     if (a.lse != nullptr && c == 0)
       a.lse[head * a.Tq + p.q0 + i] = sum == 0.0f ? kNegInf : top * 0.69314718055994530942f + logf(sum);
   }
+  if (a.mass_out == nullptr) return;
+  // The accumulated weights of the split's keys (one tile of 16 rows a problem): every row's maximum and sum again, 16
+  // threads a row.
+  __shared__ float s_lse[kAttnRows];
+  static_assert(kJoinThreads == 16 * kAttnRows, "16 threads a row");
+  const int r = threadIdx.x / 16;
+  float top = kNegInf, sum = 0.0f;
+  auto add = [&](float m, float l) {
+    const float next = fmaxf(top, m);
+    sum = sum * (next == top ? 1.0f : __builtin_amdgcn_exp2f(top - next)) + l * (m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next));
+    top = next;
+  };
+  const float* ml = a.part_ml + ((p.part - p.split) * rows + r) * 2;
+  for (int k = threadIdx.x % 16; k < p.splits; k += 16) add(ml[(int64_t)k * rows * 2], ml[(int64_t)k * rows * 2 + 1]);
+#pragma unroll
+  for (int by = 1; by < 16; by *= 2) {
+    const float m = __shfl_xor(top, by), l = __shfl_xor(sum, by);
+    add(m, l);
+  }
+  if (threadIdx.x % 16 == 0) s_lse[r] = lse_log2(top, sum);
+  __syncthreads();
+  const float* scores = score_rows_of(a, p);
+  add_weights(a, p, s_lse, (int)threadIdx.x, kJoinThreads, [&](int row, int j) {
+    return *reinterpret_cast<const f32x4*>(scores + (int64_t)row * a.cache.C + j);
+  });
 }
 
 template <typename T, int D, int R>

@@ -61,12 +61,15 @@ struct Tile8 {
   }
 };
 
-// R: row tiles of 16 that a wave takes at once; what it unpacks serves them all.
-template <typename T, int D, int R>
+// R: row tiles of 16 that a wave takes at once; what it unpacks serves them all.  kScores: the scores are
+// kept in LDS (one row tile a problem).  The accumulated weights follow from there where an item has all of the
+// problem's keys; otherwise the scores go out, and the weights follow in the join.
+template <typename T, int D, int R, bool kScores>
 __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 && R == 1 ? 4 : 2) void attn8_kernel(const AttnArgs a) {
   constexpr int kSteps = D / 32;
   constexpr int N = kParts<T>;
   __shared__ float s_join[join_floats<D>()];
+  extern __shared__ __attribute__((aligned(16))) float s_score[];  // [rows][keys of the item]
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const AttnItem p = attn_item(a, (int)blockIdx.x, (int)blockIdx.y);
@@ -107,6 +110,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 && R == 1 ? 4 : 2) 
     for (int n = 0; n < D / 16; ++n) acc[r][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   constexpr int kStep = kAttnTile * kAttnWaves;
   const int first = t0 + wave * kAttnTile;
+  const int keys = min(p.tiles * kAttnTile, p.nk - t0);  // of the item, seen or not
   Tile8<D> now(a.cache, p.h, (int64_t)p.k0 + first, i, g);
   if (first < t1) {
     now.load_keys();
@@ -143,6 +147,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 && R == 1 ? 4 : 2) 
         for (int e = 0; e < 8; ++e)
           if (t + 8 * g + e >= lim[r]) s[r][e] = kNegInf;
     }
+    if constexpr (kScores) {
+      // (lanes past the last row have its scores and write the same)
+      float* to = s_score + min(i, n_rows - 1) * keys + (t - t0) + 8 * g;
+      *reinterpret_cast<f32x4*>(to) = f32x4{s[0][0], s[0][1], s[0][2], s[0][3]};
+      *reinterpret_cast<f32x4*>(to + 4) = f32x4{s[0][4], s[0][5], s[0][6], s[0][7]};
+    }
     const float scale_v = __uint_as_float(now.vs << 23);
     bf16x8 w[R][N];
 #pragma unroll
@@ -174,21 +184,41 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 && R == 1 ? 4 : 2) 
     join_waves<T, D>(a, p, row0 + r * kAttnRows, st[r], acc[r], s_join,
                      [](int n, int lane16) { return (n >> 1) * 32 + 2 * lane16 + (n & 1); });
   }
+  if constexpr (kScores) {
+    if (p.splits > 1) {  // the join knows the rows' sums
+      float* to = score_rows_of(a, p) + t0;
+      for (int j = 4 * (int)threadIdx.x; j < t1 - t0; j += 4 * 64 * kAttnWaves)
+        for (int r = 0; r < n_rows; ++r)
+          *reinterpret_cast<f32x4*>(to + (int64_t)r * a.cache.C + j) = *reinterpret_cast<const f32x4*>(s_score + r * keys + j);
+      return;
+    }
+    __shared__ float s_lse[kAttnRows];
+    // (the tile's maxima and sums lie first in the join's place)
+    if (threadIdx.x < kAttnRows) s_lse[threadIdx.x] = lse_log2(s_join[threadIdx.x], s_join[kAttnRows + threadIdx.x]);
+    __syncthreads();
+    add_weights(a, p, s_lse, (int)threadIdx.x, 64 * kAttnWaves,
+                [&](int row, int j) { return *reinterpret_cast<const f32x4*>(s_score + row * keys + j); });
+  }
 }
 
-template <typename T, int D, int R>
+template <typename T, int D, int R, bool kScores>
 int run8(const AttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attn8_kernel<T, D, R>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves), 0, s, a);
+  hipLaunchKernelGGL((attn8_kernel<T, D, R, kScores>), dim3((unsigned)a.items, (unsigned)a.n_heads), dim3(64 * kAttnWaves),
+                     4 * (unsigned)a.score_lds, s, a);
   return hipGetLastError();
+}
+template <typename T, int D>
+int run8(const AttnArgs& a, hipStream_t s) {
+  return a.mass_out != nullptr ? run8<T, D, 1, true>(a, s) : run8<T, D, 1, false>(a, s);
 }
 
 }  // namespace
 
 int launch_attn8(const AttnArgs& a, int dtype, int d, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  if (dtype != 0) return d == 128 ? run8<float, 128, 1>(a, s) : run8<float, 64, 1>(a, s);
-  if (a.rows == kAttnPairRows) return d == 128 ? run8<bf16, 128, 2>(a, s) : run8<bf16, 64, 2>(a, s);
-  return d == 128 ? run8<bf16, 128, 1>(a, s) : run8<bf16, 64, 1>(a, s);
+  if (dtype != 0) return d == 128 ? run8<float, 128>(a, s) : run8<float, 64>(a, s);
+  if (a.rows == kAttnPairRows) return d == 128 ? run8<bf16, 128, 2, false>(a, s) : run8<bf16, 64, 2, false>(a, s);
+  return d == 128 ? run8<bf16, 128>(a, s) : run8<bf16, 64>(a, s);
 }
 
 }  // namespace twinkv

@@ -198,6 +198,39 @@ constexpr int join_floats() {
   return kAttnWaves * 2 * kAttnRows + kAttnRows * (D + 4);
 }
 
+// The weights of an item's keys, summed over the problem's rows (one tile), from their scores (score(r, j): those of
+// row r and keys j .. j + 3) and the rows' log-sum-exps in log2 units (+inf where a row sees nothing), added to what the
+// keys have.
+template <typename Score>
+__device__ inline void add_weights(const AttnArgs& a, const AttnItem& p, const float* lse, int tid, int threads,
+                                   const Score& score) {
+  const int n_rows = p.nq * a.group;
+  const int len = min(max(a.len[(int64_t)p.h * a.n_seqs + p.s], 0), p.nk);
+  const int t0 = p.split * p.tiles * kAttnTile, t1 = min(t0 + p.tiles * kAttnTile, p.nk);
+  const int64_t at = (int64_t)p.h * a.cache.C + p.k0;
+  for (int j = t0 + 4 * tid; j < t1; j += 4 * threads) {  // (a problem's rows are a multiple of 32)
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (j < len) {
+      if (a.mass != nullptr) sum = *reinterpret_cast<const f32x4*>(a.mass + at + j);
+      f32x4 more = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+      for (int r = 0; r < n_rows; ++r) {
+        const f32x4 s = score(r, j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) more[e] += __builtin_amdgcn_exp2f(s[e] - lse[r]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = j + e < len ? sum[e] + more[e] : 0.0f;
+    }
+    *reinterpret_cast<f32x4*>(a.mass_out + at + j) = sum;
+  }
+}
+// A problem's scores in memory.
+__device__ inline float* score_rows_of(const AttnArgs& a, const AttnItem& p) {
+  return a.score + (int64_t)p.h * a.score_rows * a.cache.C + p.k0;
+}
+__device__ inline float lse_log2(float m, float l) { return l == 0.0f ? -kNegInf : m + __builtin_amdgcn_logf(l); }
+
 // One wave's own 16 rows, complete, through its own LDS.
 template <typename T, int D, typename Channel>
 __device__ inline void write_own(const AttnArgs& a, const AttnItem& p, int row0, const RowStats& st,
