@@ -25,6 +25,8 @@ constexpr int kOk = 0, kMismatch = 1, kNonfinite = 2;  // TWINKV_PROBLEM_*
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kByteMin = 1, kByteMax = 248;            // 127 * 2^121 is finite in fp32 and bf16
+constexpr int kBlockBits = 5;
+static_assert(1 << kBlockBits == kCache8Block, "rows of a block");
 constexpr int kAppendBlocks = 4;                       // that one wave writes one after the other
 
 // A lane's part of a block: rows 8 sub .. 8 sub + 7, channels at .. at + kCh.
@@ -145,6 +147,10 @@ __device__ inline void store_channels(uint8_t* p, const unsigned (&ch)[CH][2]) {
     *reinterpret_cast<u32x4*>(p + c * 8) = u32x4{ch[c][0], ch[c][1], ch[c + 1][0], ch[c + 1][1]};
 }
 
+// The byte of the scale for a block whose largest magnitude has these bits: from 255/256 of a power of two on it
+// rounds up to the next.
+__device__ inline int byte_for(unsigned most) { return min(max((int)((most + 0x10000u) >> 23) - 6, kByteMin), kByteMax); }
+
 // Codes of a lane's 8 rows (those whose bit is set in `rows`; the others' are zero) under the block's scale, whose
 // byte is at least `least`.  A row with an element that is not finite is stored as zeros.  value(r, c): the
 // element's bits.  All lanes of a wave call it.
@@ -170,8 +176,7 @@ __device__ inline int encode(unsigned rows, int least, unsigned (&w)[8][CH / 4],
   for (int r = 0; r < 8; ++r) most = max(most, (rows >> r) & 1u ? top[r] : 0u);
 #pragma unroll
   for (int by = 1; by < 64; by *= 2) most = max(most, lane_xor(most, by));
-  const int need = min(max((int)((most + 0x10000u) >> 23) - 6, kByteMin), kByteMax);
-  const int byte = max(need, least);
+  const int byte = max(byte_for(most), least);
   const float inv = power_of(254 - byte);
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
@@ -451,6 +456,51 @@ __global__ __launch_bounds__(kThreads) void cache8_read_kernel(const Cache8Args 
 
 // ---- the rows that an eviction keeps ----
 
+// Codes of a lane's 8 rows (those whose bit is set in `rows`; the others' become zero) under their rows' scales, brought
+// to the scale of the block they now share; returns its byte.  Where a row of the largest scale has a code over 64, that
+// scale stays, and only rows of smaller ones change: no work for most blocks.
+template <int CH>
+__device__ inline int move_codes(unsigned rows, const int (&from)[8], unsigned (&w)[8][CH / 4]) {
+  constexpr int W = CH / 4;
+  int top = 0;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) top = max(top, (rows >> r) & 1u ? from[r] : 0);
+#pragma unroll
+  for (int by = 16; by < 64; by *= 2) top = max(top, __shfl_xor(top, by));  // (16 lanes share a row)
+  unsigned large = 0;  // a byte's upper bits differ: 64 .. 127 or -128 .. -65
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if (((rows >> r) & 1u) == 0) w[r][i] = 0u;
+      large |= from[r] == top ? (w[r][i] ^ (w[r][i] << 1)) & 0x80808080u : 0u;
+    }
+  int byte = top;
+  if (!__any(large != 0)) {
+    unsigned most = 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      float m = 0.0f;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) m = fmaxf(m, fabsf(code_of(w[r][c / 4], c & 3)));
+      most = max(most, (rows >> r) & 1u ? __float_as_uint(m * power_of(from[r])) : 0u);
+    }
+#pragma unroll
+    for (int by = 1; by < 64; by *= 2) most = max(most, lane_xor(most, by));
+    byte = byte_for(most);
+  }
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    if (from[r] == byte) continue;
+    const float f = power_of(min(max(127 + from[r] - byte, 0), 254));  // (rows of zeros may come from far above)
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      w[r][i] = pack4(nearest(code_of(w[r][i], 0) * f), nearest(code_of(w[r][i], 1) * f), nearest(code_of(w[r][i], 2) * f),
+                      nearest(code_of(w[r][i], 3) * f));
+  }
+  return byte;
+}
+
 // K12b: a wave per block of the new cache.  Its rows come from rising rows of the old one: the keys straight, the
 // values 32 rows of the old cache at a time, turned to rows in the wave's own LDS, from where each lane takes those
 // that it needs.
@@ -480,22 +530,46 @@ __global__ __launch_bounds__(kThreads) void evict8_move_kernel(const Evict8Args 
   const Part<D> p;
   const unsigned mine = rows_between(p.sub, 0, hi);
   const int64_t head = (int64_t)h * a.from.C + from0;
-  unsigned kc[8][W], vc[8][W];
-  float ks[8], vs[8];
-#pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    const int64_t at = head + __shfl(row, min(8 * p.sub + r, hi - 1));
-    load_words<W>(a.from.k_codes + at * D + p.at, kc[r]);
-    ks[r] = power_of(a.from.k_scales[at / kCache8Block]);
-    vs[r] = power_of(a.from.v_scales[at / kCache8Block]);
-#pragma unroll
-    for (int i = 0; i < W; ++i) vc[r][i] = 0u;
+  const Place<D> to(a.to, h, to0, p);
+  int k_byte = 0, v_byte = 0;
+  if (row >= 0) {
+    k_byte = a.from.k_scales[(head + row) / kCache8Block];
+    v_byte = a.from.v_scales[(head + row) / kCache8Block];
   }
-  for (int next = 0; next < hi;) {  // (next, and what follows from it, is the same in all lanes)
-    const int group = __builtin_amdgcn_readfirstlane(__shfl(row, next) / kCache8Block);
-    unsigned ch[CH][2], turned[8][W];
+  // (next, and what follows from it, is the same in all lanes)
+  auto group_at = [&](int next) { return __builtin_amdgcn_readfirstlane(__shfl(row, next) / kCache8Block); };
+  unsigned ch[CH][2];
+  auto load_group = [&](int group) {
     load_channels<CH>(a.from.v_codes + (head + group * (int64_t)kCache8Block + 8 * p.sub) * D + p.at * 8, ch);
+  };
+  int group = group_at(0);
+  int from[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) from[r] = __shfl(row, 8 * p.sub + r);  // (-1 past the last: in no group)
+  unsigned w[8][W];
+  int bytes[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) load_words<W>(a.from.k_codes + (head + max(from[r], 0)) * D + p.at, w[r]);
+  load_group(group);
+#pragma unroll
+  for (int r = 0; r < 8; ++r) bytes[r] = __shfl(k_byte, 8 * p.sub + r);
+  const int kb = move_codes<CH>(mine, bytes, w);
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+    if ((mine >> r) & 1u) store_words<W>(to.k + r * D, w[r]);
+  if (lane == 0) *to.ks = (uint8_t)kb;
+
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[r][i] = 0u;
+  for (int next = 0; next < hi;) {
+    next += (int)__popcll(__ballot(row >= 0 && row / kCache8Block == group));
+    unsigned turned[8][W];
     to_rows<CH>(ch, turned);
+    // the next group, or this one once more, on its way while this one goes through LDS
+    const int ahead = next < hi ? group_at(next) : group;
+    load_group(ahead);
 #pragma unroll
     for (int r = 0; r < 8; ++r)
 #pragma unroll
@@ -504,34 +578,26 @@ __global__ __launch_bounds__(kThreads) void evict8_move_kernel(const Evict8Args 
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      const int from = __shfl(row, 8 * p.sub + r);  // (-1 past the last: in no group)
-      if (from >= 0 && from / kCache8Block == group)
+    for (int r = 0; r < 8; ++r)
 #pragma unroll
-        for (int i = 0; i < W; ++i) vc[r][i] = s_rows[wave][from % kCache8Block][p.at / 4 + i];
-    }
-    next += (int)__popcll(__ballot(row >= 0 && row / kCache8Block == group));
+      for (int i = 0; i < W; ++i) turned[r][i] = s_rows[wave][from[r] & (kCache8Block - 1)][p.at / 4 + i];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[r][i] = from[r] >> kBlockBits == group ? turned[r][i] : w[r][i];
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    group = ahead;
   }
-  const Place<D> to(a.to, h, to0, p);
-  bool none = false;  // every value is finite
-  unsigned w[8][W];
-  const int kb = encode<CH>(mine, 0, w, none, [&](int r, int c) { return __float_as_uint(code_of(kc[r][c / 4], c & 3) * ks[r]); });
 #pragma unroll
-  for (int r = 0; r < 8; ++r)
-    if ((mine >> r) & 1u) store_words<W>(to.k + r * D, w[r]);
-  const int vb = encode<CH>(mine, 0, w, none, [&](int r, int c) { return __float_as_uint(code_of(vc[r][c / 4], c & 3) * vs[r]); });
+  for (int r = 0; r < 8; ++r) bytes[r] = __shfl(v_byte, 8 * p.sub + r);
+  const int vb = move_codes<CH>(mine, bytes, w);
   if (mine != 0) {
-    unsigned ch[CH][2];
     to_channels<CH>(w, ch);
     store_channels<CH>(to.v, ch);
   }
-  if (lane == 0) {
-    *to.ks = (uint8_t)kb;
-    *to.vs = (uint8_t)vb;
-  }
+  if (lane == 0) *to.vs = (uint8_t)vb;
 }
 
 unsigned groups_of(int blocks) { return (unsigned)((blocks + kWaves - 1) / kWaves); }

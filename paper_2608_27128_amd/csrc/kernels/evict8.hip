@@ -21,7 +21,7 @@ constexpr int kRun = 8;  // rows a thread lists
 template <int NT, int CAP>
 __global__ __launch_bounds__(NT) void evict8_select_kernel(const Evict8Args a) {
   constexpr int NW = NT / 64, DBITS = NT >= 1024 ? 11 : 8;
-  __shared__ uint32_t s_key[CAP > 0 ? CAP : 1];
+  __shared__ __attribute__((aligned(16))) uint32_t s_key[CAP > 0 ? CAP : 4];
   __shared__ int s_hist[2][1 << DBITS];
   __shared__ uint32_t s_bits[NW][2];
   __shared__ int s_wave[NW], s_pick[3];
@@ -36,10 +36,10 @@ __global__ __launch_bounds__(NT) void evict8_select_kernel(const Evict8Args a) {
   int32_t* out = a.pos_out + (int64_t)h * a.to.C + to0;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // (n_recent may be anything up to 2^31 - 1)
-  auto key_in = [&](int t) { return t < a.n_sink || t >= len - (int64_t)a.n_recent ? 0u : score_key(mass[t]); };
+  auto key_in = [&](int t, float f) { return t < a.n_sink || t >= len - (int64_t)a.n_recent ? 0u : score_key(f); };
   auto key_of = [&](int t) {
     if constexpr (CAP > 0) return s_key[t];
-    else return key_in(t);
+    else return key_in(t, mass[t]);
   };
 
   uint32_t cut_key = 0u;
@@ -48,12 +48,20 @@ __global__ __launch_bounds__(NT) void evict8_select_kernel(const Evict8Args a) {
   if (cut) {
     for (int i = tid; i < (1 << DBITS); i += NT) s_hist[0][i] = 0;
     uint32_t kand = ~0u, kor = 0u;
-#pragma unroll 4
-    for (int t = tid; t < len; t += NT) {
-      const uint32_t k = key_in(t);
+    auto see = [&](int t, float f) {
+      const uint32_t k = key_in(t, f);
       if constexpr (CAP > 0) s_key[t] = k;
       kand &= k;
       kor |= k;
+    };
+    constexpr int kLoads = CAP > 0 ? CAP / NT : 8;  // in flight together
+    for (int t0 = 0; t0 < len; t0 += kLoads * NT) {
+      float f[kLoads];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) f[u] = mass[min(t0 + u * NT + tid, len - 1)];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u)
+        if (t0 + u * NT + tid < len) see(t0 + u * NT + tid, f[u]);
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) {
