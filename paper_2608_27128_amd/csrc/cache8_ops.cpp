@@ -8,9 +8,11 @@ namespace {
 
 // ---- accumulated weights ----
 
-// A sequence's key tiles, and the splits of the rows that see one.
+// A sequence's key tiles, and the splits of the rows that see one (kMassSeqWords).
 struct MassSeq {
   int64_t tiles = 0, splits = 1, rows = 0;
+  int64_t full = 0, run = 0;
+  int64_t items = 0;
 };
 struct MassPlan {
   int64_t keys = 0;        // of a tile
@@ -35,12 +37,26 @@ constexpr int64_t kMassFew = 256;
 
 MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_sink, bool cached, const MassPlan& p) {
   MassSeq m;
-  const int64_t rows = rows_seeing(nq, nk, group, window, n_sink, p.keys, cached);
+  const int64_t rows = rows_seeing(nq, nk, group, window, n_sink, p.keys, cached), tile_rows = p.keys * group;
   m.tiles = (nk + p.keys - 1) / p.keys;
+  if (!cached && window >= nk && nq > 0 && rows > 2 * std::max(p.most_rows, tile_rows)) {
+    // Causal: tile by tile the rows that see one get fewer by tile_rows, once the tile lies behind the first query.
+    // Splits of a whole number of them make a run of tiles after which there is one split less, and no item is empty.
+    m.run = std::max<int64_t>(1, p.most_rows / tile_rows);
+    m.rows = m.run * tile_rows;
+    m.full = std::min(m.tiles, std::max<int64_t>(nk - nq, 0) / p.keys + 1);
+    m.splits = (rows + m.rows - 1) / m.rows;
+    m.items = m.full * m.splits;
+    int64_t splits = m.splits;
+    for (int64_t t = m.full; t < m.tiles; t += m.run, splits = std::max<int64_t>(1, splits - 1))
+      m.items += std::min(m.run, m.tiles - t) * splits;
+    return m;
+  }
   m.splits = std::max<int64_t>(1, (rows + p.most_rows - 1) / p.most_rows);
   const int64_t each = (rows + m.splits - 1) / m.splits;
   m.rows = std::max<int64_t>(1, (each + kMassRowTile - 1) / kMassRowTile) * kMassRowTile;
   m.splits = std::max<int64_t>(1, (rows + m.rows - 1) / m.rows);
+  m.items = m.tiles * m.splits;
   return m;
 }
 
@@ -65,8 +81,8 @@ int mass_plan(int dtype, int n_heads, int group, int n_seqs, const int64_t* cu_q
   p.most_rows = std::max((int64_t)(work / kMassItems), std::min(kMassLeast, std::max<int64_t>(even, kMassRowTile)));
   for (int s = 0; s < n_seqs; ++s) {
     const MassSeq m = mass_seq(cu_q[s + 1] - cu_q[s], cu_k[s + 1] - cu_k[s], group, window, n_sink, cached, p);
-    p.items += m.tiles * m.splits;
-    if (m.splits > 1) p.parts += m.tiles * m.splits;
+    p.items += m.items;
+    if (m.splits > 1) p.parts += m.items;
   }
   return grid_ok(p.items * n_heads, 256) && p.items <= INT32_MAX ? TWINKV_OK : TWINKV_E_ARG;
 }
@@ -130,8 +146,10 @@ int mass_args(int dtype, const void* q, int n_heads, int group, int n_seqs, cons
     w.put((int32_t)m.splits);
     w.put((int32_t)std::min<int64_t>(m.rows, INT32_MAX));
     w.put((int32_t)part);
-    item += m.tiles * m.splits;
-    if (m.splits > 1) part += m.tiles * m.splits;
+    w.put((int32_t)m.full);
+    w.put((int32_t)m.run);
+    item += m.items;
+    if (m.splits > 1) part += m.items;
   }
   return hip_status(w.finish());
 }

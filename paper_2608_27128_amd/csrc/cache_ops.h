@@ -150,11 +150,11 @@ struct Evict8Args {
 int launch_evict8_select(const Evict8Args& a, void* stream);
 int launch_evict8_move(const Evict8Args& a, int d, void* stream);
 
-// The weight that each key receives.  Rows are numbered as in the attention; an item is a tile of keys
-// and a range of row tiles, counted from the first that sees a key of the tile.  Words per sequence: first query,
-// first key, first item, items of a key tile (splits), rows of a split, first part (of sequences with more than one
-// split).
-constexpr int kMassSeqWords = 6;
+// The weight that each key receives.  Rows are numbered as in the attention; an item is a tile of keys and a split of
+// the rows that see one of them, counted from the first.  Words per sequence: first query, first key, first item, the
+// most splits of a tile, rows of a split, first part (of sequences with more than one split), full tiles, run.  The
+// first `full` tiles have all the splits; then, from run to run of tiles, one less (run 0: every tile has them all).
+constexpr int kMassSeqWords = 8;
 constexpr int kMassRowTile = 128;  // splits are whole numbers of so many rows
 constexpr int kMassKeys = 128;     // of a tile; bf16: or twice as many
 struct MassArgs {

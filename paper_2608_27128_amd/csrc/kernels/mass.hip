@@ -91,8 +91,19 @@ __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
   p.splits = seq_word(a.seq, w + 3);
   p.rows = seq_word(a.seq, w + 4);
   p.part = (int64_t)h * a.parts + seq_word(a.seq, w + 5) + i;
-  p.kt = i / p.splits;
-  p.split = i - p.kt * p.splits;
+  const int full = seq_word(a.seq, w + 6), run = seq_word(a.seq, w + 7);
+  int tile0 = 0, left = i;  // where tiles of p.splits splits begin, and the place among their items
+  if (run > 0 && left >= full * p.splits) {
+    left -= full * p.splits;
+    tile0 = full;
+    while (p.splits > 1 && left >= run * p.splits) {
+      left -= run * p.splits;
+      tile0 += run;
+      --p.splits;
+    }
+  }
+  p.kt = tile0 + left / p.splits;
+  p.split = left % p.splits;
   p.nq = seq_word(a.seq, w + kMassSeqWords) - p.q0;
   p.nk = seq_word(a.seq, w + kMassSeqWords + 1) - p.k0;
   return p;
@@ -400,6 +411,7 @@ __global__ __launch_bounds__(kTileKeys) void mass_join_kernel(const MassArgs a) 
   if (j >= p.nk) return;
   const int n = a.len != nullptr ? min(max(a.len[(int64_t)h * a.n_seqs + p.s], 0), p.nk) : p.nk;
   float sum = 0.0f;
+#pragma unroll 16
   for (int k = 0; k < p.splits; ++k) sum += a.part[(p.part + k) * kTileKeys + threadIdx.x];
   const int64_t at = (int64_t)h * a.Tk + p.k0 + j;
   a.mass_out[at] = j >= n ? 0.0f : a.mass != nullptr ? a.mass[at] + sum : sum;
