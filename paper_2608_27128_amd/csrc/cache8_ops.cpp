@@ -56,7 +56,11 @@ MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_si
   const int64_t each = (rows + m.splits - 1) / m.splits;
   m.rows = std::max<int64_t>(1, (each + kMassRowTile - 1) / kMassRowTile) * kMassRowTile;
   m.splits = std::max<int64_t>(1, (rows + m.rows - 1) / m.rows);
-  m.items = m.tiles * m.splits;
+  // tiles with sinks are seen by all queries, the others by those of a window
+  m.full = cached || n_sink == 0 ? m.tiles : std::min(m.tiles, (n_sink + p.keys - 1) / p.keys);
+  const int64_t rest = std::max<int64_t>(1, (rows_seeing(nq, nk, group, window, 0, p.keys, cached) + m.rows - 1) / m.rows);
+  m.run = -rest;
+  m.items = m.full * m.splits + (m.tiles - m.full) * rest;
   return m;
 }
 

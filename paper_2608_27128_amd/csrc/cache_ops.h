@@ -153,7 +153,8 @@ int launch_evict8_move(const Evict8Args& a, int d, void* stream);
 // The weight that each key receives.  Rows are numbered as in the attention; an item is a tile of keys and a split of
 // the rows that see one of them, counted from the first.  Words per sequence: first query, first key, first item, the
 // most splits of a tile, rows of a split, first part (of sequences with more than one split), full tiles, run.  The
-// first `full` tiles have all the splits; then, from run to run of tiles, one less (run 0: every tile has them all).
+// first `full` tiles have all the splits; of the others every run of tiles has one less than the one before, the first
+// as many, or (run < 0) each has -run.
 constexpr int kMassSeqWords = 8;
 constexpr int kMassRowTile = 128;  // splits are whole numbers of so many rows
 constexpr int kMassKeys = 128;     // of a tile; bf16: or twice as many

@@ -93,10 +93,11 @@ __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
   p.part = (int64_t)h * a.parts + seq_word(a.seq, w + 5) + i;
   const int full = seq_word(a.seq, w + 6), run = seq_word(a.seq, w + 7);
   int tile0 = 0, left = i;  // where tiles of p.splits splits begin, and the place among their items
-  if (run > 0 && left >= full * p.splits) {
+  if (left >= full * p.splits) {
     left -= full * p.splits;
     tile0 = full;
-    while (p.splits > 1 && left >= run * p.splits) {
+    if (run < 0) p.splits = -run;
+    while (run > 0 && p.splits > 1 && left >= run * p.splits) {
       left -= run * p.splits;
       tile0 += run;
       --p.splits;
