@@ -1067,6 +1067,14 @@ def _own_place(out, shape, dtype, dev, name: str):
     return out
 
 
+def _rising_by_32(cu) -> bool:
+    """Whether offsets never decrease and are multiples of 32 (few of them: without numpy's cost a call)."""
+    if cu.size > 16:
+        return not ((cu[1:] < cu[:-1]).any() or (cu & 31).any())
+    at = cu.tolist()
+    return all(x <= y for x, y in zip(at, at[1:])) and not any(x & 31 for x in at)
+
+
 class Cache8:
     """A cache held in 8 bits, a scale for 32 rows of a head (layout in include/twinkv.h): sequence s has the rows
     [cu_rows[s], cu_rows[s + 1]) of every head, a multiple of 32.  Takes the four arrays as they are;
@@ -1076,7 +1084,7 @@ class Cache8:
     def __init__(self, k_codes, k_scales, v_codes, v_scales, cu_rows):
         torch = _torch()
         cu = np.array(cu_rows, dtype=np.int64)
-        if cu.ndim != 1 or cu.size < 2 or cu[0] != 0 or (cu[1:] < cu[:-1]).any() or (cu & 31).any():
+        if cu.ndim != 1 or cu.size < 2 or cu[0] != 0 or not _rising_by_32(cu):
             raise ValueError("cu_rows must start at 0, never decrease, and be multiples of 32")
         if k_codes.dim() != 3:
             raise ValueError("k_codes must be (n_heads, C, d)")
@@ -1155,8 +1163,8 @@ def cache8_append(keys, values, cache: Cache8, length, cu_new=None, *, len_out=N
     dev = cache.device
     cu = cache._offsets(cu_new, keys.shape[1], "cu_new")
     n_in = cache._lens(length, "length")
-    len_out = _own_place(len_out, (cache.n_heads, cache.n_seqs), torch.int32, dev, "len_out")
-    status = torch.empty((cache.n_heads, cache.n_seqs), dtype=torch.int32, device=dev)
+    len_out = torch.empty_like(n_in) if len_out is None else _own_place(len_out, n_in.shape, torch.int32, dev, "len_out")
+    status = torch.empty_like(n_in)
     ws, wp, wn = _cache8_scratch(workspace, cache)
     _launch(dev, "twinkv_cache8_append", keys.data_ptr(), values.data_ptr(), dt, cu, keys.stride(0), keys.stride(1),
             values.stride(0), values.stride(1), cache._handle, n_in.data_ptr(), len_out.data_ptr(),
