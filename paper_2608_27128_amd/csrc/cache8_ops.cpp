@@ -11,14 +11,16 @@ namespace {
 // A sequence's key tiles, and the splits of the rows that see one (kMassSeqWords).
 struct MassSeq {
   int64_t tiles = 0, splits = 1, rows = 0;
-  int64_t full = 0, run = 0;
+  int64_t full = 0;
+  MassShape shape = kMassRest;
+  int64_t by = 1;
   int64_t items = 0;
 };
 struct MassPlan {
   int64_t keys = 0;        // of a tile
   int64_t most_rows = 0;   // of a split
-  int64_t items = 0, parts = 0;
-  bool few = false;
+  int64_t items = 0;
+  bool split = false, few = false;
 };
 
 // The most rows that see a key of one tile.  `cached`: how many keys there are is known on the device only.
@@ -39,17 +41,28 @@ MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_si
   MassSeq m;
   const int64_t rows = rows_seeing(nq, nk, group, window, n_sink, p.keys, cached), tile_rows = p.keys * group;
   m.tiles = (nk + p.keys - 1) / p.keys;
-  if (!cached && window >= nk && nq > 0 && rows > 2 * std::max(p.most_rows, tile_rows)) {
+  if (!cached && window >= nk && nq > 0 && rows > p.most_rows) {
     // Causal: tile by tile the rows that see one get fewer by tile_rows, once the tile lies behind the first query.
-    // Splits of a whole number of them make a run of tiles after which there is one split less, and no item is empty.
-    m.run = std::max<int64_t>(1, p.most_rows / tile_rows);
-    m.rows = m.run * tile_rows;
+    // Splits of a whole number of them, or whole parts of them, and tiles of ever fewer splits: no item is empty.
     m.full = std::min(m.tiles, std::max<int64_t>(nk - nq, 0) / p.keys + 1);
+    int64_t run = 1, drop = 1;
+    if (p.most_rows >= tile_rows) {
+      run = p.most_rows / tile_rows;
+      m.rows = run * tile_rows;
+      m.shape = kMassRuns;
+      m.by = run;
+    } else {
+      drop = tile_rows / p.most_rows;
+      while (tile_rows % (drop * kMassRowTile) != 0) --drop;
+      m.rows = tile_rows / drop;
+      m.shape = kMassDrops;
+      m.by = drop;
+    }
     m.splits = (rows + m.rows - 1) / m.rows;
     m.items = m.full * m.splits;
     int64_t splits = m.splits;
-    for (int64_t t = m.full; t < m.tiles; t += m.run, splits = std::max<int64_t>(1, splits - 1))
-      m.items += std::min(m.run, m.tiles - t) * splits;
+    for (int64_t t = m.full; t < m.tiles; t += run, splits -= splits > drop ? drop : 0)
+      m.items += std::min(run, m.tiles - t) * splits;
     return m;
   }
   m.splits = std::max<int64_t>(1, (rows + p.most_rows - 1) / p.most_rows);
@@ -59,7 +72,7 @@ MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_si
   // tiles with sinks are seen by all queries, the others by those of a window
   m.full = cached || n_sink == 0 ? m.tiles : std::min(m.tiles, (n_sink + p.keys - 1) / p.keys);
   const int64_t rest = std::max<int64_t>(1, (rows_seeing(nq, nk, group, window, 0, p.keys, cached) + m.rows - 1) / m.rows);
-  m.run = -rest;
+  m.by = rest;
   m.items = m.full * m.splits + (m.tiles - m.full) * rest;
   return m;
 }
@@ -86,7 +99,7 @@ int mass_plan(int dtype, int n_heads, int group, int n_seqs, const int64_t* cu_q
   for (int s = 0; s < n_seqs; ++s) {
     const MassSeq m = mass_seq(cu_q[s + 1] - cu_q[s], cu_k[s + 1] - cu_k[s], group, window, n_sink, cached, p);
     p.items += m.items;
-    if (m.splits > 1) p.parts += m.items;
+    if (m.splits > 1) p.split = true;
   }
   return grid_ok(p.items * n_heads, 256) && p.items <= INT32_MAX ? TWINKV_OK : TWINKV_E_ARG;
 }
@@ -97,7 +110,7 @@ struct MassLayout {
 MassLayout mass_layout(const MassPlan& p, int n_heads, int n_seqs) {
   MassLayout L;
   L.part = words_bytes(n_seqs, kMassSeqWords);
-  const size_t end = align_up(L.part + 4 * (size_t)n_heads * (size_t)p.parts * (size_t)p.keys);
+  const size_t end = align_up(L.part + (p.split ? 4 * (size_t)n_heads * (size_t)p.items * (size_t)p.keys : 0));
   L.total = end > 0 ? end + kAlign : 0;
   return L;
 }
@@ -135,12 +148,11 @@ int mass_args(int dtype, const void* q, int n_heads, int group, int n_seqs, cons
   a.group = group;
   a.n_seqs = n_seqs;
   a.items = (int)p.items;
-  a.parts = (int)p.parts;
   a.keys = (int)p.keys;
   a.few = p.few;
-  a.part = reinterpret_cast<float*>(ws + L.part);
+  a.part = p.split ? reinterpret_cast<float*>(ws + L.part) : nullptr;
   WordWriter w(a.seq, ((int64_t)n_seqs + 1) * kMassSeqWords, ws, stream);
-  int64_t item = 0, part = 0;
+  int64_t item = 0;
   for (int s = 0; s <= n_seqs; ++s) {
     MassSeq m;
     if (s < n_seqs) m = mass_seq(cu_q[s + 1] - cu_q[s], cu_k[s + 1] - cu_k[s], group, window, n_sink, cached, p);
@@ -149,11 +161,9 @@ int mass_args(int dtype, const void* q, int n_heads, int group, int n_seqs, cons
     w.put((int32_t)item);
     w.put((int32_t)m.splits);
     w.put((int32_t)std::min<int64_t>(m.rows, INT32_MAX));
-    w.put((int32_t)part);
     w.put((int32_t)m.full);
-    w.put((int32_t)m.run);
+    w.put((int32_t)m.shape << kMassShapeBits | (int32_t)m.by);
     item += m.items;
-    if (m.splits > 1) part += m.items;
   }
   return hip_status(w.finish());
 }
@@ -161,7 +171,7 @@ int mass_args(int dtype, const void* q, int n_heads, int group, int n_seqs, cons
 int run_mass(const MassArgs& a, int dtype, int d, void* stream) {
   if (a.items == 0) return TWINKV_OK;
   const int e = launch_mass(a, dtype, d, stream);
-  if (e != 0 || a.parts == 0) return hip_status(e);
+  if (e != 0 || a.part == nullptr) return hip_status(e);
   return hip_status(launch_mass_join(a, stream));
 }
 

@@ -152,10 +152,12 @@ int launch_evict8_move(const Evict8Args& a, int d, void* stream);
 
 // The weight that each key receives.  Rows are numbered as in the attention; an item is a tile of keys and a split of
 // the rows that see one of them, counted from the first.  Words per sequence: first query, first key, first item, the
-// most splits of a tile, rows of a split, first part (of sequences with more than one split), full tiles, run.  The
-// first `full` tiles have all the splits; of the others every run of tiles has one less than the one before, the first
-// as many, or (run < 0) each has -run.
-constexpr int kMassSeqWords = 8;
+// most splits of a tile, rows of a split, full tiles, shape.  The first `full` tiles have all the splits; the others,
+// by the shape's upper bits: every run of so many tiles one less than the one before, the first as many; every tile so
+// many less than the one before, the first as many; each tile so many.
+constexpr int kMassSeqWords = 7;
+enum MassShape { kMassRuns, kMassDrops, kMassRest };
+constexpr int kMassShapeBits = 28;
 constexpr int kMassRowTile = 128;  // splits are whole numbers of so many rows
 constexpr int kMassKeys = 128;     // of a tile; bf16: or twice as many
 struct MassArgs {
@@ -172,10 +174,10 @@ struct MassArgs {
   float scale_log2;
   int window, n_sink;      // at most kAttnMaxKeys each
   int n_heads, group, n_seqs;
-  int items, parts;        // per head
+  int items;               // per head
   int keys;                // of a tile
   bool few;                // rows see a tile (bf16)
-  float* part;             // [n_heads][parts][keys]
+  float* part;             // nullable [n_heads][items][keys], where a tile has more than one split
 };
 int launch_mass(const MassArgs& a, int dtype, int d, void* stream);
 int launch_mass_join(const MassArgs& a, void* stream);

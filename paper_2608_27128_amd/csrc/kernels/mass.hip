@@ -90,17 +90,22 @@ __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
   const int i = item - seq_word(a.seq, w + 2);
   p.splits = seq_word(a.seq, w + 3);
   p.rows = seq_word(a.seq, w + 4);
-  p.part = (int64_t)h * a.parts + seq_word(a.seq, w + 5) + i;
-  const int full = seq_word(a.seq, w + 6), run = seq_word(a.seq, w + 7);
+  p.part = (int64_t)h * a.items + item;
+  const int full = seq_word(a.seq, w + 5), shape = seq_word(a.seq, w + 6);
+  const int kind = shape >> kMassShapeBits, by = shape & ((1 << kMassShapeBits) - 1);
   int tile0 = 0, left = i;  // where tiles of p.splits splits begin, and the place among their items
   if (left >= full * p.splits) {
     left -= full * p.splits;
     tile0 = full;
-    if (run < 0) p.splits = -run;
-    while (run > 0 && p.splits > 1 && left >= run * p.splits) {
-      left -= run * p.splits;
-      tile0 += run;
-      --p.splits;
+    if (kind == kMassRest) {
+      p.splits = by;
+    } else {
+      const int run = kind == kMassRuns ? by : 1, drop = kind == kMassRuns ? 1 : by;
+      while (p.splits > drop && left >= run * p.splits) {
+        left -= run * p.splits;
+        tile0 += run;
+        p.splits -= drop;
+      }
     }
   }
   p.kt = tile0 + left / p.splits;

@@ -28,7 +28,7 @@
 namespace {
 using namespace twinkv;
 
-int64_t g_mass = 0, g_joins = 0, g_far = 0, g_runs = 0, g_rest = 0, g_scores = 0, g_fresh = 0, g_split_scores = 0;
+int64_t g_mass = 0, g_joins = 0, g_far = 0, g_runs = 0, g_drops = 0, g_rest = 0, g_scores = 0, g_fresh = 0, g_split_scores = 0;
 volatile unsigned char g_sink = 0;
 std::vector<int64_t> g_cu_q, g_cu_k, g_cu_to, g_budget;
 bool g_cached = false, g_want = false;
@@ -67,16 +67,17 @@ int launch_mass(const MassArgs& a, int dtype, int, void*) {
   CHECK(a.keys == (dtype == TWINKV_F32 ? kMassKeys : 2 * kMassKeys));
   CHECK((a.k == nullptr) == g_cached);
   CHECK((int64_t)a.items * a.n_heads * 256 <= (int64_t)UINT32_MAX);
-  int64_t item = 0, part = 0;
+  int64_t item = 0;
+  bool split_any = false;
   for (int s = 0; s < a.n_seqs; ++s) {
     const int64_t w = (int64_t)s * kMassSeqWords;
     const int64_t nq = g_cu_q[s + 1] - g_cu_q[s], nk = g_cu_k[s + 1] - g_cu_k[s], tiles = (nk + a.keys - 1) / a.keys;
     CHECK(word(a.seq, w) == g_cu_q[s] && word(a.seq, w + 1) == g_cu_k[s] && word(a.seq, w + 2) == item);
-    const int64_t most = word(a.seq, w + 3), rows = word(a.seq, w + 4), full = word(a.seq, w + 6), run = word(a.seq, w + 7);
-    CHECK(most >= 1 && rows >= 1 && rows % kMassRowTile == 0);
-    CHECK(most == 1 || word(a.seq, w + 5) == part);
-    if (run > 0 && full < tiles) ++g_runs;
-    if (run < 0 && full < tiles && -run < most) ++g_rest;
+    const int64_t most = word(a.seq, w + 3), rows = word(a.seq, w + 4), full = word(a.seq, w + 5);
+    const int shape = word(a.seq, w + 6), kind = shape >> kMassShapeBits, by = shape & ((1 << kMassShapeBits) - 1);
+    CHECK(most >= 1 && rows >= 1 && rows % kMassRowTile == 0 && by >= 1);
+    split_any |= most > 1;
+    if (full < tiles) ++(kind == kMassRuns ? g_runs : kind == kMassDrops ? g_drops : g_rest);
     const int64_t next = word(a.seq, w + kMassSeqWords + 2);
     // as the kernel takes an item apart
     int64_t tile = 0, split = 0;
@@ -85,11 +86,15 @@ int launch_mass(const MassArgs& a, int dtype, int, void*) {
       if (left >= full * splits) {
         left -= full * splits;
         tile0 = full;
-        if (run < 0) splits = -run;
-        while (run > 0 && splits > 1 && left >= run * splits) {
-          left -= run * splits;
-          tile0 += run;
-          --splits;
+        if (kind == kMassRest) {
+          splits = by;
+        } else {
+          const int64_t run = kind == kMassRuns ? by : 1, drop = kind == kMassRuns ? 1 : by;
+          while (splits > drop && left >= run * splits) {
+            left -= run * splits;
+            tile0 += run;
+            splits -= drop;
+          }
         }
       }
       CHECK(tile0 + left / splits == tile && left % splits == split);
@@ -101,16 +106,15 @@ int launch_mass(const MassArgs& a, int dtype, int, void*) {
       if (++split == splits) split = 0, ++tile;
     }
     CHECK(split == 0 && tile == tiles);
-    if (most > 1) part += next - item;
     item = next;
   }
-  CHECK(a.items == item && a.parts == part);
-  touch(a.part, part * a.n_heads * a.keys * 4);
+  CHECK(a.items == item && (a.part != nullptr) == split_any);
+  if (split_any) touch(a.part, item * a.n_heads * a.keys * 4);
   if (g_cached) touch(a.lse, 4 * a.Tq * a.n_heads * a.group);
   return 0;
 }
 int launch_mass_join(const MassArgs& a, void*) {
-  CHECK(a.parts > 0);
+  CHECK(a.part != nullptr);
   ++g_joins;
   return 0;
 }
@@ -268,7 +272,7 @@ int main() {
     CHECK(twinkv_cache8_evict(&c, len, fakef, nullptr, g_budget.data(), (int)upto(10), INT32_MAX, &to, len, fakef, len, w, nc,
                               nullptr) == TWINKV_OK);
   }
-  CHECK(g_mass > 1200 && g_joins > 200 && g_far > 40 && g_runs > 40 && g_rest > 8);
+  CHECK(g_mass > 1200 && g_joins > 200 && g_far > 40 && g_runs > 40 && g_drops > 20 && g_rest > 8);
   CHECK(g_scores > 80 && g_fresh > 80 && g_split_scores > 40);
   std::printf("cache8 ops ok: %lld weights, %lld joined, %lld runs, %lld with scores\n", (long long)g_mass,
               (long long)g_joins, (long long)g_runs, (long long)g_scores);
