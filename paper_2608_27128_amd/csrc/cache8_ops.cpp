@@ -34,6 +34,9 @@ int64_t rows_seeing(int64_t nq, int64_t nk, int group, int64_t window, int64_t n
 // least, whose products cover the way of the item's keys to the registers; of fewer where there would not be two for
 // every CU.
 constexpr int64_t kMassItems = 16384, kMassSlots = 512, kMassLeast = 1024;
+// Up to so many rounds of items a CU's slots are counted; an item's start takes about as long as so many steps.
+constexpr int64_t kMassRounds = 6;
+constexpr double kMassStart = 1.5;
 // Up to so many rows (bf16) the keys' way to the registers is what takes the time: fewer registers, more workgroups.
 constexpr int64_t kMassFew = 256;
 
@@ -77,7 +80,7 @@ MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_si
   return m;
 }
 
-int mass_plan(int dtype, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
+int mass_plan(int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
               int64_t n_sink, bool cached, MassPlan& p) {
   p.keys = dtype == TWINKV_BF16 ? 2 * kMassKeys : kMassKeys;
   double work = 0;  // rows times tiles
@@ -95,11 +98,31 @@ int mass_plan(int dtype, int n_heads, int group, int n_seqs, const int64_t* cu_q
   }
   p.few = longest <= kMassFew;
   const int64_t even = (int64_t)(work / kMassSlots);
-  p.most_rows = std::max((int64_t)(work / kMassItems), std::min(kMassLeast, std::max<int64_t>(even, kMassRowTile)));
-  for (int s = 0; s < n_seqs; ++s) {
-    const MassSeq m = mass_seq(cu_q[s + 1] - cu_q[s], cu_k[s + 1] - cu_k[s], group, window, n_sink, cached, p);
-    p.items += m.items;
-    if (m.splits > 1) p.split = true;
+  const int64_t base = std::max((int64_t)(work / kMassItems), std::min(kMassLeast, std::max<int64_t>(even, kMassRowTile)));
+  // Few rounds of items: the split whose rounds, of the items' steps and their start, take least.
+  const int64_t slots = kCus * (dtype == TWINKV_BF16 ? (p.few ? (d == 64 ? 4 : 3) : d == 64 ? 4 : 2) : d == 64 ? 4 : 2);
+  auto items_of = [&](int64_t most_rows, int64_t& rows) {
+    p.most_rows = most_rows;
+    p.items = rows = 0;
+    p.split = false;
+    for (int s = 0; s < n_seqs; ++s) {
+      const MassSeq m = mass_seq(cu_q[s + 1] - cu_q[s], cu_k[s + 1] - cu_k[s], group, window, n_sink, cached, p);
+      p.items += m.items;
+      p.split |= m.splits > 1;
+      rows = std::max(rows, m.rows);
+    }
+  };
+  int64_t rows, best = base;
+  items_of(base, rows);
+  if (p.split && p.items * n_heads < kMassRounds * slots) {
+    double least = 0;
+    for (const int64_t most_rows : {base, base / 2, 2 * base, 4 * base}) {
+      if (most_rows < kMassRowTile) continue;
+      items_of(most_rows, rows);
+      const double cost = (double)((p.items * n_heads + slots - 1) / slots) * ((double)rows / kMassRowTile + kMassStart);
+      if (least == 0 || cost < 0.95 * least) least = cost, best = most_rows;
+    }
+    items_of(best, rows);
   }
   return grid_ok(p.items * n_heads, 256) && p.items <= INT32_MAX ? TWINKV_OK : TWINKV_E_ARG;
 }
@@ -116,14 +139,14 @@ MassLayout mass_layout(const MassPlan& p, int n_heads, int n_seqs) {
 }
 
 // The rows' side of a call, the plan, the words and the parts.
-int mass_args(int dtype, const void* q, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k,
+int mass_args(int dtype, int d, const void* q, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k,
               int64_t q_head_stride, int64_t q_token_stride, int64_t window, int64_t n_sink, float scale, bool cached,
               const float* lse, const float* mass, float* mass_out, void* workspace, int64_t workspace_bytes,
               void* stream, MassArgs& a) {
   MassPlan p;
   window = std::min<int64_t>(window, kAttnMaxKeys);
   n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
-  const int rc = mass_plan(dtype, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, cached, p);
+  const int rc = mass_plan(dtype, d, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, cached, p);
   if (rc != TWINKV_OK) return rc;
   const MassLayout L = mass_layout(p, n_heads, n_seqs);
   if (L.total > 0 && (workspace == nullptr || workspace_bytes < (int64_t)L.total)) return TWINKV_E_WORKSPACE;
@@ -222,7 +245,7 @@ int attn8_layout(int dtype, int d, int n_heads, int group, int n_seqs, const int
     return TWINKV_OK;
   }
   MassPlan m;
-  rc = mass_plan(dtype, n_heads, group, n_seqs, cu_q, cu_rows, kAttnMaxKeys, 0, true, m);
+  rc = mass_plan(dtype, d, n_heads, group, n_seqs, cu_q, cu_rows, kAttnMaxKeys, 0, true, m);
   if (rc != TWINKV_OK) return rc;
   L.lse = align_up(4 * (size_t)n_heads * (size_t)group * (size_t)cu_q[n_seqs]) + kAlign;
   L.mass = mass_layout(m, n_heads, n_seqs).total;
@@ -255,7 +278,7 @@ int64_t twinkv_mass_workspace_bytes(int dtype, int d, int n_heads, int group, in
   if (rc == TWINKV_OK && (window < 0 || n_sink < 0)) rc = TWINKV_E_ARG;
   if (rc != TWINKV_OK) return -rc;
   MassPlan p;
-  rc = mass_plan(dtype, n_heads, group, n_seqs, cu_q, cu_k, std::min<int64_t>(window, kAttnMaxKeys),
+  rc = mass_plan(dtype, d, n_heads, group, n_seqs, cu_q, cu_k, std::min<int64_t>(window, kAttnMaxKeys),
                  std::min<int64_t>(n_sink, kAttnMaxKeys), false, p);
   return rc != TWINKV_OK ? -rc : (int64_t)mass_layout(p, n_heads, n_seqs).total;
 }
@@ -278,7 +301,7 @@ int twinkv_attention_mass(const void* q, const void* k, int dtype, int d, int n_
   if ((lse == nullptr && !no_q) || (mass_out == nullptr && !no_k)) return TWINKV_E_NULL;
   if (no_k) return TWINKV_OK;
   MassArgs a;
-  rc = mass_args(dtype, q, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride, window, n_sink, scale, false,
+  rc = mass_args(dtype, d, q, n_heads, group, n_seqs, cu_q, cu_k, q_head_stride, q_token_stride, window, n_sink, scale, false,
                  lse, mass, mass_out, workspace, workspace_bytes, stream, a);
   if (rc != TWINKV_OK) return rc;
   const int64_t esz = dtype == TWINKV_F32 ? 4 : 2;
@@ -426,7 +449,7 @@ int twinkv_cache8_attention(const void* q, int dtype, int group, const int64_t* 
   }
   if (!want_mass || L.scores) return TWINKV_OK;
   MassArgs a;
-  rc = mass_args(dtype, q, n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride, INT64_MAX, 0, scale,
+  rc = mass_args(dtype, d, q, n_heads, group, n_seqs, cu_q, cache->cu_rows, q_head_stride, q_token_stride, INT64_MAX, 0, scale,
                  true, lse, mass, mass_out, ws + L.attn + L.lse, (int64_t)L.mass, stream, a);
   if (rc != TWINKV_OK) return rc;
   a.cache = device_cache(cache);

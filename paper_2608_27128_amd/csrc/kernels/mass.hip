@@ -123,13 +123,11 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
   typedef typename Own::Row Row;
   constexpr int kWaveKeys = 32 * Own::kBlocks, kTileKeys = 4 * kWaveKeys, kTileRows = 32 * Own::kRowBlocks;
   constexpr int kRowBytes = D * (int)sizeof(T), kPieces = kRowBytes / 16, kAtOnce = kThreads / kPieces;
-  constexpr int kCopies = kTileRows / kAtOnce, kStats = 3;
+  constexpr int kCopies = kTileRows / kAtOnce;
   // Two objects, so that the compiler sees that reading one need not wait for the loads into the other.
   __shared__ __attribute__((aligned(16))) char s_even[kTileRows * kRowBytes];
   __shared__ __attribute__((aligned(16))) char s_odd[kMode == kFew ? 16 : kTileRows * kRowBytes];
-  // (of three steps: a block's epilogue runs beside the next block's products, which may be the next step's)
-  __shared__ __attribute__((aligned(16))) float s_lse[kStats][kTileRows];  // in log2 units
-  __shared__ __attribute__((aligned(16))) int s_pos[kStats][kTileRows];    // of the rows' queries; below 0: no row
+  __shared__ __attribute__((aligned(16))) float s_lse[2][kTileRows];  // in log2 units
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = (int)(blockIdx.x % (unsigned)a.n_heads);
@@ -198,7 +196,6 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
     from = q_head0 + sub * a.q_head + (int64_t)query * a.q_token;
   }
   float next_lse = 0.0f;
-  int next_pos = -1;
   auto bring = [&](auto F, int r0) {
     char* to = (F == 0 ? s_even : s_odd) + wave * 1024;
     if (even && r0 + kTileRows <= n_rows) {
@@ -217,23 +214,22 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
       }
     }
     if (tid < kTileRows) {
-      next_pos = -1;
       next_lse = 0.0f;
       if (r0 + tid < row1) {
         int sub;
         const int query = query_of(r0 + tid, sub);
-        next_pos = offset + query;
         next_lse = a.lse[((int64_t)h * a.group + sub) * a.Tq + p.q0 + query];
       }
     }
   };
 
+  int r0 = row0;  // first row of the step
   float total[Own::kBlocks], run[Own::kBlocks];
 #pragma unroll
   for (int b = 0; b < Own::kBlocks; ++b) total[b] = run[b] = 0.0f;
   f32x16 acc[kMode == kFused ? 2 : 1][Own::kBlocks];  // the block at hand, and the one before it
   f32x4 l[kMode == kFused ? 2 : 1][4];                // their rows' log-sum-exps
-  int before = 0, stats_at = 0;   // that one: none, every row sees every key of the wave, or some do; its step's statistics
+  int before = 0, row_before = 0;  // that one: none, every row sees every key of the wave, or some do; its first row
   const int lane_row = col * kRowBytes;
   int place[Own::kSteps];
 #pragma unroll
@@ -241,26 +237,29 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
 
   const std::integral_constant<int, 0> zero;
   const std::integral_constant<int, 1> one;
-  // The weights of block `rb` of a step (statistics `at`).
-  auto weigh = [&](auto all, auto H, int at, int rb) {
+  // The rows of the item that see this lane's key of block b: from first[b] on, so many.
+  int first[Own::kBlocks];
+  unsigned many[Own::kBlocks];
+#pragma unroll
+  for (int b = 0; b < Own::kBlocks; ++b) {
+    const int64_t pos = wave_key + 32 * b + col, lo = (pos - offset) * a.group;
+    const int64_t end = pos >= n ? row0 : pos < a.n_sink ? row1 : min((int64_t)row1, lo + (int64_t)a.window * a.group);
+    first[b] = (int)min(max(lo, (int64_t)row0), (int64_t)row1);
+    many[b] = (unsigned)max(end - first[b], (int64_t)0);
+  }
+  auto seen = [&](int row, int b) { return (unsigned)(row - first[b]) < many[b]; };
+  // The weights of the block of rows from `row` on.
+  auto weigh = [&](auto all, auto H, int row) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {  // rows 8x + 4hi .. + 3 of the block
-      int pos[4];
-      if constexpr (!decltype(all)::value) __builtin_memcpy(pos, &s_pos[at][32 * rb + 8 * x + 4 * hi], 16);
 #pragma unroll
-      for (int b = 0; b < Own::kBlocks; ++b) {
-        const int j = wave_key + 32 * b + col;
+      for (int b = 0; b < Own::kBlocks; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[H][b][4 * x + e], scale[b], -l[H][x][e]));
-          if constexpr (decltype(all)::value) {
-            run[b] += w;
-          } else {
-            const bool seen = (j < n) & (j <= pos[e]) & ((pos[e] - j < a.window) | (j < a.n_sink));
-            run[b] += seen ? w : 0.0f;
-          }
+          const float arg = __builtin_fmaf(acc[H][b][4 * x + e], scale[b], -l[H][x][e]);
+          if constexpr (decltype(all)::value) run[b] += __builtin_amdgcn_exp2f(arg);
+          else run[b] += __builtin_amdgcn_exp2f(seen(row + 4 * hi + 8 * x + e, b) ? arg : kNegInf);
         }
-      }
     }
   };
   Row ahead[kAhead];               // the first pieces of the next block's rows
@@ -284,22 +283,22 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
       for (int b = 0; b < Own::kBlocks; ++b) own.product(j, b, q, acc[H][b]);
     }
   };
-  // Block `rb` of the step in buffer F: its products, and the weights of the block before.
-  auto block = [&](auto H, auto F, auto RB, int now, int state) {
-    if constexpr (kMode != kFused) {
-      if (state == 0) return;
-      multiply(zero, (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes);
-      bring_stats(zero, now, RB);
-      if (state == 1) weigh(std::true_type(), zero, now, RB);
-      else weigh(std::false_type(), zero, now, RB);
-    } else {
-    constexpr int kBefore = (RB + Own::kRowBlocks - 1) % Own::kRowBlocks;  // that block's place in its step
+  // Block `rb` of the step in buffer F by itself.
+  auto block_apart = [&](auto F, auto RB, int state) {
+    if (state == 0) return;
+    multiply(zero, (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes);
+    bring_stats(zero, F, RB);
+    if (state == 1) weigh(std::true_type(), zero, r0 + 32 * RB);
+    else weigh(std::false_type(), zero, r0 + 32 * RB);
+  };
+  // Its products, and the weights of the block before.
+  auto block_fused = [&](auto H, auto F, auto RB, int state) {
     std::integral_constant<int, 1 - H> other;
     const char* rows = (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes;
-    if (sizeof(T) == 2 && before == 1 && state != 0) {
-      // The epilogue of the block before goes between the products, two elements (d 64: four) to each, its three
-      // steps on three elements' pairs at a time.  (The products of a whole block, then the weights, take the sum of
-      // both times, whether or not other waves are there to use the other unit.)
+    // The epilogue of the block before goes between the products, two elements to each, its three steps on the elements
+    // of three products at a time.  (The products of a whole block, then the weights, take the sum of both times, whether
+    // or not other waves are there to use the other unit.)
+    auto together = [&](auto all) {
       constexpr int kProducts = Own::kSteps * Own::kBlocks, kEach = 16 * Own::kBlocks / kProducts;
       Row q[Own::kSteps];
 #pragma unroll
@@ -318,36 +317,42 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
             q[j + kAhead] = *reinterpret_cast<const Row*>(rows + place[j + kAhead]);
           own.product(j, i % Own::kBlocks, q[j], acc[H][i % Own::kBlocks]);
         }
-        if (i == kProducts - 3) bring_stats(H, now, RB);
+        if (i == kProducts - 3) bring_stats(H, F, RB);
         if (RB + 1 < Own::kRowBlocks && i == kProducts - 1) look_ahead(rows + 32 * kRowBytes);
 #pragma unroll
         for (int x = 0; x < kEach; ++x) {
-          const int e = i * kEach + x;  // element e / kBlocks of key block e % kBlocks
+          const int e = (i * kEach + x) / Own::kBlocks, b = (i * kEach + x) % Own::kBlocks;  // element e of key block b
           if (i >= 2) run[x % Own::kBlocks] += w[i & 1][x];
           if (i >= 1 && i <= kProducts) w[(i - 1) & 1][x] = __builtin_amdgcn_exp2f(arg[(i - 1) & 1][x]);
-          if (i < kProducts)
-            arg[i & 1][x] = __builtin_fmaf(acc[1 - H][e % Own::kBlocks][e / Own::kBlocks], scale[e % Own::kBlocks],
-                                           -l[1 - H][e / Own::kBlocks / 4][e / Own::kBlocks % 4]);
+          if (i < kProducts) {
+            arg[i & 1][x] = __builtin_fmaf(acc[1 - H][b][e], scale[b], -l[1 - H][e / 4][e % 4]);
+            if constexpr (!decltype(all)::value) arg[i & 1][x] = seen(row_before + 4 * hi + e / 4 * 8 + e % 4, b) ? arg[i & 1][x] : kNegInf;
+          }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
+    };
+    if (state != 0 && before == 1) {
+      together(std::true_type());
     } else {
-      if (before == 1) weigh(std::true_type(), other, stats_at, kBefore);
-      if (before == 2) weigh(std::false_type(), other, stats_at, kBefore);
+      if (before == 1) weigh(std::true_type(), other, row_before);
+      if (before == 2) weigh(std::false_type(), other, row_before);
       if (state != 0) multiply(H, rows);
-      bring_stats(H, now, RB);
+      bring_stats(H, F, RB);
       if constexpr (RB + 1 < Own::kRowBlocks) look_ahead(rows + 32 * kRowBytes);
     }
     before = state;
-    stats_at = now;
-    }
+    row_before = r0 + 32 * RB;
   };
-  int r0 = row0, now = 0, flush = 0;
+  auto block = [&](auto H, auto F, auto RB, int state) {
+    if constexpr (kMode == kFused) block_fused(H, F, RB, state);
+    else block_apart(F, RB, state);
+  };
+  int flush = 0;
   auto step = [&](auto F) {
     if (tid < kTileRows) {
       // a row that sees nothing has weight nowhere
-      s_lse[now][tid] = next_lse == kNegInf ? -kNegInf : next_lse * 1.44269504088896340736f;
-      s_pos[now][tid] = next_pos;
+      s_lse[F][tid] = next_lse == kNegInf ? -kNegInf : next_lse * 1.44269504088896340736f;
     }
     // this step's rows lie in LDS (the barrier alone does not wait for a wave's loads to LDS), and nobody reads the
     // other buffer
@@ -361,14 +366,13 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
       return first >= all0 && first + 32 <= all1 ? 1 : 2;
     };
     if constexpr (kMode == kFused) look_ahead(F == 0 ? s_even : s_odd);
-    block(zero, F, std::integral_constant<int, 0>(), now, state_of(0));
-    block(one, F, std::integral_constant<int, 1>(), now, state_of(1));
+    block(zero, F, std::integral_constant<int, 0>(), state_of(0));
+    block(one, F, std::integral_constant<int, 1>(), state_of(1));
     if constexpr (Own::kRowBlocks == 4) {
-      block(zero, F, std::integral_constant<int, 2>(), now, state_of(2));
-      block(one, F, std::integral_constant<int, 3>(), now, state_of(3));
+      block(zero, F, std::integral_constant<int, 2>(), state_of(2));
+      block(one, F, std::integral_constant<int, 3>(), state_of(3));
     }
     r0 += kTileRows;
-    now = now == kStats - 1 ? 0 : now + 1;
   };
   if (row0 < row1) bring(zero, row0);
   while (r0 < row1) {
@@ -389,8 +393,8 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
     }
   }
   if constexpr (kMode == kFused) {
-    if (before == 1) weigh(std::true_type(), one, stats_at, Own::kRowBlocks - 1);
-    if (before == 2) weigh(std::false_type(), one, stats_at, Own::kRowBlocks - 1);
+    if (before == 1) weigh(std::true_type(), one, row_before);
+    if (before == 2) weigh(std::false_type(), one, row_before);
   }
 #pragma unroll
   for (int b = 0; b < Own::kBlocks; ++b) {
