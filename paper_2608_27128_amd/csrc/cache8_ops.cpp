@@ -30,14 +30,20 @@ int64_t rows_seeing(int64_t nq, int64_t nk, int group, int64_t window, int64_t n
   return (n_sink > 0 ? seen : std::min(seen, window + keys - 1)) * group;
 }
 
-// Items of equal work, many to a CU so that the last ones to end leave little of the machine idle, but of 1024 rows at
-// least, whose products cover the way of the item's keys to the registers; of fewer where there would not be two for
-// every CU.
-constexpr int64_t kMassItems = 16384, kMassSlots = 512, kMassLeast = 1024;
-// Up to so many rounds of items a CU's slots are counted; an item's start takes about as long as so many steps.
-constexpr int64_t kMassRounds = 6;
-constexpr double kMassStart = 1.5;
-// Up to so many rows (bf16) the keys' way to the registers is what takes the time: fewer registers, more workgroups.
+// Items of equal work, many to a CU so that the last ones to end leave little of the machine idle (16384: a window of
+// 9460 in 9828 tokens of d 64 282 us, with 2048 items 306), but of 1024 rows at least, whose products cover the way of
+// the item's keys to the registers (a prompt of 8192 tokens, d 64: 190 us, with 256 rows 238, with 4096 200); of fewer
+// where there would not be two for every CU.
+constexpr int64_t kMassItems = 16384, kMassSlots = 2 * kCus, kMassLeast = 1024;
+// Up to so many items for each CU, these are counted for splits of half to four times that size, and the split is taken
+// whose fullest CU has least to do; an item's start takes as long as 0.7 of a step of kMassRowTile rows, and an item alone
+// on its CU 1.5 times as long as one of many.  (Sequences of 244 and 2061 tokens, 8 query heads a head: 66 us, without the
+// count 78.)
+constexpr int64_t kMassCounted = 16;
+constexpr double kMassStart = 0.7, kMassAlone = 1.5;
+// Up to so many rows (bf16) the keys' way to the registers is what takes the time: one buffer of rows and no look-ahead,
+// for more workgroups a CU.  (64 sequences of 1024 to 4096 keys, d 128: the last 32 queries of 4 heads 88 us for 103, the
+// last one 74 for 90.)
 constexpr int64_t kMassFew = 256;
 
 MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_sink, bool cached, const MassPlan& p) {
@@ -80,7 +86,7 @@ MassSeq mass_seq(int64_t nq, int64_t nk, int group, int64_t window, int64_t n_si
   return m;
 }
 
-int mass_plan(int dtype, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
+int mass_plan(int dtype, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k, int64_t window,
               int64_t n_sink, bool cached, MassPlan& p) {
   p.keys = dtype == TWINKV_BF16 ? 2 * kMassKeys : kMassKeys;
   double work = 0;  // rows times tiles
@@ -99,8 +105,6 @@ int mass_plan(int dtype, int d, int n_heads, int group, int n_seqs, const int64_
   p.few = longest <= kMassFew;
   const int64_t even = (int64_t)(work / kMassSlots);
   const int64_t base = std::max((int64_t)(work / kMassItems), std::min(kMassLeast, std::max<int64_t>(even, kMassRowTile)));
-  // Few rounds of items: the split whose rounds, of the items' steps and their start, take least.
-  const int64_t slots = kCus * (dtype == TWINKV_BF16 ? (p.few ? (d == 64 ? 4 : 3) : d == 64 ? 4 : 2) : d == 64 ? 4 : 2);
   auto items_of = [&](int64_t most_rows, int64_t& rows) {
     p.most_rows = most_rows;
     p.items = rows = 0;
@@ -114,13 +118,17 @@ int mass_plan(int dtype, int d, int n_heads, int group, int n_seqs, const int64_
   };
   int64_t rows, best = base;
   items_of(base, rows);
-  if (p.split && p.items * n_heads < kMassRounds * slots) {
+  if (p.split && p.items * n_heads < kMassCounted * kCus) {
     double least = 0;
     for (const int64_t most_rows : {base, base / 2, 2 * base, 4 * base}) {
       if (most_rows < kMassRowTile) continue;
       items_of(most_rows, rows);
-      const double cost = (double)((p.items * n_heads + slots - 1) / slots) * ((double)rows / kMassRowTile + kMassStart);
-      if (least == 0 || cost < 0.95 * least) least = cost, best = most_rows;
+      const double fullest = std::max((double)((p.items * n_heads + kCus - 1) / kCus), kMassAlone);
+      const double cost = fullest * ((double)rows / kMassRowTile + kMassStart);
+      if (least == 0 || cost < 0.95 * least) {
+        least = cost;
+        best = most_rows;
+      }
     }
     items_of(best, rows);
   }
@@ -146,7 +154,7 @@ int mass_args(int dtype, int d, const void* q, int n_heads, int group, int n_seq
   MassPlan p;
   window = std::min<int64_t>(window, kAttnMaxKeys);
   n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
-  const int rc = mass_plan(dtype, d, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, cached, p);
+  const int rc = mass_plan(dtype, n_heads, group, n_seqs, cu_q, cu_k, window, n_sink, cached, p);
   if (rc != TWINKV_OK) return rc;
   const MassLayout L = mass_layout(p, n_heads, n_seqs);
   if (L.total > 0 && (workspace == nullptr || workspace_bytes < (int64_t)L.total)) return TWINKV_E_WORKSPACE;
@@ -245,7 +253,7 @@ int attn8_layout(int dtype, int d, int n_heads, int group, int n_seqs, const int
     return TWINKV_OK;
   }
   MassPlan m;
-  rc = mass_plan(dtype, d, n_heads, group, n_seqs, cu_q, cu_rows, kAttnMaxKeys, 0, true, m);
+  rc = mass_plan(dtype, n_heads, group, n_seqs, cu_q, cu_rows, kAttnMaxKeys, 0, true, m);
   if (rc != TWINKV_OK) return rc;
   L.lse = align_up(4 * (size_t)n_heads * (size_t)group * (size_t)cu_q[n_seqs]) + kAlign;
   L.mass = mass_layout(m, n_heads, n_seqs).total;
@@ -278,7 +286,7 @@ int64_t twinkv_mass_workspace_bytes(int dtype, int d, int n_heads, int group, in
   if (rc == TWINKV_OK && (window < 0 || n_sink < 0)) rc = TWINKV_E_ARG;
   if (rc != TWINKV_OK) return -rc;
   MassPlan p;
-  rc = mass_plan(dtype, d, n_heads, group, n_seqs, cu_q, cu_k, std::min<int64_t>(window, kAttnMaxKeys),
+  rc = mass_plan(dtype, n_heads, group, n_seqs, cu_q, cu_k, std::min<int64_t>(window, kAttnMaxKeys),
                  std::min<int64_t>(n_sink, kAttnMaxKeys), false, p);
   return rc != TWINKV_OK ? -rc : (int64_t)mass_layout(p, n_heads, n_seqs).total;
 }

@@ -7,10 +7,22 @@
 // head) that see them; rows come to LDS 16 bytes a lane without registers, into one of two buffers while the other
 // is read, and serve all four waves.  The products put a key in a lane and 16 rows in its registers, so a key's
 // weights are added up inside the lane.
-//  * bf16: v_mfma_f32_32x32x16_bf16, 64 keys a wave, 64 rows a step.
-//  * fp32: v_mfma_f32_32x32x2_f32, 32 keys a wave, 32 rows a step.
+//  * bf16: v_mfma_f32_32x32x16_bf16, 64 keys a wave, 128 rows a step.
+//  * fp32: v_mfma_f32_32x32x2_f32, 32 keys a wave, 64 rows a step.
 //  * keys in 8 bits: their codes become bf16 (fp32 for fp32 queries) once, as they are loaded; the block's scale goes
 //    into the multiply-add.
+// Which rows see a lane's key is one run of rows, so a mask is a subtraction and a comparison, and blocks that see all
+// of the wave's keys, or none, have none.
+//
+// What bounds it at length is the matrix unit and the vector unit by turns: they hardly overlap from wave to wave, and a
+// weight costs a multiply-add, an addition and an exponential of four times their price.  So, per block of 32 rows:
+//  * kFused (bf16, d 128): one block's weights go between the next block's products, in the same wave.  A prompt of 32768
+//    tokens (8 heads of 4): 4.2 ms, 1044 TFLOP/s; apart 4.5.  Two blocks' accumulators: 220 registers, 2 waves a SIMD.
+//  * kApart (bf16 of d 64, fp32): products, then weights.  With half the products to hide behind, twice the waves count for
+//    more: 8192 tokens of d 64 190 us, fused 217.
+//  * kFew (bf16, at most kMassFew rows a key): the keys' way to the registers is the work, so one buffer of rows, and more
+//    workgroups.  64 sequences of 1024 to 4096 keys, the last 32 queries: 88 us, 4.0 TB/s of keys and scales.
+//
 // Sums: 32 bits, in two levels, since one chain over 100000 rows loses 3 digits: a lane adds 16 steps' weights,
 // then their sum to the total.  Rows are split over workgroups where there are too few keys, and a second kernel
 // adds the parts in their order; nothing is added atomically.
@@ -117,8 +129,10 @@ __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
 
 // kMode: how a block's products and weights go together (see above).
 enum { kFused, kApart, kFew };
+template <typename T, int D, int kMode>
+constexpr int kMassWaves = kMode == kFused || (sizeof(T) == 4 && D == 128) ? 2 : kMode == kFew && D == 128 ? 3 : 4;  // a SIMD
 template <typename T, int D, int B, int kMode, bool kCodes>
-__global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D == 128) ? 2 : kMode == kFew && D == 128 ? 3 : 4) void mass_kernel(const MassArgs a) {
+__global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kernel(const MassArgs a) {
   typedef Keys<T, D, B> Own;
   typedef typename Own::Row Row;
   constexpr int kWaveKeys = 32 * Own::kBlocks, kTileKeys = 4 * kWaveKeys, kTileRows = 32 * Own::kRowBlocks;
@@ -167,10 +181,15 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
 
   // Of these rows some see some of the wave's keys, and in between all see all.
   const int far_key = wave_key + kWaveKeys - 1;
-  auto row_at = [&](int64_t pos) { return __builtin_amdgcn_readfirstlane((int)min(max((int64_t)query_at(pos) * a.group, (int64_t)row0), (int64_t)max(row0, row1))); };
-  const int some0 = row_at(wave_key), some1 = wave_key >= n ? row0 : wave_key < a.n_sink ? max(row0, row1) : row_at((int64_t)far_key + a.window);
-  const int all0 = far_key < n ? row_at(far_key) : max(row0, row1);
-  const int all1 = far_key < a.n_sink ? max(row0, row1) : row_at((int64_t)wave_key + a.window);
+  const int row_end = max(row0, row1);
+  auto row_at = [&](int64_t pos) {
+    const int64_t row = (int64_t)query_at(pos) * a.group;
+    return __builtin_amdgcn_readfirstlane((int)min(max(row, (int64_t)row0), (int64_t)row_end));
+  };
+  const int some0 = row_at(wave_key);
+  const int some1 = wave_key >= n ? row0 : wave_key < a.n_sink ? row_end : row_at((int64_t)far_key + a.window);
+  const int all0 = far_key < n ? row_at(far_key) : row_end;
+  const int all1 = far_key < a.n_sink ? row_end : row_at((int64_t)wave_key + a.window);
 
   // Rows to LDS.  Where whole runs of rows have the same query heads a thread's rows lie at fixed distances, and
   // move by a fixed one from step to step; otherwise, and in the last step, each row's place is worked out.
@@ -276,11 +295,16 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
     for (int b = 0; b < Own::kBlocks; ++b)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[H][b][e] = 0.0f;
+    constexpr int kFirst = kMode == kFused || D == 64 ? Own::kSteps : 1;  // rows' pieces on their way before the products
+    Row q[Own::kSteps];
+#pragma unroll
+    for (int j = 0; j < kFirst; ++j) q[j] = kMode == kFused && j < kAhead ? ahead[j] : *reinterpret_cast<const Row*>(rows + place[j]);
+    if (kFirst > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < Own::kSteps; ++j) {
-      const Row q = kMode == kFused && j < kAhead ? ahead[j] : *reinterpret_cast<const Row*>(rows + place[j]);
+      if (j >= kFirst) q[j] = *reinterpret_cast<const Row*>(rows + place[j]);
 #pragma unroll
-      for (int b = 0; b < Own::kBlocks; ++b) own.product(j, b, q, acc[H][b]);
+      for (int b = 0; b < Own::kBlocks; ++b) own.product(j, b, q[j], acc[H][b]);
     }
   };
   // Block `rb` of the step in buffer F by itself.
@@ -295,10 +319,9 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
   auto block_fused = [&](auto H, auto F, auto RB, int state) {
     std::integral_constant<int, 1 - H> other;
     const char* rows = (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes;
-    // The epilogue of the block before goes between the products, two elements to each, its three steps on the elements
-    // of three products at a time.  (The products of a whole block, then the weights, take the sum of both times, whether
-    // or not other waves are there to use the other unit.)
-    auto together = [&](auto all) {
+    // The weights of the block before go between the products, two elements to each, their three steps on the elements of
+    // three products at a time.
+    if (state != 0 && before == 1) {
       constexpr int kProducts = Own::kSteps * Own::kBlocks, kEach = 16 * Own::kBlocks / kProducts;
       Row q[Own::kSteps];
 #pragma unroll
@@ -324,16 +347,10 @@ __global__ __launch_bounds__(kThreads, kMode == kFused || (sizeof(T) == 4 && D =
           const int e = (i * kEach + x) / Own::kBlocks, b = (i * kEach + x) % Own::kBlocks;  // element e of key block b
           if (i >= 2) run[x % Own::kBlocks] += w[i & 1][x];
           if (i >= 1 && i <= kProducts) w[(i - 1) & 1][x] = __builtin_amdgcn_exp2f(arg[(i - 1) & 1][x]);
-          if (i < kProducts) {
-            arg[i & 1][x] = __builtin_fmaf(acc[1 - H][b][e], scale[b], -l[1 - H][e / 4][e % 4]);
-            if constexpr (!decltype(all)::value) arg[i & 1][x] = seen(row_before + 4 * hi + e / 4 * 8 + e % 4, b) ? arg[i & 1][x] : kNegInf;
-          }
+          if (i < kProducts) arg[i & 1][x] = __builtin_fmaf(acc[1 - H][b][e], scale[b], -l[1 - H][e / 4][e % 4]);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-    };
-    if (state != 0 && before == 1) {
-      together(std::true_type());
     } else {
       if (before == 1) weigh(std::true_type(), other, row_before);
       if (before == 2) weigh(std::false_type(), other, row_before);
