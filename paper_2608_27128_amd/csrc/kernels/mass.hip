@@ -179,17 +179,24 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     }
   }
 
-  // Of these rows some see some of the wave's keys, and in between all see all.
-  const int far_key = wave_key + kWaveKeys - 1;
+  // These rows see all of the wave's keys; of each block of 32 keys some rows from some0 to some1 see a key.
   const int row_end = max(row0, row1);
   auto row_at = [&](int64_t pos) {
     const int64_t row = (int64_t)query_at(pos) * a.group;
     return __builtin_amdgcn_readfirstlane((int)min(max(row, (int64_t)row0), (int64_t)row_end));
   };
-  const int some0 = row_at(wave_key);
-  const int some1 = wave_key >= n ? row0 : wave_key < a.n_sink ? row_end : row_at((int64_t)far_key + a.window);
+  const int far_key = wave_key + kWaveKeys - 1;
   const int all0 = far_key < n ? row_at(far_key) : row_end;
   const int all1 = far_key < a.n_sink ? row_end : row_at((int64_t)wave_key + a.window);
+  int some0[Own::kBlocks], some1[Own::kBlocks];
+#pragma unroll
+  for (int b = 0; b < Own::kBlocks; ++b) {
+    const int key = wave_key + 32 * b;
+    some0[b] = row_at(key);
+    some1[b] = key >= n ? row0 : key < a.n_sink ? row_end : row_at((int64_t)key + 31 + a.window);
+  }
+  auto all_see = [&](int row) { return row >= all0 && row + 32 <= all1; };           // of the 32 rows from `row` on
+  auto some_see = [&](int row, int b) { return row < some1[b] && row + 32 > some0[b]; };
 
   // Rows to LDS.  Where whole runs of rows have the same query heads a thread's rows lie at fixed distances, and
   // move by a fixed one from step to step; otherwise, and in the last step, each row's place is worked out.
@@ -248,7 +255,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
   for (int b = 0; b < Own::kBlocks; ++b) total[b] = run[b] = 0.0f;
   f32x16 acc[kMode == kFused ? 2 : 1][Own::kBlocks];  // the block at hand, and the one before it
   f32x4 l[kMode == kFused ? 2 : 1][4];                // their rows' log-sum-exps
-  int before = 0, row_before = 0;  // that one: none, every row sees every key of the wave, or some do; its first row
+  bool before = false;                // there is one, whose rows see all of the wave's keys
   const int lane_row = col * kRowBytes;
   int place[Own::kSteps];
 #pragma unroll
@@ -267,12 +274,12 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     many[b] = (unsigned)max(end - first[b], (int64_t)0);
   }
   auto seen = [&](int row, int b) { return (unsigned)(row - first[b]) < many[b]; };
-  // The weights of the block of rows from `row` on.
-  auto weigh = [&](auto all, auto H, int row) {
+  // The weights of the block of rows from `row` on, for key blocks B0 .. B1 - 1.
+  auto weigh = [&](auto all, auto H, auto B0, auto B1, int row) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {  // rows 8x + 4hi .. + 3 of the block
 #pragma unroll
-      for (int b = 0; b < Own::kBlocks; ++b)
+      for (int b = B0; b < B1; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float arg = __builtin_fmaf(acc[H][b][4 * x + e], scale[b], -l[H][x][e]);
@@ -290,9 +297,9 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
 #pragma unroll
     for (int x = 0; x < 4; ++x) l[H][x] = *reinterpret_cast<const f32x4*>(&s_lse[at][32 * rb + 8 * x + 4 * hi]);
   };
-  auto multiply = [&](auto H, const char* rows) {
+  auto multiply = [&](auto H, auto B0, auto B1, const char* rows) {
 #pragma unroll
-    for (int b = 0; b < Own::kBlocks; ++b)
+    for (int b = B0; b < B1; ++b)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[H][b][e] = 0.0f;
     constexpr int kFirst = kMode == kFused || D == 64 ? Own::kSteps : 1;  // rows' pieces on their way before the products
@@ -304,24 +311,40 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     for (int j = 0; j < Own::kSteps; ++j) {
       if (j >= kFirst) q[j] = *reinterpret_cast<const Row*>(rows + place[j]);
 #pragma unroll
-      for (int b = 0; b < Own::kBlocks; ++b) own.product(j, b, q[j], acc[H][b]);
+      for (int b = B0; b < B1; ++b) own.product(j, b, q[j], acc[H][b]);
     }
   };
-  // Block `rb` of the step in buffer F by itself.
-  auto block_apart = [&](auto F, auto RB, int state) {
-    if (state == 0) return;
-    multiply(zero, (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes);
-    bring_stats(zero, F, RB);
-    if (state == 1) weigh(std::true_type(), zero, r0 + 32 * RB);
-    else weigh(std::false_type(), zero, r0 + 32 * RB);
+  const std::integral_constant<int, Own::kBlocks> blocks;
+  // Block RB of the step in buffer F, where some rows do not see all: a block of keys after the other.
+  auto block_masked = [&](auto H, auto F, auto RB) {
+    const char* rows = (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes;
+    const int row = r0 + 32 * RB;
+    auto part = [&](auto B0, auto B1) {
+      if (!some_see(row, B0)) return;
+      multiply(H, B0, B1, rows);
+      weigh(std::false_type(), H, B0, B1, row);
+    };
+    part(zero, one);
+    if constexpr (Own::kBlocks == 2) part(one, blocks);
+  };
+  auto block_apart = [&](auto F, auto RB) {
+    if (all_see(r0 + 32 * RB)) {
+      multiply(zero, zero, blocks, (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes);
+      bring_stats(zero, F, RB);
+      weigh(std::true_type(), zero, zero, blocks, 0);
+    } else {
+      bring_stats(zero, F, RB);
+      block_masked(zero, F, RB);
+    }
   };
   // Its products, and the weights of the block before.
-  auto block_fused = [&](auto H, auto F, auto RB, int state) {
+  auto block_fused = [&](auto H, auto F, auto RB) {
+    const bool all = all_see(r0 + 32 * RB);
     std::integral_constant<int, 1 - H> other;
     const char* rows = (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes;
     // The weights of the block before go between the products, two elements to each, their three steps on the elements of
     // three products at a time.
-    if (state != 0 && before == 1) {
+    if (all && before) {
       constexpr int kProducts = Own::kSteps * Own::kBlocks, kEach = 16 * Own::kBlocks / kProducts;
       Row q[Own::kSteps];
 #pragma unroll
@@ -352,18 +375,17 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
       }
       __builtin_amdgcn_sched_barrier(0);
     } else {
-      if (before == 1) weigh(std::true_type(), other, row_before);
-      if (before == 2) weigh(std::false_type(), other, row_before);
-      if (state != 0) multiply(H, rows);
+      if (before) weigh(std::true_type(), other, zero, blocks, 0);
       bring_stats(H, F, RB);
+      if (all) multiply(H, zero, blocks, rows);
+      else block_masked(H, F, RB);
       if constexpr (RB + 1 < Own::kRowBlocks) look_ahead(rows + 32 * kRowBytes);
     }
-    before = state;
-    row_before = r0 + 32 * RB;
+    before = all;
   };
-  auto block = [&](auto H, auto F, auto RB, int state) {
-    if constexpr (kMode == kFused) block_fused(H, F, RB, state);
-    else block_apart(F, RB, state);
+  auto block = [&](auto H, auto F, auto RB) {
+    if constexpr (kMode == kFused) block_fused(H, F, RB);
+    else block_apart(F, RB);
   };
   int flush = 0;
   auto step = [&](auto F) {
@@ -376,18 +398,12 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     __builtin_amdgcn_s_waitcnt(kNoLoads);
     __syncthreads();
     if (kMode != kFew && r0 + kTileRows < row1) bring(std::integral_constant<int, 1 - F>(), r0 + kTileRows);
-    // what block rb's rows see of the wave's keys
-    auto state_of = [&](int rb) {
-      const int first = r0 + 32 * rb;
-      if (first >= some1 || first + 32 <= some0) return 0;
-      return first >= all0 && first + 32 <= all1 ? 1 : 2;
-    };
     if constexpr (kMode == kFused) look_ahead(F == 0 ? s_even : s_odd);
-    block(zero, F, std::integral_constant<int, 0>(), state_of(0));
-    block(one, F, std::integral_constant<int, 1>(), state_of(1));
+    block(zero, F, std::integral_constant<int, 0>());
+    block(one, F, std::integral_constant<int, 1>());
     if constexpr (Own::kRowBlocks == 4) {
-      block(zero, F, std::integral_constant<int, 2>(), state_of(2));
-      block(one, F, std::integral_constant<int, 3>(), state_of(3));
+      block(zero, F, std::integral_constant<int, 2>());
+      block(one, F, std::integral_constant<int, 3>());
     }
     r0 += kTileRows;
   };
@@ -410,8 +426,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     }
   }
   if constexpr (kMode == kFused) {
-    if (before == 1) weigh(std::true_type(), one, row_before);
-    if (before == 2) weigh(std::false_type(), one, row_before);
+    if (before) weigh(std::true_type(), one, zero, blocks, 0);
   }
 #pragma unroll
   for (int b = 0; b < Own::kBlocks; ++b) {
