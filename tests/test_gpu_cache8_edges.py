@@ -36,6 +36,21 @@ def test_attention_scores_that_fill_the_lds(rows, nq, G, dtype):
         assert not bool(got["mass"][h, n:].any())
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("sink", [1, 32, 33, 100, 300])
+def test_mass_of_sinks_past_the_window(sink, dtype, d):
+    """Sinks that many rows behind their window see: in one block of keys, in more, in all of a tile and the next; two
+    sequences, the second with fewer keys than sinks, and old weights."""
+    import torch
+    g = gen(1000 + sink)
+    H, G, W, cu = 2, 3, 100, [0, 1700, 1700 + 29]
+    q, k = randn(g, H * G, cu[-1], d, dtype=dtype), randn(g, H, cu[-1], d, dtype=dtype)
+    lse = lse_of(q, k, cu, cu, W, sink, d ** -0.5)
+    old = torch.rand((H, cu[-1]), generator=g, device="cuda")
+    got = binding.attention_mass(q, k, lse, W, sink, None, cu, cu, mass=old)["mass"]
+    check_mass(got, q, k, lse, cu, cu, lambda s, h, m, n: ref.seen_by(m, n, W, sink), d ** -0.5, old)
+
+
 def test_attention_more_queries_than_rows():
     """A problem with fewer rows than queries: the first queries see nothing, and neither do those of an empty one."""
     import torch
