@@ -6,6 +6,11 @@
 // order-reversing) comes from an MSB-first radix select; then the rows before the cut, and the first ones equal to
 // it, are listed in rising order, 8 a thread, one scan of both counts.  Problems of up to CAP rows keep their keys
 // in LDS, longer ones read their weights again in every pass.
+//
+// A chain of short steps that wait for each other bounds it (barriers, the scan of a histogram), not its 4 bytes a row.
+// So few threads for few rows, whose barriers and histograms (2^8 bins, 4 passes) cost less, and for more rows more
+// threads and 2^11 bins (3 passes).  8 problems of 300 / 2000 / 4001 / 9000 / 30000 rows: 7 / 10 / 12 / 19 / 32 us; 4608 of
+// 107 rows 19, with 256 threads 28; 4001 rows with 256 threads 16; 30000 whose keys are read again 50.
 #include <hip/hip_runtime.h>
 
 #include "../cache_ops.h"
@@ -20,7 +25,7 @@ constexpr int kRun = 8;  // rows a thread lists
 
 template <int NT, int CAP>
 __global__ __launch_bounds__(NT) void evict8_select_kernel(const Evict8Args a) {
-  constexpr int NW = NT / 64, DBITS = NT >= 1024 ? 11 : 8;
+  constexpr int NW = NT / 64, DBITS = NT >= 512 ? 11 : 8;
   __shared__ __attribute__((aligned(16))) uint32_t s_key[CAP > 0 ? CAP : 4];
   __shared__ int s_hist[2][1 << DBITS];
   __shared__ uint32_t s_bits[NW][2];
@@ -125,8 +130,11 @@ int run(const Evict8Args& a, hipStream_t s) {
 
 int launch_evict8_select(const Evict8Args& a, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  if (a.max_rows <= 4096) return run<256, 4096>(a, s);
+  if (a.max_rows <= 512) return run<128, 512>(a, s);
+  if (a.max_rows <= 2048) return run<256, 2048>(a, s);
+  if (a.max_rows <= 4096) return run<512, 4096>(a, s);
   if (a.max_rows <= 16384) return run<1024, 16384>(a, s);
+  if (a.max_rows <= 32768) return run<1024, 32768>(a, s);
   return run<1024, 0>(a, s);
 }
 

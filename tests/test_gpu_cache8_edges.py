@@ -51,6 +51,31 @@ def test_mass_of_sinks_past_the_window(sink, dtype, d):
     check_mass(got, q, k, lse, cu, cu, lambda s, h, m, n: ref.seen_by(m, n, W, sink), d ** -0.5, old)
 
 
+@pytest.mark.parametrize("rows", [31, 512, 513, 2048, 2049, 4096, 4097, 16385, 32768, 32769, 50000])
+def test_evict_selects_at_every_length(rows):
+    """Lengths at and around those where the selection takes another number of threads, or does not keep its keys: the
+    kept rows of two heads of their own lengths, weights with ties, and a problem beside them that has one row."""
+    import torch
+    g = gen(rows)
+    H, d, budget = 2, 64, [rows // 2 + 1, 1]
+    cache, to = binding.Cache8.empty(H, [rows, 1], d), binding.Cache8.empty(H, budget, d)
+    for c in (cache.k_codes, cache.v_codes):
+        c.zero_()
+    for c in (cache.k_scales, cache.v_scales):
+        c.fill_(127)
+    r0 = int(cache.cu_rows[1])
+    length = torch.tensor([[rows, 1], [rows - rows // 5, 0]], dtype=torch.int32, device="cuda")
+    mass = (torch.rand((H, int(cache.cu_rows[-1])), generator=g, device="cuda") * 3000).floor() / 64
+    got = binding.cache8_evict(cache, length, mass, budget, to, 4, 16)
+    for h in range(H):
+        n, m = int(length[h, 0]), int(got["len"][h, 0])
+        kept = ref8.kept_rows(mass[h, :n].tolist(), n, budget[0], 4, 16)
+        assert m == len(kept) and got["pos"][h, :m].tolist() == list(kept)
+        assert bool((got["pos"][h, m:int(to.cu_rows[1])] == -1).all())
+    assert got["len"][:, 1].tolist() == [1, 0]
+    assert got["mass"][:, int(to.cu_rows[1])].tolist() == [float(mass[0, r0]), 0.0]
+
+
 def test_attention_more_queries_than_rows():
     """A problem with fewer rows than queries: the first queries see nothing, and neither do those of an empty one."""
     import torch
