@@ -8,23 +8,25 @@
 // is read, and serve all four waves.  The products put a key in a lane and 16 rows in its registers, so a key's
 // weights are added up inside the lane.
 //  * bf16: v_mfma_f32_32x32x16_bf16, 64 keys a wave, 128 rows a step.
-//  * fp32: v_mfma_f32_32x32x2_f32, 32 keys a wave, 64 rows a step.
-//  * keys in 8 bits: their codes become bf16 (fp32 for fp32 queries) once, as they are loaded; the block's scale goes
-//    into the multiply-add.
+//  * fp32: a number is the sum of three bf16 (24 bits), a product the six of their products that reach 2^-24 of the
+//    largest: 6 x 32 cycles for 16 channels, where v_mfma_f32_32x32x2_f32 takes 512.  Rows pass through registers and are
+//    taken apart once for the four waves, 64 a step; 32 keys a wave.  A prompt of 4096 tokens (d 128, 8 heads of 4) 399 us,
+//    with the fp32 instruction 665.
+//  * keys in 8 bits: their codes become bf16, exactly, as they are loaded; the block's scale goes into the multiply-add.
 // Which rows see a lane's key is one run of rows, so a mask is a subtraction and a comparison, and blocks that see all
 // of the wave's keys, or none, have none.
 //
 // What bounds it at length is the matrix unit and the vector unit by turns: they hardly overlap from wave to wave, and a
-// weight costs a multiply-add, an addition and an exponential of four times their price.  So, per block of 32 rows:
+// weight costs a multiply-add, an addition and an exponential of twice their price.  So, per block of 32 rows:
 //  * kFused (bf16, d 128): one block's weights go between the next block's products, in the same wave.  A prompt of 32768
-//    tokens (8 heads of 4): 4.2 ms, 1044 TFLOP/s; apart 4.5.  Two blocks' accumulators: 220 registers, 2 waves a SIMD.
+//    tokens (8 heads of 4): 4.1 ms, 1070 TFLOP/s; apart 4.5.  Two blocks' accumulators: 233 registers, 2 waves a SIMD.
 //  * kApart (bf16 of d 64, fp32): products, then weights.  With half the products to hide behind, twice the waves count for
 //    more: 8192 tokens of d 64 190 us, fused 217.
 //  * kFew (bf16, at most kMassFew rows a key): the keys' way to the registers is the work, so one buffer of rows, and more
 //    workgroups.  64 sequences of 1024 to 4096 keys, the last 32 queries: 88 us, 4.0 TB/s of keys and scales.
 //
-// Sums: 32 bits, in two levels, since one chain over 100000 rows loses 3 digits: a lane adds 16 steps' weights,
-// then their sum to the total.  Rows are split over workgroups where there are too few keys, and a second kernel
+// Sums: 32 bits, in two levels, since one chain over 100000 rows loses 3 digits: a lane adds up to 16 steps'
+// weights, then their sum to the total.  Rows are split over workgroups where there are too few keys, and a second kernel
 // adds the parts in their order; nothing is added atomically.
 #include <hip/hip_runtime.h>
 
@@ -40,12 +42,12 @@ constexpr int kThreads = 256;
 constexpr int kFlush = 16;  // steps between additions to the total
 constexpr int kAhead = 3;   // steps of the contraction whose rows are on their way from LDS
 
-// A wave's keys, and the rows of a step.
-template <typename T, int D, int B>
+// A wave's keys, and the rows of a step.  P: bf16 parts of a key.
+template <typename T, int D, int B, int P>
 struct Keys;
 
-template <int D, int B>
-struct Keys<bf16, D, B> {
+template <int D, int B, int P>
+struct Keys<bf16, D, B, P> {
   static constexpr int kBlocks = B, kRowBlocks = 4, kSteps = D / 16;  // of 32 keys, of 32 rows, of 16 channels
   bf16x8 k[kBlocks][kSteps];
   __device__ void load(int b, const char* row, int hi) {
@@ -66,22 +68,37 @@ struct Keys<bf16, D, B> {
   }
 };
 
-template <int D>
-struct Keys<float, D, 1> {
-  static constexpr int kBlocks = 1, kRowBlocks = 2, kSteps = D / 8;
-  f32x4 k[kBlocks][kSteps];
-  __device__ void load(int b, const char* row, int hi) {
+template <int D, int P>
+struct Keys<float, D, 1, P> {
+  static constexpr int kBlocks = 1, kRowBlocks = 2, kSteps = D / 16;
+  bf16x8 k[kSteps][P];
+  __device__ void load(int, const char* row, int hi) {
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) k[b][j] = *reinterpret_cast<const f32x4*>(row + (2 * j + hi) * 16);
+    for (int j = 0; j < kSteps; ++j) {
+      const f32x4* at = reinterpret_cast<const f32x4*>(row) + (2 * j + hi) * 2;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = at[e / 4][e % 4];
+      split8(x, k[j]);
+    }
   }
-  __device__ void load_codes(int b, const uint8_t* row, int hi) {
+  __device__ void load_codes(int, const uint8_t* row, int hi) {
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) k[b][j] = codes4_f32(*reinterpret_cast<const unsigned*>(row + (2 * j + hi) * 4));
+    for (int j = 0; j < kSteps; ++j) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(row + (2 * j + hi) * 8);
+      k[j][0] = codes8_bf16(w[0], w[1]);
+    }
   }
-  typedef f32x4 Row;
-  __device__ void product(int j, int b, const Row& q, f32x16& acc) const {
+  // The parts' products, the smallest first: of 24 bits those from 2^-24 of the largest on.
+  struct Row {
+    bf16x8 part[3];
+  };
+  __device__ void product(int j, int, const Row& q, f32x16& acc) const {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(q[e], k[b][j][e], acc, 0, 0, 0);
+    for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+      for (int of_k = 0; of_k <= sum && of_k < P; ++of_k)
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q.part[sum - of_k], k[j][of_k], acc, 0, 0, 0);
   }
 };
 
@@ -130,17 +147,18 @@ __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
 // kMode: how a block's products and weights go together (see above).
 enum { kFused, kApart, kFew };
 template <typename T, int D, int kMode>
-constexpr int kMassWaves = kMode == kFused || (sizeof(T) == 4 && D == 128) ? 2 : kMode == kFew && D == 128 ? 3 : 4;  // a SIMD
+constexpr int kMassWaves = kMode == kFused || (sizeof(T) == 4 && D == 128) ? 2 : (kMode == kFew && D == 128) || sizeof(T) == 4 ? 3 : 4;  // a SIMD
 template <typename T, int D, int B, int kMode, bool kCodes>
 __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kernel(const MassArgs a) {
-  typedef Keys<T, D, B> Own;
+  typedef Keys<T, D, B, kCodes || sizeof(T) == 2 ? 1 : 3> Own;
   typedef typename Own::Row Row;
   constexpr int kWaveKeys = 32 * Own::kBlocks, kTileKeys = 4 * kWaveKeys, kTileRows = 32 * Own::kRowBlocks;
-  constexpr int kRowBytes = D * (int)sizeof(T), kPieces = kRowBytes / 16, kAtOnce = kThreads / kPieces;
+  constexpr bool kSplit = sizeof(T) == 4;  // rows of fp32 lie in LDS as three tiles of bf16, their parts
+  constexpr int kRowBytes = D * 2, kPieces = kRowBytes / 16, kAtOnce = kThreads / kPieces;
   constexpr int kCopies = kTileRows / kAtOnce;
   // Two objects, so that the compiler sees that reading one need not wait for the loads into the other.
-  __shared__ __attribute__((aligned(16))) char s_even[kTileRows * kRowBytes];
-  __shared__ __attribute__((aligned(16))) char s_odd[kMode == kFew ? 16 : kTileRows * kRowBytes];
+  __shared__ __attribute__((aligned(16))) char s_even[(kSplit ? 3 : 1) * kTileRows * kRowBytes];
+  __shared__ __attribute__((aligned(16))) char s_odd[kMode == kFew || kSplit ? 16 : kTileRows * kRowBytes];
   __shared__ __attribute__((aligned(16))) float s_lse[2][kTileRows];  // in log2 units
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -222,6 +240,16 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     from = q_head0 + sub * a.q_head + (int64_t)query * a.q_token;
   }
   float next_lse = 0.0f;
+  auto bring_lse = [&](int r0) {
+    if (tid < kTileRows) {
+      next_lse = 0.0f;
+      if (r0 + tid < row1) {
+        int sub;
+        const int query = query_of(r0 + tid, sub);
+        next_lse = a.lse[((int64_t)h * a.group + sub) * a.Tq + p.q0 + query];
+      }
+    }
+  };
   auto bring = [&](auto F, int r0) {
     char* to = (F == 0 ? s_even : s_odd) + wave * 1024;
     if (even && r0 + kTileRows <= n_rows) {
@@ -239,13 +267,30 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
         to_lds(q_head0 + sub * a.q_head + (int64_t)query * a.q_token + (piece ^ turn(r)) * 16, to + c * (kThreads * 16));
       }
     }
-    if (tid < kTileRows) {
-      next_lse = 0.0f;
-      if (r0 + tid < row1) {
-        int sub;
-        const int query = query_of(r0 + tid, sub);
-        next_lse = a.lse[((int64_t)h * a.group + sub) * a.Tq + p.q0 + query];
-      }
+    bring_lse(r0);
+  };
+  // fp32: through registers, 8 channels a thread and row
+  float next[kSplit ? kCopies : 1][8];
+  auto fetch = [&](int r0) {
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      int sub;
+      const int query = query_of(min(r0 + c * kAtOnce + r_lane, n_rows - 1), sub);
+      const f32x4* row = reinterpret_cast<const f32x4*>(q_head0 + sub * a.q_head + (int64_t)query * a.q_token) + 2 * piece;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) next[c][e] = row[e / 4][e % 4];
+    }
+    bring_lse(r0);
+  };
+  auto store = [&]() {
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      const int r = c * kAtOnce + r_lane;
+      bf16x8 part[3];
+      split8(next[c], part);
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        *reinterpret_cast<bf16x8*>(s_even + (i * kTileRows + r) * kRowBytes + (piece ^ turn(r)) * 16) = part[i];
     }
   };
 
@@ -288,10 +333,20 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
         }
     }
   };
+  auto row_piece = [&](const char* rows, int j) {
+    if constexpr (kSplit) {
+      Row q;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) q.part[i] = *reinterpret_cast<const bf16x8*>(rows + i * kTileRows * kRowBytes + place[j]);
+      return q;
+    } else {
+      return *reinterpret_cast<const Row*>(rows + place[j]);
+    }
+  };
   Row ahead[kAhead];               // the first pieces of the next block's rows
   auto look_ahead = [&](const char* rows) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) ahead[j] = *reinterpret_cast<const Row*>(rows + place[j]);
+    for (int j = 0; j < kAhead; ++j) ahead[j] = row_piece(rows, j);
   };
   auto bring_stats = [&](auto H, int at, int rb) {
 #pragma unroll
@@ -302,14 +357,14 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     for (int b = B0; b < B1; ++b)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[H][b][e] = 0.0f;
-    constexpr int kFirst = kMode == kFused || D == 64 ? Own::kSteps : 1;  // rows' pieces on their way before the products
+    constexpr int kFirst = kMode == kFused || (D == 64 && !kSplit) ? Own::kSteps : 1;  // rows' pieces on their way before the products
     Row q[Own::kSteps];
 #pragma unroll
-    for (int j = 0; j < kFirst; ++j) q[j] = kMode == kFused && j < kAhead ? ahead[j] : *reinterpret_cast<const Row*>(rows + place[j]);
+    for (int j = 0; j < kFirst; ++j) q[j] = kMode == kFused && j < kAhead ? ahead[j] : row_piece(rows, j);
     if (kFirst > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < Own::kSteps; ++j) {
-      if (j >= kFirst) q[j] = *reinterpret_cast<const Row*>(rows + place[j]);
+      if (j >= kFirst) q[j] = row_piece(rows, j);
 #pragma unroll
       for (int b = B0; b < B1; ++b) own.product(j, b, q[j], acc[H][b]);
     }
@@ -360,7 +415,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
         __builtin_amdgcn_sched_barrier(0);
         if (i < kProducts) {
           if (i % Own::kBlocks == 0 && j + kAhead < Own::kSteps)
-            q[j + kAhead] = *reinterpret_cast<const Row*>(rows + place[j + kAhead]);
+            q[j + kAhead] = row_piece(rows, j + kAhead);
           own.product(j, i % Own::kBlocks, q[j], acc[H][i % Own::kBlocks]);
         }
         if (i == kProducts - 3) bring_stats(H, F, RB);
@@ -395,9 +450,14 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     }
     // this step's rows lie in LDS (the barrier alone does not wait for a wave's loads to LDS), and nobody reads the
     // other buffer
-    __builtin_amdgcn_s_waitcnt(kNoLoads);
+    if constexpr (kSplit) store();
+    else __builtin_amdgcn_s_waitcnt(kNoLoads);
     __syncthreads();
-    if (kMode != kFew && r0 + kTileRows < row1) bring(std::integral_constant<int, 1 - F>(), r0 + kTileRows);
+    if constexpr (kSplit) {
+      if (r0 + kTileRows < row1) fetch(r0 + kTileRows);
+    } else {
+      if (kMode != kFew && r0 + kTileRows < row1) bring(std::integral_constant<int, 1 - F>(), r0 + kTileRows);
+    }
     if constexpr (kMode == kFused) look_ahead(F == 0 ? s_even : s_odd);
     block(zero, F, std::integral_constant<int, 0>());
     block(one, F, std::integral_constant<int, 1>());
@@ -407,10 +467,15 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     }
     r0 += kTileRows;
   };
-  if (row0 < row1) bring(zero, row0);
+  if (row0 < row1) {
+    if constexpr (kSplit) fetch(row0);
+    else bring(zero, row0);
+  }
   while (r0 < row1) {
     step(zero);
-    if constexpr (kMode == kFew) {
+    if constexpr (kSplit) {
+      __syncthreads();  // the rows have been read
+    } else if constexpr (kMode == kFew) {
       __syncthreads();  // the rows have been read
       if (r0 < row1) bring(zero, r0);
     } else {

@@ -51,6 +51,20 @@ def test_mass_of_sinks_past_the_window(sink, dtype, d):
     check_mass(got, q, k, lse, cu, cu, lambda s, h, m, n: ref.seen_by(m, n, W, sink), d ** -0.5, old)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [-90, -30, 30, 90])
+def test_mass_of_fp32_at_every_magnitude(power, d):
+    """Queries and keys scaled by powers of two that cancel weigh the same, bit for bit."""
+    import torch
+    g = gen(power + 200)
+    H, G, n = 2, 2, 300
+    q, k = randn(g, H * G, n, d, dtype="f32"), randn(g, H, n, d, dtype="f32")
+    lse = lse_of(q, k, [0, n], [0, n], n, 0, 0.1)
+    want = binding.attention_mass(q, k, lse, n, 0, 0.1)["mass"]
+    got = binding.attention_mass(q * 2.0 ** power, k * 2.0 ** -power, lse, n, 0, 0.1)["mass"]
+    assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("rows", [31, 512, 513, 2048, 2049, 4096, 4097, 16385, 32768, 32769, 50000])
 def test_evict_selects_at_every_length(rows):
     """Lengths at and around those where the selection takes another number of threads, or does not keep its keys: the
