@@ -10,7 +10,7 @@
 //  * bf16: v_mfma_f32_32x32x16_bf16, 64 keys a wave, 128 rows a step.
 //  * fp32: a number is the sum of three bf16 (24 bits), a product the six of their products that reach 2^-24 of the
 //    largest: 6 x 32 cycles for 16 channels, where v_mfma_f32_32x32x2_f32 takes 512.  Rows pass through registers and are
-//    taken apart once for the four waves, 64 a step; 32 keys a wave.  A prompt of 4096 tokens (d 128, 8 heads of 4) 399 us,
+//    taken apart once for the four waves, 64 a step; 32 keys a wave.  A prompt of 4096 tokens (d 128, 8 heads of 4) 390 us,
 //    with the fp32 instruction 665.
 //  * keys in 8 bits: their codes become bf16, exactly, as they are loaded; the block's scale goes into the multiply-add.
 // Which rows see a lane's key is one run of rows, so a mask is a subtraction and a comparison, and blocks that see all
@@ -102,13 +102,16 @@ struct Keys<float, D, 1, P> {
   }
 };
 
-// What an item is.
+// What an item is.  Parts lie tile by tile, a tile's splits side by side; kByRows: the items at work together are those of
+// many tiles and the same rows, which one XCD's L2 then holds (a prompt of 32768 tokens reads
+// 1.4 GB instead of 12.9; one of 4096 in fp32 takes 388 us for 421).
 struct MassItem {
   int h, s, kt, split, splits;
   int q0, nq, k0, nk;
   int rows;       // of a split
   int64_t part;   // among the parts of all heads, where splits > 1
 };
+template <bool kByRows>
 __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
   MassItem p;
   p.h = h;
@@ -116,31 +119,77 @@ __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
   const int w = p.s * kMassSeqWords;
   p.q0 = seq_word(a.seq, w);
   p.k0 = seq_word(a.seq, w + 1);
-  const int i = item - seq_word(a.seq, w + 2);
-  p.splits = seq_word(a.seq, w + 3);
+  const int item0 = seq_word(a.seq, w + 2), splits = seq_word(a.seq, w + 3);
   p.rows = seq_word(a.seq, w + 4);
-  p.part = (int64_t)h * a.items + item;
   const int full = seq_word(a.seq, w + 5), shape = seq_word(a.seq, w + 6);
   const int kind = shape >> kMassShapeBits, by = shape & ((1 << kMassShapeBits) - 1);
-  int tile0 = 0, left = i;  // where tiles of p.splits splits begin, and the place among their items
-  if (left >= full * p.splits) {
-    left -= full * p.splits;
-    tile0 = full;
-    if (kind == kMassRest) {
-      p.splits = by;
-    } else {
-      const int run = kind == kMassRuns ? by : 1, drop = kind == kMassRuns ? 1 : by;
-      while (p.splits > drop && left >= run * p.splits) {
-        left -= run * p.splits;
-        tile0 += run;
-        p.splits -= drop;
-      }
-    }
-  }
-  p.kt = tile0 + left / p.splits;
-  p.split = left % p.splits;
   p.nq = seq_word(a.seq, w + kMassSeqWords) - p.q0;
   p.nk = seq_word(a.seq, w + kMassSeqWords + 1) - p.k0;
+  int left = item - item0, at = left;  // the place among the items not looked at yet, and among the parts
+  p.splits = splits;
+  if (kind == kMassRest) {  // `full` tiles of `splits` splits, the others of `by`
+    if (left >= full * splits) {
+      left -= full * splits;
+      p.splits = by;
+      p.kt = full + left / by;
+      p.split = left % by;
+    } else if (kByRows) {
+      p.kt = left % full;
+      p.split = left / full;
+      at = p.kt * splits + p.split;
+    } else {
+      p.kt = left / splits;
+      p.split = left % splits;
+    }
+  } else {  // `full` tiles of `splits` splits, then runs of tiles, each run of `drop` splits less, the last ones of `least`
+    const int run = kind == kMassRuns ? by : 1, drop = kind == kMassRuns ? 1 : by;
+    if (kByRows) {
+      // Split i of run g begins about where split i + g drop of the full tiles does: level by level of those.
+      const int tiles = (p.nk + a.keys - 1) / a.keys, runs = (splits + drop - 1) / drop, least = splits - (runs - 1) * drop;
+      int level = 0, here = min(tiles, full + run);  // tiles that have a split at this level
+      while (level < splits) {
+        const int n = min(drop, splits - level) * here;
+        if (left < n) break;
+        left -= n;
+        level += drop;
+        here = min(tiles, here + run);
+      }
+      int g = 0;
+      if (level < splits) {
+        p.kt = left % here;
+        p.split = level + left / here;
+        if (p.kt >= full) {
+          g = (p.kt - full) / run;
+          p.splits = splits - g * drop;
+          p.split -= g * drop;
+        }
+      } else {
+        p.splits = least;
+        p.kt = full + run * runs + left / least;
+        p.split = left % least;
+        g = (p.kt - full) / run;
+      }
+      const int m = min(g, runs);
+      at = p.kt < full ? p.kt * splits
+                       : full * splits + run * (m * splits - drop * (m * (m - 1) / 2) + (g - m) * least) +
+                             (p.kt - full - run * g) * p.splits;
+      at += p.split;
+    } else {
+      int tile0 = 0;
+      if (left >= full * splits) {
+        left -= full * splits;
+        tile0 = full;
+        while (p.splits > drop && left >= run * p.splits) {
+          left -= run * p.splits;
+          tile0 += run;
+          p.splits -= drop;
+        }
+      }
+      p.kt = tile0 + left / p.splits;
+      p.split = left % p.splits;
+    }
+  }
+  p.part = (int64_t)h * a.items + item0 + at;
   return p;
 }
 
@@ -163,7 +212,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = (int)(blockIdx.x % (unsigned)a.n_heads);
-  const MassItem p = mass_item(a, (int)(blockIdx.x / (unsigned)a.n_heads), h);
+  const MassItem p = mass_item<true>(a, (int)(blockIdx.x / (unsigned)a.n_heads), h);
   const int n = kCodes ? min(max(__builtin_amdgcn_readfirstlane(a.len[(int64_t)h * a.n_seqs + p.s]), 0), p.nk) : p.nk;
   const int offset = n - p.nq;                 // position of query 0
   const int key0 = p.kt * kTileKeys;
@@ -512,7 +561,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
 template <int kTileKeys>
 __global__ __launch_bounds__(kTileKeys) void mass_join_kernel(const MassArgs a) {
   const int h = (int)(blockIdx.x % (unsigned)a.n_heads);
-  const MassItem p = mass_item(a, (int)(blockIdx.x / (unsigned)a.n_heads), h);
+  const MassItem p = mass_item<false>(a, (int)(blockIdx.x / (unsigned)a.n_heads), h);
   if (p.splits <= 1 || p.split != 0) return;
   const int j = p.kt * kTileKeys + (int)threadIdx.x;
   if (j >= p.nk) return;
