@@ -12,6 +12,9 @@
 // contracts over rows).  One wave makes the 32 rows of a scale: a lane has 8 rows of d/16 channels, so the turn
 // from rows to channels stays in its registers (4 x 4 bytes in 8 v_perm), and the largest element takes six
 // exchanges in the wave.
+//
+// HBM bounds all of it at size.  288 heads, 6553 of 16384 rows of 128 in bf16: gathered in 281 us (966 MB read, 483
+// written: 5.2 TB/s), read back in 250 (5.8 TB/s).  64 sequences of 1024 to 4096 rows, three quarters moved: 135 us.
 #include <hip/hip_runtime.h>
 
 #include "../cache_ops.h"
