@@ -152,17 +152,20 @@ int cache_words(const C* c, const int64_t* cu, Blocks which, int unit, Cache4Arg
   const size_t need = words_bytes(c->n_seqs, kCacheSeqWords);
   if (need > 0 && (workspace == nullptr || workspace_bytes < (int64_t)(need + kAlign))) return TWINKV_E_WORKSPACE;
   WordWriter w(a.seq, ((int64_t)c->n_seqs + 1) * kCacheSeqWords, need > 0 ? aligned_base(workspace) : nullptr, stream);
-  int64_t at = 0;
+  int64_t at = 0, most = 0;
   for (int s = 0; s <= c->n_seqs; ++s) {
     w.put((int32_t)cu[s]);
     w.put((int32_t)c->cu_rows[s]);
     w.put((int32_t)at);
-    if (s < c->n_seqs) at += blocks_in(s);
+    if (s == c->n_seqs) break;
+    at += blocks_in(s);
+    most = std::max(most, cu[s + 1] - cu[s]);
   }
   a.cache = device_cache(c);
   a.n_heads = c->n_heads;
   a.n_seqs = c->n_seqs;
   a.n_blocks = (int)blocks;
+  a.max_tokens = (int)most;
   return hip_status(w.finish());
 }
 

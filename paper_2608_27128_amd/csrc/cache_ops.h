@@ -66,6 +66,7 @@ struct Cache4Args {
   int64_t C_out;
   int n_heads, n_seqs;
   int n_blocks;          // blocks of all sequences of a head
+  int max_tokens;        // of a sequence
 };
 int launch_cache4_positions(const Cache4Args& a, void* stream);
 int launch_cache4_gather(const Cache4Args& a, int dtype, int d, void* stream);

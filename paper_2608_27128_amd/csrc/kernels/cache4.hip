@@ -23,7 +23,6 @@ namespace {
 
 constexpr int kOk = 0, kMismatch = 1, kNonfinite = 2;  // TWINKV_PROBLEM_*
 constexpr int kThreads = 256;                          // gather, read
-constexpr int kPosThreads = 1024;
 constexpr int kMaxWaves = 16;                          // append: blocks a workgroup takes at once
 
 __device__ inline unsigned quad_xor1(unsigned x) {
@@ -146,6 +145,7 @@ __device__ inline bool write_block(const Cache4& c, int h, int64_t blk, int lo, 
 // ---- compaction ----
 
 // Exclusive ranks of the threads' counts in the workgroup, and their total.
+template <int kPosThreads>
 __device__ inline int block_rank(int n, int& total, int* s_wave) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int incl = n;
@@ -166,7 +166,9 @@ __device__ inline int block_rank(int n, int& total, int* s_wave) {
   return before + incl - n;
 }
 
-// K7a: one workgroup per problem lists its retained positions, 16 mask bytes a thread at a time.
+// K7a: one workgroup per problem lists its retained positions, 16 mask bytes a thread at a time.  Threads for the longest
+// sequence: 2560 problems of 39 to 784 tokens take 7 us, 31 with 1024 threads; 512 of 1024 to 4096 tokens 6, 9.
+template <int kPosThreads>
 __global__ __launch_bounds__(kPosThreads) void cache4_positions_kernel(const Cache4Args a) {
   __shared__ int s_wave[kPosThreads / 64];
   const int s = (int)blockIdx.x % a.n_seqs, h = (int)blockIdx.x / a.n_seqs;
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(kPosThreads) void cache4_positions_kernel(const Cac
       for (int e = 0; at + e < n; ++e) bits |= (m[at + e] != 0 ? 1u : 0u) << e;
     }
     int total;
-    int row = have + block_rank(__popc(bits), total, s_wave);
+    int row = have + block_rank<kPosThreads>(__popc(bits), total, s_wave);
     while (bits != 0) {
       const int e = __ffs(bits) - 1;
       bits &= bits - 1;
@@ -427,8 +429,11 @@ int launch_read(const Cache4Args& a, hipStream_t s) {
 }  // namespace
 
 int launch_cache4_positions(const Cache4Args& a, void* stream) {
-  hipLaunchKernelGGL(cache4_positions_kernel, dim3((unsigned)a.n_heads * (unsigned)a.n_seqs), dim3(kPosThreads), 0,
-                     (hipStream_t)stream, a);
+  const dim3 grid((unsigned)a.n_heads * (unsigned)a.n_seqs);
+  hipStream_t s = (hipStream_t)stream;
+  if (a.max_tokens <= 1024) hipLaunchKernelGGL(cache4_positions_kernel<64>, grid, dim3(64), 0, s, a);
+  else if (a.max_tokens <= 4096) hipLaunchKernelGGL(cache4_positions_kernel<256>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cache4_positions_kernel<1024>, grid, dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
