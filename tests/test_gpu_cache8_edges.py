@@ -90,6 +90,28 @@ def test_evict_selects_at_every_length(rows):
     assert got["mass"][:, int(to.cu_rows[1])].tolist() == [float(mass[0, r0]), 0.0]
 
 
+def test_evict_selects_of_many_long_problems():
+    """More problems than CUs, the longest between 4096 and 8192 rows."""
+    import torch
+    g = gen(77)
+    H, d, rows = 150, 64, [5000, 90]
+    cache, to = binding.Cache8.empty(H, rows, d), binding.Cache8.empty(H, [64, 64], d)
+    for c in (cache.k_codes, cache.v_codes):
+        c.zero_()
+    for c in (cache.k_scales, cache.v_scales):
+        c.fill_(127)
+    length = torch.tensor([rows] * H, dtype=torch.int32, device="cuda")
+    length[:, 0] -= torch.arange(H, device="cuda", dtype=torch.int32)
+    mass = (torch.rand((H, int(cache.cu_rows[-1])), generator=g, device="cuda") * 300).floor() / 64
+    got = binding.cache8_evict(cache, length, mass, [50, 61], to, 4, 16)
+    for h in range(0, H, 7):
+        for s in range(2):
+            n, r0, t0 = int(length[h, s]), int(cache.cu_rows[s]), int(to.cu_rows[s])
+            kept = ref8.kept_rows(mass[h, r0:r0 + n].tolist(), n, [50, 61][s], 4, 16)
+            assert got["pos"][h, t0:t0 + len(kept)].tolist() == list(kept)
+    assert got["len"].tolist() == [[50, 61]] * H
+
+
 def test_attention_more_queries_than_rows():
     """A problem with fewer rows than queries: the first queries see nothing, and neither do those of an empty one."""
     import torch
