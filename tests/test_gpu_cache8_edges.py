@@ -51,6 +51,18 @@ def test_mass_of_sinks_past_the_window(sink, dtype, d):
     check_mass(got, q, k, lse, cu, cu, lambda s, h, m, n: ref.seen_by(m, n, W, sink), d ** -0.5, old)
 
 
+@pytest.mark.parametrize("dtype,d,H,G", [("bf16", 128, 19, 1), ("bf16", 64, 8, 2), ("f32", 64, 9, 3), ("bf16", 128, 16, 1)])
+def test_mass_of_many_heads(dtype, d, H, G):
+    """Whole and partial groups of eight heads, ragged prompts whose rows are split."""
+    g = gen(H + d)
+    lens = [1300, 1, 400]
+    cu = cum(lens)
+    q, k = randn(g, H * G, sum(lens), d, dtype=dtype), randn(g, H, sum(lens), d, dtype=dtype)
+    lse = lse_of(q, k, cu, cu, 2000, 0, 0.1)
+    got = binding.attention_mass(q, k, lse, 2000, 0, 0.1, cu, cu)["mass"]
+    check_mass(got, q, k, lse, cu, cu, lambda s, h, m, n: ref.seen_by(m, n, 2000, 0), 0.1)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("power", [-90, -30, 30, 90])
 def test_mass_of_fp32_at_every_magnitude(power, d):
