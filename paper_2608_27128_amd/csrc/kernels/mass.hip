@@ -23,7 +23,8 @@
 //  * kApart (bf16 of d 64, fp32): products, then weights.  With half the products to hide behind, twice the waves count for
 //    more: 8192 tokens of d 64 190 us, fused 217.
 //  * kFew (bf16, at most kMassFew rows a key): the keys' way to the registers is the work, so one buffer of rows, and more
-//    workgroups.  64 sequences of 1024 to 4096 keys, the last 32 queries: 88 us, 4.0 TB/s of keys and scales.
+//    workgroups.  64 sequences of 1024 to 4096 keys, the last 32 queries: 88 us, 4.0 TB/s of keys; with 32 keys a wave 100, with
+//    the keys of several tiles passing by one staged copy of the rows 106.
 //
 // Sums: 32 bits, in two levels, since one chain over 100000 rows loses 3 digits: a lane adds up to 16 steps'
 // weights, then their sum to the total.  Rows are split over workgroups where there are too few keys, and a second kernel
