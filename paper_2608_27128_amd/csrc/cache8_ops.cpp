@@ -232,12 +232,16 @@ int attn8_layout(int dtype, int d, int n_heads, int group, int n_seqs, const int
                  bool want_mass, Attn8Layout& L) {
   L.scores = want_mass && keeps_scores(group, n_seqs, cu_q, cu_rows);
   int64_t most_tiles = kAttnMaxKeys;  // of a split
+  // Scores are kept for one tile of rows an item.  (Queries of sequences without rows count in the plan's mean, and
+  // could ask for two.)
+  const int most_rows = L.scores ? kAttnRows : kAttnPairRows;
   if (L.scores) {
     for (int s = 0; s < n_seqs; ++s)
       if (cu_rows[s + 1] > cu_rows[s]) L.score_rows = std::max(L.score_rows, (int)((cu_q[s + 1] - cu_q[s]) * group));
     most_tiles = kAttnMostLds / (4 * kAttnTile * std::max(L.score_rows, 1));
   }
-  int rc = attn_plan(cached_keys(dtype), d, n_heads, group, n_seqs, cu_q, cu_rows, INT64_MAX, 0, L.plan, most_tiles);
+  int rc = attn_plan(cached_keys(dtype), d, n_heads, group, n_seqs, cu_q, cu_rows, INT64_MAX, 0, L.plan, most_tiles,
+                     most_rows);
   if (rc != TWINKV_OK) return rc;
   L.attn = attn_layout(L.plan, d, n_heads, n_seqs).total;
   if (!want_mass) return TWINKV_OK;

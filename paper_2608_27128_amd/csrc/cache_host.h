@@ -284,14 +284,16 @@ constexpr int64_t kPairWork = 49152;
 // 769 / 709; two rows a token, 2048 tokens (1) 136 / 136, 3000 (0.68) 240 / 224.
 constexpr int64_t kWideTiles = 20, kLongTiles64 = 96;
 
-// most_tiles: a split has no more.
+// most_tiles: a split has no more.  most_rows: nor has an item of rows over a cache.
 inline int attn_plan(KeysAre keys, int d, int n_heads, int group, int n_seqs, const int64_t* cu_q, const int64_t* cu_k,
-                     int64_t window, int64_t n_sink, AttnPlan& p, int64_t most_tiles = kAttnMaxKeys) {
+                     int64_t window, int64_t n_sink, AttnPlan& p, int64_t most_tiles = kAttnMaxKeys,
+                     int most_rows = kAttnPairRows) {
   p.window = std::min<int64_t>(window, kAttnMaxKeys);
   p.n_sink = std::min<int64_t>(n_sink, kAttnMaxKeys);
   const bool cached = keys == KeysAre::kCached || keys == KeysAre::kCachedFp32;
   AttnWork few = work_of(n_heads, group, n_seqs, cu_q, cu_k, p);
-  if (keys == KeysAre::kCached && few.tiles >= kPairWork && cu_q[n_seqs] * group > kAttnRows * live_of(n_seqs, cu_q)) {
+  if (keys == KeysAre::kCached && most_rows >= kAttnPairRows && few.tiles >= kPairWork &&
+      cu_q[n_seqs] * group > kAttnRows * live_of(n_seqs, cu_q)) {
     p.rows = kAttnPairRows;
     few = work_of(n_heads, group, n_seqs, cu_q, cu_k, p);
   }

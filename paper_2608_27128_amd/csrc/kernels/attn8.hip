@@ -221,6 +221,7 @@ int run8(const AttnArgs& a, hipStream_t s) {
 int launch_attn8(const AttnArgs& a, int dtype, int d, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   if (dtype != 0) return d == 128 ? run8<float, 128>(a, s) : run8<float, 64>(a, s);
+  if (a.rows == kAttnPairRows && a.mass_out != nullptr) return hipErrorInvalidValue;  // (no such kernel)
   if (a.rows == kAttnPairRows) return d == 128 ? run8<bf16, 128, 2, false>(a, s) : run8<bf16, 64, 2, false>(a, s);
   return d == 128 ? run8<bf16, 128>(a, s) : run8<bf16, 64>(a, s);
 }

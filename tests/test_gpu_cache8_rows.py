@@ -1,0 +1,49 @@
+"""Attention over the 8-bit cache in batches whose plan takes two row tiles a wave, or would if the queries of
+sequences without rows decided it (tests/host/cache8_plans_test.cpp holds the plans of these batches to that)."""
+import math
+
+import pytest
+
+import cache_ops_ref as ref
+from paper_2608_27128_amd import binding
+from test_gpu_cache8 import check_mass, filled
+from test_gpu_cache_ops import check_attention, cum, gen, randn
+
+pytestmark = pytest.mark.gpu
+
+
+def check_problem(got, q, cache, length, keys, values, h, s, cu_q, G, old):
+    """One problem's outputs (of its first and last query head), log-sum-exps and weights."""
+    a, b, r0, r1 = int(cu_q[s]), int(cu_q[s + 1]), int(cache.cu_rows[s]), int(cache.cu_rows[s + 1])
+    n, d = int(length[h, s]), cache.d
+    k, v = keys[h, r0:r0 + n], values[h, r0:r0 + n]
+    seen = ref.seen_by(b - a, n, 1 << 40, 0)
+    for x in sorted({0, G - 1}):
+        one = slice(h * G + x, h * G + x + 1)
+        check_attention(got["out"][one, a:b], q[one, a:b], k[None], v[None], [0, b - a], [0, n], lambda *_: seen,
+                        d ** -0.5, "bf16", got["lse"][one, a:b])
+    hs = slice(h * G, h * G + G)
+    check_mass(got["mass"][None, h, r0:r0 + n], q[hs, a:b], k[None], got["lse"][hs, a:b], [0, b - a], [0, n],
+               lambda *_: seen, d ** -0.5, old[None, h, r0:r0 + n])
+    assert not bool(got["mass"][h, r0 + n:r1].any())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,G,rows,nq", [(16, 8, [131072, 0], [1, 40]), (8, 4, [4096] * 64 + [0], [1] * 64 + [300]),
+                                         (8, 8, [4096] * 64 + [0], [1] * 64 + [512])])
+def test_weights_beside_queries_without_rows(H, G, rows, nq, d):
+    """Few rows a problem, in one split and in many, beside a sequence of many queries and no cached row, which gets
+    zeros."""
+    import torch
+    g = gen(len(rows) + G + d)
+    cache, length, keys, values = filled(g, H, rows, d)
+    cu_q = cum(nq)
+    q = randn(g, H * G, int(cu_q[-1]), d)
+    old = torch.rand(keys.shape[:2], generator=g, device="cuda")
+    new = torch.full_like(old, math.nan)
+    got = binding.cache8_attention(q, cache, length, None, cu_q, want_lse=True, mass=old, mass_out=new)
+    for h, s in [(0, 0), (H - 1, 0), (1, len(rows) - 2), (H // 2, (len(rows) - 1) // 2)]:
+        check_problem(got, q, cache, length, keys, values, h, s, cu_q, G, old)
+    assert bool(torch.isfinite(got["mass"]).all())
+    last = int(cu_q[-2])
+    assert not bool(got["out"][:, last:].any()) and bool((got["lse"][:, last:] == -math.inf).all())
