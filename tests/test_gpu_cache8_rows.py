@@ -47,3 +47,39 @@ def test_weights_beside_queries_without_rows(H, G, rows, nq, d):
     assert bool(torch.isfinite(got["mass"]).all())
     last = int(cu_q[-2])
     assert not bool(got["out"][:, last:].any()) and bool((got["lse"][:, last:] == -math.inf).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_two_row_tiles_over_a_long_cache(d):
+    """28 rows a problem, the second tile of 12, keys in many splits."""
+    import torch
+    g = gen(d)
+    H, G, nq, rows = 8, 4, 7, 131072
+    cache, length, keys, values = filled(g, H, [rows], d, lens=[[rows - 1000 * h - h] for h in range(H)])
+    q = randn(g, H * G, nq, d)
+    old = torch.rand(keys.shape[:2], generator=g, device="cuda")
+    got = binding.cache8_attention(q, cache, length, None, [0, nq], want_lse=True, mass=old)
+    alone = binding.cache8_attention(q, cache, length, None, [0, nq], want_lse=True)
+    assert torch.equal(alone["out"], got["out"]) and torch.equal(alone["lse"], got["lse"])
+    for h in (0, 5, H - 1):
+        check_problem(got, q, cache, length, keys, values, h, 0, [0, nq], G, old)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_two_row_tiles_of_many_sequences(d):
+    """17 to 40 rows a problem, so that the last tile has 1 to 16; lengths of all kinds, fewer than queries and none
+    among them, that differ from head to head; one problem of 32 cached rows."""
+    import torch
+    g = gen(100 + d)
+    H, G, S = 4, 1, 64
+    nq, rows = [17 + s % 24 for s in range(S)], [32 if s == 5 else 4096 for s in range(S)]
+    lens = [[min(rows[s], [(997 * s + 131 * h) % 4097, 4096, 0, 20, 1][s % 5 if s % 3 else 0]) for s in range(S)]
+            for h in range(H)]
+    cache, length, keys, values = filled(g, H, rows, d, lens=lens)
+    cu_q = cum(nq)
+    q = randn(g, H * G, int(cu_q[-1]), d)
+    old = torch.rand(keys.shape[:2], generator=g, device="cuda")
+    got = binding.cache8_attention(q, cache, length, None, cu_q, want_lse=True, mass=old)
+    for s in range(S):
+        check_problem(got, q, cache, length, keys, values, s % H, s, cu_q, G, old)
+    assert bool(torch.isfinite(got["out"].float()).all()) and bool(torch.isfinite(got["mass"]).all())
