@@ -206,6 +206,7 @@ __device__ inline void add_weights(const AttnArgs& a, const AttnItem& p, const f
                                    const Score& score) {
   const int n_rows = p.nq * a.group;
   const int len = min(max(a.len[(int64_t)p.h * a.n_seqs + p.s], 0), p.nk);
+  const int lim_all = len - (p.nq - 1);  // every row sees so many keys
   const int t0 = p.split * p.tiles * kAttnTile, t1 = min(t0 + p.tiles * kAttnTile, p.nk);
   const int64_t at = (int64_t)p.h * a.cache.C + p.k0;
   for (int j = t0 + 4 * tid; j < t1; j += 4 * threads) {  // (a problem's rows are a multiple of 32)
@@ -213,11 +214,20 @@ __device__ inline void add_weights(const AttnArgs& a, const AttnItem& p, const f
     if (j < len) {
       if (a.mass != nullptr) sum = *reinterpret_cast<const f32x4*>(a.mass + at + j);
       f32x4 more = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (j + 4 <= lim_all) {
 #pragma unroll 4
-      for (int r = 0; r < n_rows; ++r) {
-        const f32x4 s = score(r, j);
+        for (int r = 0; r < n_rows; ++r) {
+          const f32x4 s = score(r, j);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) more[e] += __builtin_amdgcn_exp2f(s[e] - lse[r]);
+          for (int e = 0; e < 4; ++e) more[e] += __builtin_amdgcn_exp2f(s[e] - lse[r]);
+        }
+      } else {  // (a score of -inf is not enough: a row whose log-sum-exp is NaN has no weight either on a key it does not see)
+        for (int r = 0; r < n_rows; ++r) {
+          const f32x4 s = score(r, j);
+          const int lim = lim_all + r / a.group;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) more[e] += j + e < lim ? __builtin_amdgcn_exp2f(s[e] - lse[r]) : 0.0f;
+        }
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = j + e < len ? sum[e] + more[e] : 0.0f;

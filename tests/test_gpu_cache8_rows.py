@@ -83,3 +83,22 @@ def test_two_row_tiles_of_many_sequences(d):
     for s in range(S):
         check_problem(got, q, cache, length, keys, values, s % H, s, cu_q, G, old)
     assert bool(torch.isfinite(got["out"].float()).all()) and bool(torch.isfinite(got["mass"]).all())
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("rows,nq,G", [(300, 3, 4), (9000, 5, 3), (300, 9, 4), (9000, 8, 3)])
+def test_weights_of_a_nan_query_reach_the_keys_that_it_sees(rows, nq, G, dtype, d):
+    """And no key behind it: with scores kept in one split and in many, and with weights computed afresh."""
+    import torch
+    g = gen(rows + nq)
+    H = 2
+    cache, length, _, _ = filled(g, H, [rows], d, dtype)
+    q = randn(g, H * G, nq, d, dtype=dtype)
+    clean = binding.cache8_attention(q, cache, length, None, [0, nq], want_lse=True, want_mass=True)
+    q[1, 0] = math.nan
+    q[G, nq - 2, d - 1] = math.nan
+    got = binding.cache8_attention(q, cache, length, None, [0, nq], want_lse=True, want_mass=True)
+    for h, first in ((0, 0), (1, nq - 2)):
+        seen = int(length[h, 0]) - (nq - 1 - first)  # keys that the query sees
+        assert bool(torch.isnan(got["mass"][h, :seen]).all())
+        assert torch.equal(got["mass"][h, seen:], clean["mass"][h, seen:]) and bool(clean["mass"][h, seen] > 0)
