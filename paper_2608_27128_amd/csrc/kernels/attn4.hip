@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(const AttnArgs 
   if (a.mass_out == nullptr) return;
   // The accumulated weights of the split's keys (one tile of 16 rows a problem): every row's maximum and sum again, 16
   // threads a row.
-  __shared__ float s_lse[kAttnRows];
+  __shared__ RowLse s_lse;
   static_assert(kJoinThreads == 16 * kAttnRows, "16 threads a row");
   const int r = threadIdx.x / 16;
   float top = kNegInf, sum = 0.0f;
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(const AttnArgs 
     const float m = __shfl_xor(top, by), l = __shfl_xor(sum, by);
     add(m, l);
   }
-  if (threadIdx.x % 16 == 0) s_lse[r] = lse_log2(top, sum);
+  if (threadIdx.x % 16 == 0) s_lse.put(r, top, sum);
   __syncthreads();
   const float* scores = score_rows_of(a, p);
   add_weights(a, p, s_lse, (int)threadIdx.x, kJoinThreads, [&](int row, int j) {

@@ -196,9 +196,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, sizeof(T) == 2 && R == 1 ? 4 : 2) 
           *reinterpret_cast<f32x4*>(to + (int64_t)r * a.cache.C + j) = *reinterpret_cast<const f32x4*>(s_score + r * keys + j);
       return;
     }
-    __shared__ float s_lse[kAttnRows];
+    __shared__ RowLse s_lse;
     // (the tile's maxima and sums lie first in the join's place)
-    if (threadIdx.x < kAttnRows) s_lse[threadIdx.x] = lse_log2(s_join[threadIdx.x], s_join[kAttnRows + threadIdx.x]);
+    if (threadIdx.x < kAttnRows) s_lse.put((int)threadIdx.x, s_join[threadIdx.x], s_join[kAttnRows + threadIdx.x]);
     __syncthreads();
     add_weights(a, p, s_lse, (int)threadIdx.x, 64 * kAttnWaves,
                 [&](int row, int j) { return *reinterpret_cast<const f32x4*>(s_score + row * keys + j); });

@@ -198,39 +198,44 @@ constexpr int join_floats() {
   return kAttnWaves * 2 * kAttnRows + kAttnRows * (D + 4);
 }
 
-// The weights of an item's keys, summed over the problem's rows (one tile), from their scores (score(r, j): those of
-// row r and keys j .. j + 3) and the rows' log-sum-exps in log2 units (+inf where a row sees nothing), added to what the
-// keys have.
+// The log-sum-exps of a problem's rows (one tile), in log2 units, from their maxima and sums: +inf where a row sees
+// nothing, and where there is none (a NaN), which is noted apart.
+struct RowLse {
+  float at[kAttnRows];
+  int none[kAttnRows];
+  __device__ void put(int r, float m, float l) {
+    const float x = l == 0.0f ? -kNegInf : m + __builtin_amdgcn_logf(l);
+    none[r] = x != x;
+    at[r] = x != x ? -kNegInf : x;
+  }
+};
+
+// The weights of an item's keys, summed over the problem's rows, from their scores (score(r, j): those of row r and
+// keys j .. j + 3, -inf where not seen) and the rows' log-sum-exps, added to what the keys have.
 template <typename Score>
-__device__ inline void add_weights(const AttnArgs& a, const AttnItem& p, const float* lse, int tid, int threads,
+__device__ inline void add_weights(const AttnArgs& a, const AttnItem& p, const RowLse& lse, int tid, int threads,
                                    const Score& score) {
   const int n_rows = p.nq * a.group;
   const int len = min(max(a.len[(int64_t)p.h * a.n_seqs + p.s], 0), p.nk);
-  const int lim_all = len - (p.nq - 1);  // every row sees so many keys
   const int t0 = p.split * p.tiles * kAttnTile, t1 = min(t0 + p.tiles * kAttnTile, p.nk);
   const int64_t at = (int64_t)p.h * a.cache.C + p.k0;
+  // The keys before nan_end are seen by a row without a log-sum-exp.  (A later row sees more.)
+  const int lane = tid & 63;
+  const unsigned none = (unsigned)__ballot(lane < n_rows && lse.none[lane & (kAttnRows - 1)] != 0);
+  const int nan_end = none == 0 ? 0 : len - (p.nq - 1) + (31 - __builtin_clz(none)) / a.group;
   for (int j = t0 + 4 * tid; j < t1; j += 4 * threads) {  // (a problem's rows are a multiple of 32)
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     if (j < len) {
       if (a.mass != nullptr) sum = *reinterpret_cast<const f32x4*>(a.mass + at + j);
       f32x4 more = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (j + 4 <= lim_all) {
 #pragma unroll 4
-        for (int r = 0; r < n_rows; ++r) {
-          const f32x4 s = score(r, j);
+      for (int r = 0; r < n_rows; ++r) {
+        const f32x4 s = score(r, j);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) more[e] += __builtin_amdgcn_exp2f(s[e] - lse[r]);
-        }
-      } else {  // (a score of -inf is not enough: a row whose log-sum-exp is NaN has no weight either on a key it does not see)
-        for (int r = 0; r < n_rows; ++r) {
-          const f32x4 s = score(r, j);
-          const int lim = lim_all + r / a.group;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) more[e] += j + e < lim ? __builtin_amdgcn_exp2f(s[e] - lse[r]) : 0.0f;
-        }
+        for (int e = 0; e < 4; ++e) more[e] += __builtin_amdgcn_exp2f(s[e] - lse.at[r]);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] = j + e < len ? sum[e] + more[e] : 0.0f;
+      for (int e = 0; e < 4; ++e) sum[e] = j + e >= len ? 0.0f : j + e < nan_end ? __builtin_nanf("") : sum[e] + more[e];
     }
     *reinterpret_cast<f32x4*>(a.mass_out + at + j) = sum;
   }
@@ -239,7 +244,6 @@ __device__ inline void add_weights(const AttnArgs& a, const AttnItem& p, const f
 __device__ inline float* score_rows_of(const AttnArgs& a, const AttnItem& p) {
   return a.score + (int64_t)p.h * a.score_rows * a.cache.C + p.k0;
 }
-__device__ inline float lse_log2(float m, float l) { return l == 0.0f ? -kNegInf : m + __builtin_amdgcn_logf(l); }
 
 // One wave's own 16 rows, complete, through its own LDS.
 template <typename T, int D, typename Channel>
