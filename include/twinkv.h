@@ -510,7 +510,8 @@ int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* 
  *   workspace  twinkv_mass_workspace_bytes(...) bytes (may be NULL when that is 0).
  * Scores and sums are fp32, and the order of the sums does not change from call to call.  Products of fp32 elements
  * keep 24 bits where the elements lie between 2^-100 and 2^127 (smaller ones lose low bits, larger ones may count as
- * infinite).  A key that a query does not see never changes another key's sum, NaN and infinities included.
+ * infinite); an infinite element counts as that.  A key that a query does not see never changes another key's sum, NaN and
+ * infinities included.
  */
 int twinkv_attention_mass(const void* q, const void* k, int dtype, int d, int n_heads, int group, int n_seqs,
                           const int64_t* cu_q, const int64_t* cu_k, int64_t q_head_stride,

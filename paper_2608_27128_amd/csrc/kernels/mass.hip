@@ -68,6 +68,7 @@ struct Keys<bf16, D, B, P> {
   __device__ void product(int j, int b, const Row& q, f32x16& acc) const {
     acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[b][j], acc, 0, 0, 0);
   }
+  __device__ void product_each(int j, int b, const Row& q, f32x16& acc) const { product(j, b, q, acc); }
 };
 
 template <int D, int P>
@@ -101,6 +102,19 @@ struct Keys<float, D, 1, P> {
 #pragma unroll
       for (int of_k = 0; of_k <= sum && of_k < P; ++of_k)
         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q.part[sum - of_k], k[j][of_k], acc, 0, 0, 0);
+  }
+  // The products of the numbers that the parts are of, whose infinities keep their meaning: two channels at a time.
+  static __device__ float number(float first, float rest) {  // (of an infinite number the rest is NaN)
+    return __builtin_isfinite(first) ? first + rest : first;
+  }
+  __device__ void product_each(int j, int, const Row& q, f32x16& acc) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = number((float)q.part[0][e], (float)q.part[1][e] + (float)q.part[2][e]);
+      float y = (float)k[j][0][e];
+      if constexpr (P == 3) y = number(y, (float)k[j][1][e] + (float)k[j][2][e]);
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, acc, 0, 0, 0);
+    }
   }
 };
 
@@ -211,6 +225,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
   __shared__ __attribute__((aligned(16))) char s_even[(kSplit ? 3 : 1) * kTileRows * kRowBytes];
   __shared__ __attribute__((aligned(16))) char s_odd[kMode == kFew || kSplit ? 16 : kTileRows * kRowBytes];
   __shared__ __attribute__((aligned(16))) float s_lse[2][kTileRows];  // in log2 units
+  __shared__ int s_odd_sum;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // (8 heads at a time, one an XCD: of more at once an XCD's L2 would not hold the rows that its items share; 288 heads of
@@ -288,12 +303,12 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
   const bool even = kAtOnce % a.group == 0 && row0 % a.group == 0;
   const int64_t copy_bytes = even ? kAtOnce / a.group * a.q_token : 0, step_bytes = copy_bytes * kCopies;
   const int r_lane = tid / kPieces, piece = tid % kPieces;
-  const char* from;
-  {
+  auto first_row = [&]() {
     int sub;
     const int query = query_of(row0 + r_lane, sub);
-    from = q_head0 + sub * a.q_head + (int64_t)query * a.q_token;
-  }
+    return q_head0 + sub * a.q_head + (int64_t)query * a.q_token;
+  };
+  const char* from = first_row();
   float next_lse = 0.0f;
   auto bring_lse = [&](int r0) {
     if (tid < kTileRows) {
@@ -363,6 +378,9 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
 
   const std::integral_constant<int, 0> zero;
   const std::integral_constant<int, 1> one;
+  enum { kAll, kSeen, kEach };  // whose weights
+  const std::integral_constant<int, kAll> of_all;
+  const std::integral_constant<int, kSeen> of_seen;
   // The rows of the item that see this lane's key of block b: from first[b] on, so many.
   int first[Own::kBlocks];
   unsigned many[Own::kBlocks];
@@ -374,7 +392,8 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     many[b] = (unsigned)max(end - first[b], (int64_t)0);
   }
   auto seen = [&](int row, int b) { return (unsigned)(row - first[b]) < many[b]; };
-  // The weights of the block of rows from `row` on, for key blocks B0 .. B1 - 1.
+  // The weights of the block of rows from `row` on, for key blocks B0 .. B1 - 1.  (kEach: of the rows that see a key, an
+  // element at a time.)
   auto weigh = [&](auto all, auto H, auto B0, auto B1, int row) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {  // rows 8x + 4hi .. + 3 of the block
@@ -383,8 +402,9 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float arg = __builtin_fmaf(acc[H][b][4 * x + e], scale[b], -l[H][x][e]);
-          if constexpr (decltype(all)::value) run[b] += __builtin_amdgcn_exp2f(arg);
-          else run[b] += __builtin_amdgcn_exp2f(seen(row + 4 * hi + 8 * x + e, b) ? arg : kNegInf);
+          if constexpr (all == kAll) run[b] += __builtin_amdgcn_exp2f(arg);
+          else if constexpr (all == kSeen) run[b] += __builtin_amdgcn_exp2f(seen(row + 4 * hi + 8 * x + e, b) ? arg : kNegInf);
+          else run[b] += seen(row + 4 * hi + 8 * x + e, b) ? __builtin_amdgcn_exp2f(arg) : 0.0f;
         }
     }
   };
@@ -432,7 +452,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     auto part = [&](auto B0, auto B1) {
       if (!some_see(row, B0)) return;
       multiply(H, B0, B1, rows);
-      weigh(std::false_type(), H, B0, B1, row);
+      weigh(of_seen, H, B0, B1, row);
     };
     part(zero, one);
     if constexpr (Own::kBlocks == 2) part(one, blocks);
@@ -441,7 +461,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     if (all_see(r0 + 32 * RB)) {
       multiply(zero, zero, blocks, (F == 0 ? s_even : s_odd) + RB * 32 * kRowBytes);
       bring_stats(zero, F, RB);
-      weigh(std::true_type(), zero, zero, blocks, 0);
+      weigh(of_all, zero, zero, blocks, 0);
     } else {
       bring_stats(zero, F, RB);
       block_masked(zero, F, RB);
@@ -485,7 +505,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
       }
       __builtin_amdgcn_sched_barrier(0);
     } else {
-      if (before) weigh(std::true_type(), other, zero, blocks, 0);
+      if (before) weigh(of_all, other, zero, blocks, 0);
       bring_stats(H, F, RB);
       if (all) multiply(H, zero, blocks, rows);
       else block_masked(H, F, RB);
@@ -522,6 +542,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     }
     r0 += kTileRows;
   };
+  if (tid == 0) s_odd_sum = 0;
   if (row0 < row1) {
     if constexpr (kSplit) fetch(row0);
     else bring(zero, row0);
@@ -546,19 +567,81 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     }
   }
   if constexpr (kMode == kFused) {
-    if (before) weigh(std::true_type(), one, zero, blocks, 0);
+    if (before) weigh(of_all, one, zero, blocks, 0);
+  }
+  float sum[Own::kBlocks];
+  bool odd = false;  // a sum is NaN or infinite
+#pragma unroll
+  for (int b = 0; b < Own::kBlocks; ++b) {
+    sum[b] = total[b] + run[b];
+    sum[b] += __shfl_xor(sum[b], 32);
+    odd |= !(sum[b] < -kNegInf);
+  }
+  // Such a sum is computed once more, where fp32 elements are multiplied as they are: an infinite one is not the sum of its
+  // parts.  (The same for the workgroup.  Where there is none the check costs nothing measurable: 32768 tokens 3891 us / 3898,
+  // 8192 of d 64 185.0 / 185.4.)
+  if (row0 < row1) {
+    if (__any(odd) && lane == 0) s_odd_sum = 1;
+    __syncthreads();
+    if (s_odd_sum != 0) {
+      from = first_row();
+      r0 = row0;
+      flush = 0;
+#pragma unroll
+      for (int b = 0; b < Own::kBlocks; ++b) total[b] = run[b] = 0.0f;
+      while (r0 < row1) {
+        __syncthreads();  // the rows before have been read
+        if constexpr (kSplit) {
+          fetch(r0);
+          store();
+        } else {
+          bring(zero, r0);
+        }
+        if (tid < kTileRows) s_lse[0][tid] = next_lse == kNegInf ? -kNegInf : next_lse * 1.44269504088896340736f;
+        if constexpr (!kSplit) __builtin_amdgcn_s_waitcnt(kNoLoads);
+        __syncthreads();
+#pragma unroll 1
+        for (int rb = 0; rb < Own::kRowBlocks; ++rb) {
+          bring_stats(zero, 0, rb);
+          auto part = [&](auto B0, auto B1) {
+            if (!some_see(r0 + 32 * rb, B0)) return;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[0][B0][e] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < Own::kSteps; ++j)
+              own.product_each(j, B0, row_piece(s_even + rb * 32 * kRowBytes, j), acc[0][B0]);
+            weigh(std::integral_constant<int, kEach>(), zero, B0, B1, r0 + 32 * rb);
+          };
+          part(zero, one);
+          if constexpr (Own::kBlocks == 2) part(one, blocks);
+        }
+        r0 += kTileRows;
+        if (++flush == kFlush) {
+          flush = 0;
+#pragma unroll
+          for (int b = 0; b < Own::kBlocks; ++b) {
+            total[b] += run[b];
+            run[b] = 0.0f;
+          }
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < Own::kBlocks; ++b) {
+        float again = total[b] + run[b];
+        again += __shfl_xor(again, 32);
+        if (!(sum[b] < -kNegInf)) sum[b] = again;  // the others stay as they are, bit for bit
+      }
+    }
   }
 #pragma unroll
   for (int b = 0; b < Own::kBlocks; ++b) {
-    float sum = total[b] + run[b];
-    sum += __shfl_xor(sum, 32);
     const int j = wave_key + 32 * b + col;
     if (hi != 0 || j >= p.nk) continue;
     if (p.splits > 1) {
-      a.part[p.part * kTileKeys + wave * kWaveKeys + 32 * b + col] = sum;
+      a.part[p.part * kTileKeys + wave * kWaveKeys + 32 * b + col] = sum[b];
     } else {
       const int64_t at = (int64_t)h * a.Tk + p.k0 + j;
-      a.mass_out[at] = j >= n ? 0.0f : a.mass != nullptr ? a.mass[at] + sum : sum;
+      a.mass_out[at] = j >= n ? 0.0f : a.mass != nullptr ? a.mass[at] + sum[b] : sum[b];
     }
   }
 }
