@@ -504,7 +504,8 @@ int twinkv_cache4_attention(const void* q, int dtype, int group, const int64_t* 
  * observation window: q, lse and cu_q of those).
  *
  *   q, k, window, n_sink, scale  as in twinkv_sink_attention.
- *   lse       [n_heads*group][T_q] fp32, as that call returns it.  A query whose lse is -inf has no weights.
+ *   lse       [n_heads*group][T_q] fp32, as that call returns it.  A query whose lse is -inf has no weights,
+ *             whatever its elements are.
  *   mass      [n_heads][T_k] fp32, added to the result (what earlier chunks gave).  Nullable.
  *   mass_out  [n_heads][T_k] fp32.  May be `mass`.
  *   workspace  twinkv_mass_workspace_bytes(...) bytes (may be NULL when that is 0).

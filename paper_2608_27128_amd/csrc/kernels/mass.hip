@@ -392,8 +392,8 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     many[b] = (unsigned)max(end - first[b], (int64_t)0);
   }
   auto seen = [&](int row, int b) { return (unsigned)(row - first[b]) < many[b]; };
-  // The weights of the block of rows from `row` on, for key blocks B0 .. B1 - 1.  (kEach: of the rows that see a key, an
-  // element at a time.)
+  // The weights of the block of rows from `row` on, for key blocks B0 .. B1 - 1.  (kEach: of the rows that see a key and
+  // whose log-sum-exp is not -inf, whatever their scores are.)
   auto weigh = [&](auto all, auto H, auto B0, auto B1, int row) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {  // rows 8x + 4hi .. + 3 of the block
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
           const float arg = __builtin_fmaf(acc[H][b][4 * x + e], scale[b], -l[H][x][e]);
           if constexpr (all == kAll) run[b] += __builtin_amdgcn_exp2f(arg);
           else if constexpr (all == kSeen) run[b] += __builtin_amdgcn_exp2f(seen(row + 4 * hi + 8 * x + e, b) ? arg : kNegInf);
-          else run[b] += seen(row + 4 * hi + 8 * x + e, b) ? __builtin_amdgcn_exp2f(arg) : 0.0f;
+          else run[b] += seen(row + 4 * hi + 8 * x + e, b) && l[H][x][e] != kNegInf ? __builtin_amdgcn_exp2f(arg) : 0.0f;
         }
     }
   };
@@ -577,9 +577,9 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
     sum[b] += __shfl_xor(sum[b], 32);
     odd |= !(sum[b] < -kNegInf);
   }
-  // Such a sum is computed once more, where fp32 elements are multiplied as they are: an infinite one is not the sum of its
-  // parts.  (The same for the workgroup.  Where there is none the check costs nothing measurable: 32768 tokens 3891 us / 3898,
-  // 8192 of d 64 185.0 / 185.4.)
+  // Such a sum is computed once more, where a row without weights counts for nothing whatever its scores are, and fp32
+  // elements are multiplied as they are: an infinite one is not the sum of its parts.  (The same for the workgroup.  Where
+  // there is none the check costs nothing measurable: 32768 tokens 3891 us / 3898, 8192 of d 64 185.0 / 185.4.)
   if (row0 < row1) {
     if (__any(odd) && lane == 0) s_odd_sum = 1;
     __syncthreads();
@@ -597,7 +597,7 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
         } else {
           bring(zero, r0);
         }
-        if (tid < kTileRows) s_lse[0][tid] = next_lse == kNegInf ? -kNegInf : next_lse * 1.44269504088896340736f;
+        if (tid < kTileRows) s_lse[0][tid] = next_lse * 1.44269504088896340736f;
         if constexpr (!kSplit) __builtin_amdgcn_s_waitcnt(kNoLoads);
         __syncthreads();
 #pragma unroll 1
