@@ -1228,6 +1228,13 @@ def cache8_attention(q, cache: Cache8, length, scale: Optional[float] = None, cu
     return res
 
 
+def _ends(n_sink: int, n_recent: int):
+    """Numbers of first and last rows as the library takes them, in 32 bits: no problem has more rows."""
+    if n_sink < 0 or n_recent < 0:
+        raise ValueError("n_sink and n_recent must not be negative")
+    return min(int(n_sink), (1 << 31) - 1), min(int(n_recent), (1 << 31) - 1)
+
+
 def cache8_evict(cache: Cache8, length, mass, budget, to: Cache8, n_sink: int = 4, n_recent: int = 64, *, pos=None,
                  len_out=None, workspace=None) -> dict:
     """Keeps of every problem's ``length`` (n_heads, n_seqs) int32 rows the ``budget`` (an int, or one per sequence)
@@ -1236,6 +1243,7 @@ def cache8_evict(cache: Cache8, length, mass, budget, to: Cache8, n_sink: int = 
     pos is what ``pos`` (n_heads, C) int32 held for the rows, or their rows in ``cache``; -1, and mass 0, on rows
     not in use.  ``len_out`` may be ``length``."""
     torch = _torch()
+    n_sink, n_recent = _ends(n_sink, n_recent)
     dev = cache.device
     if (to.n_heads, to.n_seqs, to.d, to.device) != (cache.n_heads, cache.n_seqs, cache.d, dev):
         raise ValueError("the caches must have the same heads, sequences, channels and device")
@@ -1250,7 +1258,6 @@ def cache8_evict(cache: Cache8, length, mass, budget, to: Cache8, n_sink: int = 
            "mass": torch.empty((cache.n_heads, C), dtype=torch.float32, device=dev),
            "pos": torch.empty((cache.n_heads, C), dtype=torch.int32, device=dev)}
     ws, wp, wn = _cache8_scratch(workspace, cache)
-    _launch(dev, "twinkv_cache8_evict", cache._handle, n.data_ptr(), mass.data_ptr(), _ptr(pos), keep, int(n_sink),
-            int(n_recent), to._handle, out["len"].data_ptr(), out["mass"].data_ptr(), out["pos"].data_ptr(), wp, wn,
-            _stream(dev))
+    _launch(dev, "twinkv_cache8_evict", cache._handle, n.data_ptr(), mass.data_ptr(), _ptr(pos), keep, n_sink, n_recent,
+            to._handle, out["len"].data_ptr(), out["mass"].data_ptr(), out["pos"].data_ptr(), wp, wn, _stream(dev))
     return out

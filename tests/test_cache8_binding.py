@@ -1,0 +1,66 @@
+"""The binding's own checks of the 8-bit cache's arguments, on the CPU: only the call into the library is replaced."""
+import numpy as np
+import pytest
+
+from paper_2608_27128_amd import binding
+
+
+class Lib:
+    """Takes the calls' arguments down, as ctypes would hand them over."""
+
+    def __init__(self):
+        self.sent = {}
+
+    def __getattr__(self, name):
+        if not name.startswith("twinkv_"):
+            raise AttributeError(name)
+        types = binding.SIGNATURES[name][1]
+
+        def call(*args):
+            self.sent[name] = [a if x is None else getattr(x(a), "value", a) if isinstance(a, int) else a
+                               for x, a in zip(types, args)]
+            return 0
+        return call
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    L = Lib()
+    monkeypatch.setattr(binding, "_lib", L)
+    monkeypatch.setattr(binding, "_launch", lambda dev, name, *args: getattr(L, name)(*args))
+    monkeypatch.setattr(binding, "_stream", lambda dev: None)
+    return L
+
+
+def cache(H=2, rows=64, d=64, at=None):
+    """A Cache8 of host memory (its constructor takes memory of a GPU only); `at`: its four arrays."""
+    import torch
+    C = rows // 32 * 32
+    c = object.__new__(binding.Cache8)
+    made = (torch.zeros((H, C, d), dtype=torch.int8), torch.zeros((H, C // 32), dtype=torch.uint8),
+            torch.zeros((H, C // 8, d, 8), dtype=torch.int8), torch.zeros((H, C // 32), dtype=torch.uint8))
+    c.k_codes, c.k_scales, c.v_codes, c.v_scales = made if at is None else at
+    c.cu_rows, c.n_heads, c.n_seqs, c.d, c.device = np.array([0, C]), H, 1, d, made[0].device
+    c._handle = None
+    return c
+
+
+def evict(c, to, *args, **kw):
+    import torch
+    return binding.cache8_evict(c, torch.zeros((2, 1), dtype=torch.int32), torch.zeros((2, 64)), 10, to, *args, **kw)
+
+
+@pytest.mark.parametrize("sink,recent,want", [(4, 64, (4, 64)), (0, 1 << 32, (0, 2 ** 31 - 1)), (1 << 32, 0, (2 ** 31 - 1, 0)),
+                                              ((1 << 32) + 7, 1 << 40, (2 ** 31 - 1, 2 ** 31 - 1)),
+                                              (np.int64(1 << 33), 2 ** 31 - 1, (2 ** 31 - 1, 2 ** 31 - 1))])
+def test_evict_protects_any_number_of_rows(lib, sink, recent, want):
+    """More than 32 bits of first or last rows are all of them, not what the low bits say."""
+    evict(cache(), cache(), sink, recent)
+    assert tuple(lib.sent["twinkv_cache8_evict"][5:7]) == want
+
+
+@pytest.mark.parametrize("sink,recent", [(-1, 0), (0, -1), (-(1 << 32), 4), (4, -(1 << 40))])
+def test_evict_refuses_negative_numbers_of_rows(lib, sink, recent):
+    with pytest.raises(ValueError, match="negative"):
+        evict(cache(), cache(), sink, recent)
+    assert "twinkv_cache8_evict" not in lib.sent
