@@ -609,8 +609,9 @@ int64_t twinkv_cache8_attention_workspace_bytes(int dtype, int d, int n_heads, i
  * twinkv_select_topk (the n_sink first and n_recent last rows, by row; then more weight, equal weights by row, NaN
  * after every number), moved in row order to the front of the problem's part of another cache.
  *
- *   from, to  same d, n_heads and n_seqs; no array in common.  Rows that meet in a block of `to` take the smallest
- *             scale that holds them all; their codes are rounded again only where that is larger than their own.
+ *   from, to  same d, n_heads and n_seqs; no memory in common (of which equal addresses are refused).  Rows that
+ *             meet in a block of `to` take the smallest scale that holds them all; their codes are rounded again only
+ *             where that is larger than their own.
  *   len       [n_heads * n_seqs] int32 rows of `from` in use (taken as at least 0 and at most the problem's rows).
  *   mass      [n_heads][C of from] fp32, 16-byte aligned.
  *   pos       [n_heads][C of from] int32, any number kept beside a row (its token's position).  Nullable.

@@ -1099,6 +1099,7 @@ class Cache8:
             raise ValueError("the cache must be on a GPU")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self.cu_rows, self.n_heads, self.n_seqs, self.d, self.device = cu, H, cu.size - 1, d, dev
+        self._spans = _spans(k_codes, k_scales, v_codes, v_scales)
         self._cu = (ctypes.c_int64 * cu.size).from_buffer(cu)
         self._struct = _Cache8Struct(d, H, cu.size - 1, ctypes.cast(self._cu, _PI64), k_codes.data_ptr(),
                                      k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
@@ -1235,18 +1236,35 @@ def _ends(n_sink: int, n_recent: int):
     return min(int(n_sink), (1 << 31) - 1), min(int(n_recent), (1 << 31) - 1)
 
 
+def _spans(*arrays):
+    """The bytes that tensors take, (first, past the last) each."""
+    return [(x.data_ptr(), x.data_ptr() + _nbytes(x)) for x in arrays if x.numel() > 0]
+
+
+def _apart(spans) -> bool:
+    """Whether no two of the spans have a byte in common."""
+    end = 0
+    for x in sorted(spans):
+        if x[0] < end:
+            return False
+        end = x[1]
+    return True
+
+
 def cache8_evict(cache: Cache8, length, mass, budget, to: Cache8, n_sink: int = 4, n_recent: int = 64, *, pos=None,
                  len_out=None, workspace=None) -> dict:
     """Keeps of every problem's ``length`` (n_heads, n_seqs) int32 rows the ``budget`` (an int, or one per sequence)
     that ``select_topk`` would: the first ``n_sink`` and last ``n_recent``, then those of most ``mass`` (n_heads, C)
-    float32.  They move, in row order, to the front of another cache ``to``.  Returns len, mass and pos of ``to``:
-    pos is what ``pos`` (n_heads, C) int32 held for the rows, or their rows in ``cache``; -1, and mass 0, on rows
-    not in use.  ``len_out`` may be ``length``."""
+    float32.  They move, in row order, to the front of another cache ``to``, which shares no memory with this one.
+    Returns len, mass and pos of ``to``: pos is what ``pos`` (n_heads, C) int32 held for the rows, or their rows in
+    ``cache``; -1, and mass 0, on rows not in use.  ``len_out`` may be ``length``."""
     torch = _torch()
     n_sink, n_recent = _ends(n_sink, n_recent)
     dev = cache.device
     if (to.n_heads, to.n_seqs, to.d, to.device) != (cache.n_heads, cache.n_seqs, cache.d, dev):
         raise ValueError("the caches must have the same heads, sequences, channels and device")
+    if not _apart(cache._spans + to._spans):
+        raise ValueError("the caches must not overlap")
     n = cache._lens(length, "length")
     if mass is None:
         raise ValueError("mass is required")

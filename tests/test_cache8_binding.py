@@ -41,7 +41,7 @@ def cache(H=2, rows=64, d=64, at=None):
             torch.zeros((H, C // 8, d, 8), dtype=torch.int8), torch.zeros((H, C // 32), dtype=torch.uint8))
     c.k_codes, c.k_scales, c.v_codes, c.v_scales = made if at is None else at
     c.cu_rows, c.n_heads, c.n_seqs, c.d, c.device = np.array([0, C]), H, 1, d, made[0].device
-    c._handle = None
+    c._handle, c._spans = None, binding._spans(c.k_codes, c.k_scales, c.v_codes, c.v_scales)
     return c
 
 
@@ -64,3 +64,43 @@ def test_evict_refuses_negative_numbers_of_rows(lib, sink, recent):
     with pytest.raises(ValueError, match="negative"):
         evict(cache(), cache(), sink, recent)
     assert "twinkv_cache8_evict" not in lib.sent
+
+
+def test_evict_refuses_caches_that_overlap(lib):
+    """Arrays of the two caches in one buffer: from every start, against their bytes listed one by one."""
+    import torch
+    H, rows, d = 2, 64, 64
+    codes, scales = H * rows * d, H * rows // 32
+    buf = torch.zeros(8 * codes, dtype=torch.int8)
+
+    def placed(k, v, s):
+        """Codes at k and v, scales at s and behind them."""
+        u8 = buf.view(torch.uint8)
+        return cache(H, rows, d, (buf[k:k + codes].view(H, rows, d), u8[s:s + scales].view(H, -1),
+                                  buf[v:v + codes].view(H, rows // 8, d, 8), u8[s + scales:s + 2 * scales].view(H, -1)))
+    a = placed(codes, 3 * codes, 5 * codes)
+    mine = [(codes, 2 * codes), (3 * codes, 4 * codes), (5 * codes, 5 * codes + 2 * scales)]
+    refused = kept = 0
+    starts = sorted({x + y for x in (0, codes, 2 * codes, 3 * codes, 4 * codes) for y in (-codes, -1, 0, 1, codes // 2)})
+    for k in starts:
+        for v in (6 * codes, 2 * codes + 5):
+            for s in (7 * codes, 5 * codes - scales, 5 * codes + scales, 5 * codes + 2 * scales, 5 * codes - 2 * scales):
+                if k < 0:
+                    continue
+                b = placed(k, v, s)
+                spans = mine + [(k, k + codes), (v, v + codes), (s, s + 2 * scales)]
+                taken = np.zeros(len(buf), dtype=np.int32)
+                for x, y in spans:
+                    taken[x:y] += 1
+                if taken.max() > 1:
+                    refused += 1
+                    for pair in ((a, b), (b, a)):
+                        with pytest.raises(ValueError, match="overlap"):
+                            evict(*pair)
+                else:
+                    kept += 1
+                    evict(a, b)
+    assert refused > 20 and kept > 5
+    with pytest.raises(ValueError, match="overlap"):
+        evict(a, a)
+    assert cache(2, 0, 64)._spans == []  # no rows: nothing to share
