@@ -1132,8 +1132,9 @@ def cache8_compact(keys, values, retained, cache: Cache8, cu_seqlens=None, *, to
     become the first rows of its part of ``cache``.  Returns len (n_heads, n_seqs) int32, pos (n_heads, C) int32 (-1
     on rows not in use) and status (n_heads, n_seqs) int32; a problem that keeps more than its rows stores nothing
     (PROBLEM_BUDGET_MISMATCH, len 0).  With ``token_mass`` (n_heads, T) float32 also mass (n_heads, C), the cached
-    rows' weights."""
+    rows' weights.  There is no gradient: inputs that require one are refused (torch.no_grad() lifts that)."""
     torch = _torch()
+    _no_gradient("cache8_compact", keys, values, token_mass)
     keys, values, dt = _cache_rows(keys, values, cache)
     H, T, _ = keys.shape
     dev, C = cache.device, int(cache.cu_rows[-1])
@@ -1158,8 +1159,10 @@ def cache8_append(keys, values, cache: Cache8, length, cu_new=None, *, len_out=N
     """The keys and values (n_heads, T, d) of new tokens, [cu_new[s], cu_new[s + 1]) of sequence s, as the rows after
     the ``length`` (n_heads, n_seqs) int32 ones in use.  Returns len (``len_out`` if given, which may be ``length``
     itself) and status; a problem whose new tokens do not fit stays as it is.  Where a row needs a larger scale
-    than its block of 32 has, the block's rows are rounded once more."""
+    than its block of 32 has, the block's rows are rounded once more.  There is no gradient: inputs that require one
+    are refused (torch.no_grad() lifts that)."""
     torch = _torch()
+    _no_gradient("cache8_append", keys, values)
     keys, values, dt = _cache_rows(keys, values, cache)
     dev = cache.device
     cu = cache._offsets(cu_new, keys.shape[1], "cu_new")
@@ -1257,8 +1260,10 @@ def cache8_evict(cache: Cache8, length, mass, budget, to: Cache8, n_sink: int = 
     that ``select_topk`` would: the first ``n_sink`` and last ``n_recent``, then those of most ``mass`` (n_heads, C)
     float32.  They move, in row order, to the front of another cache ``to``, which shares no memory with this one.
     Returns len, mass and pos of ``to``: pos is what ``pos`` (n_heads, C) int32 held for the rows, or their rows in
-    ``cache``; -1, and mass 0, on rows not in use.  ``len_out`` may be ``length``."""
+    ``cache``; -1, and mass 0, on rows not in use.  ``len_out`` may be ``length``.  There is no gradient: a mass that
+    requires one is refused (torch.no_grad() lifts that)."""
     torch = _torch()
+    _no_gradient("cache8_evict", mass)
     n_sink, n_recent = _ends(n_sink, n_recent)
     dev = cache.device
     if (to.n_heads, to.n_seqs, to.d, to.device) != (cache.n_heads, cache.n_seqs, cache.d, dev):

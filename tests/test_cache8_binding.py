@@ -104,3 +104,22 @@ def test_evict_refuses_caches_that_overlap(lib):
     with pytest.raises(ValueError, match="overlap"):
         evict(a, a)
     assert cache(2, 0, 64)._spans == []  # no rows: nothing to share
+
+
+def test_binding_refuses_inputs_that_require_a_gradient(lib):
+    """The calls that fill a cache or move its weights, whose gradient would be lost without a word; under no_grad they
+    go on."""
+    import torch
+    c, to = cache(), cache()
+    x = torch.zeros((2, 32, 64), dtype=torch.bfloat16)
+    y, m = x.clone().requires_grad_(), torch.zeros((2, 32), requires_grad=True)
+    ones, n = torch.ones((2, 32), dtype=torch.uint8), torch.zeros((2, 1), dtype=torch.int32)
+    w = torch.zeros((2, 64), requires_grad=True)
+    for call in (lambda: binding.cache8_compact(y, x, ones, c), lambda: binding.cache8_compact(x, y, ones, c),
+                 lambda: binding.cache8_compact(x, x, ones, c, token_mass=m), lambda: binding.cache8_append(y, x, c, n),
+                 lambda: binding.cache8_append(x, y, c, n), lambda: binding.cache8_evict(c, n, w, 10, to)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    with torch.no_grad():
+        binding.cache8_evict(c, n, w, 10, to)
+    assert "twinkv_cache8_evict" in lib.sent and "twinkv_cache8_append" not in lib.sent
