@@ -180,6 +180,81 @@ struct MassArgs {
   bool few;                // rows see a tile (bf16)
   float* part;             // nullable [n_heads][items][keys], where a tile has more than one split
 };
+// The place of a sequence's item `left`: its tile, split, the splits of that tile, and its place among the parts, which
+// lie tile by tile, a tile's splits side by side.  kByRows: items come in the order of the rows, many tiles and the same
+// rows together; otherwise in the order of the parts.  (constexpr: for the host and the device.)
+struct MassPlace {
+  int tile, split, splits, part;
+};
+template <bool kByRows>
+constexpr MassPlace mass_place(int left, int splits, int full, int shape, int tiles) {
+  const int kind = shape >> kMassShapeBits, by = shape & ((1 << kMassShapeBits) - 1);
+  MassPlace p = {0, 0, splits, left};
+  if (kind == kMassRest) {  // `full` tiles of `splits` splits, the others of `by`
+    if (left >= full * splits) {
+      left -= full * splits;
+      p.splits = by;
+      p.tile = full + left / by;
+      p.split = left % by;
+    } else if (kByRows) {
+      p.tile = left % full;
+      p.split = left / full;
+      p.part = p.tile * splits + p.split;
+    } else {
+      p.tile = left / splits;
+      p.split = left % splits;
+    }
+    return p;
+  }
+  // `full` tiles of `splits` splits, then runs of tiles, each run of `drop` splits less, the last ones of `least`
+  const int run = kind == kMassRuns ? by : 1, drop = kind == kMassRuns ? 1 : by;
+  if (!kByRows) {
+    int tile0 = 0;
+    if (left >= full * splits) {
+      left -= full * splits;
+      tile0 = full;
+      while (p.splits > drop && left >= run * p.splits) {
+        left -= run * p.splits;
+        tile0 += run;
+        p.splits -= drop;
+      }
+    }
+    p.tile = tile0 + left / p.splits;
+    p.split = left % p.splits;
+    return p;
+  }
+  // Split i of run g begins about where split i + g drop of the full tiles does: level by level of those.
+  const int runs = (splits + drop - 1) / drop, least = splits - (runs - 1) * drop;
+  int level = 0, here = tiles < full + run ? tiles : full + run;  // tiles that have a split at this level
+  while (level < splits) {
+    const int n = (drop < splits - level ? drop : splits - level) * here;
+    if (left < n) break;
+    left -= n;
+    level += drop;
+    here = tiles < here + run ? tiles : here + run;
+  }
+  int g = 0;
+  if (level < splits) {
+    p.tile = left % here;
+    p.split = level + left / here;
+    if (p.tile >= full) {
+      g = (p.tile - full) / run;
+      p.splits = splits - g * drop;
+      p.split -= g * drop;
+    }
+  } else {
+    p.splits = least;
+    p.tile = full + run * runs + left / least;
+    p.split = left % least;
+    g = (p.tile - full) / run;
+  }
+  const int m = g < runs ? g : runs;
+  p.part = p.tile < full ? p.tile * splits
+                         : full * splits + run * (m * splits - drop * (m * (m - 1) / 2) + (g - m) * least) +
+                               (p.tile - full - run * g) * p.splits;
+  p.part += p.split;
+  return p;
+}
 int launch_mass(const MassArgs& a, int dtype, int d, void* stream);
 int launch_mass_join(const MassArgs& a, void* stream);
 

@@ -118,9 +118,8 @@ struct Keys<float, D, 1, P> {
   }
 };
 
-// What an item is.  Parts lie tile by tile, a tile's splits side by side; kByRows: the items at work together are those of
-// many tiles and the same rows, which one XCD's L2 then holds (a prompt of 32768 tokens reads
-// 1.4 GB instead of 12.9; one of 4096 in fp32 takes 388 us for 421).
+// What an item is.  kByRows (mass_place): the items at work together are those of many tiles and the same rows, which one
+// XCD's L2 then holds (a prompt of 32768 tokens reads 1.4 GB instead of 12.9; one of 4096 in fp32 takes 388 us for 421).
 struct MassItem {
   int h, s, kt, split, splits;
   int q0, nq, k0, nk;
@@ -138,74 +137,13 @@ __device__ inline MassItem mass_item(const MassArgs& a, int item, int h) {
   const int item0 = seq_word(a.seq, w + 2), splits = seq_word(a.seq, w + 3);
   p.rows = seq_word(a.seq, w + 4);
   const int full = seq_word(a.seq, w + 5), shape = seq_word(a.seq, w + 6);
-  const int kind = shape >> kMassShapeBits, by = shape & ((1 << kMassShapeBits) - 1);
   p.nq = seq_word(a.seq, w + kMassSeqWords) - p.q0;
   p.nk = seq_word(a.seq, w + kMassSeqWords + 1) - p.k0;
-  int left = item - item0, at = left;  // the place among the items not looked at yet, and among the parts
-  p.splits = splits;
-  if (kind == kMassRest) {  // `full` tiles of `splits` splits, the others of `by`
-    if (left >= full * splits) {
-      left -= full * splits;
-      p.splits = by;
-      p.kt = full + left / by;
-      p.split = left % by;
-    } else if (kByRows) {
-      p.kt = left % full;
-      p.split = left / full;
-      at = p.kt * splits + p.split;
-    } else {
-      p.kt = left / splits;
-      p.split = left % splits;
-    }
-  } else {  // `full` tiles of `splits` splits, then runs of tiles, each run of `drop` splits less, the last ones of `least`
-    const int run = kind == kMassRuns ? by : 1, drop = kind == kMassRuns ? 1 : by;
-    if (kByRows) {
-      // Split i of run g begins about where split i + g drop of the full tiles does: level by level of those.
-      const int tiles = (p.nk + a.keys - 1) / a.keys, runs = (splits + drop - 1) / drop, least = splits - (runs - 1) * drop;
-      int level = 0, here = min(tiles, full + run);  // tiles that have a split at this level
-      while (level < splits) {
-        const int n = min(drop, splits - level) * here;
-        if (left < n) break;
-        left -= n;
-        level += drop;
-        here = min(tiles, here + run);
-      }
-      int g = 0;
-      if (level < splits) {
-        p.kt = left % here;
-        p.split = level + left / here;
-        if (p.kt >= full) {
-          g = (p.kt - full) / run;
-          p.splits = splits - g * drop;
-          p.split -= g * drop;
-        }
-      } else {
-        p.splits = least;
-        p.kt = full + run * runs + left / least;
-        p.split = left % least;
-        g = (p.kt - full) / run;
-      }
-      const int m = min(g, runs);
-      at = p.kt < full ? p.kt * splits
-                       : full * splits + run * (m * splits - drop * (m * (m - 1) / 2) + (g - m) * least) +
-                             (p.kt - full - run * g) * p.splits;
-      at += p.split;
-    } else {
-      int tile0 = 0;
-      if (left >= full * splits) {
-        left -= full * splits;
-        tile0 = full;
-        while (p.splits > drop && left >= run * p.splits) {
-          left -= run * p.splits;
-          tile0 += run;
-          p.splits -= drop;
-        }
-      }
-      p.kt = tile0 + left / p.splits;
-      p.split = left % p.splits;
-    }
-  }
-  p.part = (int64_t)h * a.items + item0 + at;
+  const MassPlace place = mass_place<kByRows>(item - item0, splits, full, shape, (p.nk + a.keys - 1) / a.keys);
+  p.kt = place.tile;
+  p.split = place.split;
+  p.splits = place.splits;
+  p.part = (int64_t)h * a.items + item0 + place.part;
   return p;
 }
 

@@ -1,5 +1,6 @@
 """More of the host layer of the 8-bit cache under AddressSanitizer and UndefinedBehaviorSanitizer, on the CPU, built
-with g++ (host code only), no GPU needed: which kernels the attention starts (tests/host/cache8_plans_test.cpp)."""
+with g++ (host code only), no GPU needed: which kernels the attention starts (tests/host/cache8_plans_test.cpp), and the
+places of the accumulated weights' items (tests/host/mass_places_test.cpp)."""
 import os
 import shutil
 import subprocess
@@ -29,3 +30,7 @@ def run_host(tmp_path, name, sources, said):
 
 def test_attention_starts_a_kernel_that_gives_its_weights(tmp_path):
     run_host(tmp_path, "cache8_plans_test", ["cache8_ops.cpp"], "cache8 plans ok")
+
+
+def test_every_split_of_the_weights_once(tmp_path):
+    run_host(tmp_path, "mass_places_test", ["cache8_ops.cpp"], "mass places ok")
