@@ -584,7 +584,8 @@ int twinkv_cache8_read(const twinkv_cache8* cache, const int32_t* len, const int
                        int64_t workspace_bytes, void* stream);
 
 /*
- * Attention over an 8-bit cache; q, len, scale, out and lse as in twinkv_cache4_attention, and
+ * Attention over an 8-bit cache; q, len, scale, out and lse as in twinkv_cache4_attention (with mass_out, out may not
+ * be q: the weights are computed from it, for more than 16 rows a problem after out is written), and
  *   mass      [n_heads][C] fp32, 16-byte aligned: accumulated weights of the rows in use.  Nullable (0).
  *   mass_out  [n_heads][C] fp32, 16-byte aligned: with the weights of this call's queries added (sum over the queries that see the
  *             row and the head's query heads); 0 on rows not in use, so that rows appended later begin with 0.

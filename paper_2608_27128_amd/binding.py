@@ -1205,8 +1205,8 @@ def cache8_attention(q, cache: Cache8, length, scale: Optional[float] = None, cu
     ``length`` (n_heads, n_seqs) int32 rows in use, as ``cache4_attention`` computes it.  Returns out, with
     ``want_lse`` lse (Hq, Tq) float32, and with ``want_mass``, ``mass`` or ``mass_out`` mass (n_heads, C) float32:
     the rows' weights so far (``mass``; None: 0) and those of this call's queries, 0 on rows not in use.
-    ``mass_out`` may be ``mass``.  There is no gradient: a q that requires one is refused (torch.no_grad() lifts
-    that)."""
+    ``mass_out`` may be ``mass``; where weights are wanted ``out`` may not be q, which they are computed from.  There is
+    no gradient: a q that requires one is refused (torch.no_grad() lifts that)."""
     torch = _torch()
     _no_gradient("cache8_attention", q, mass, mass_out, out)
     dev = cache.device
@@ -1217,6 +1217,8 @@ def cache8_attention(q, cache: Cache8, length, scale: Optional[float] = None, cu
     n = cache._lens(length, "length")
     want_mass = want_mass or mass is not None or mass_out is not None
     mass = cache._weights(mass, "mass")
+    if want_mass and out is not None and out.data_ptr() == q.data_ptr() and q.numel() > 0:
+        raise ValueError("out may not be q where weights are wanted")
     res = {"out": _out_rows(out, (Hq, Tq, d), q, "out")}
     if want_lse:
         res["lse"] = torch.empty((Hq, Tq), dtype=torch.float32, device=dev)

@@ -102,3 +102,21 @@ def test_weights_of_a_nan_query_reach_the_keys_that_it_sees(rows, nq, G, dtype, 
         seen = int(length[h, 0]) - (nq - 1 - first)  # keys that the query sees
         assert bool(torch.isnan(got["mass"][h, :seen]).all())
         assert torch.equal(got["mass"][h, seen:], clean["mass"][h, seen:]) and bool(clean["mass"][h, seen] > 0)
+
+
+@pytest.mark.parametrize("nq", [1, 9])
+def test_outputs_in_the_queries_place(nq):
+    """Refused where weights are wanted, which come from the queries after the output is written (36 rows a problem);
+    without weights a tile of rows reads its queries before it writes."""
+    import torch
+    g = gen(nq)
+    cache, length, _, _ = filled(g, 2, [3000], 128)
+    q = randn(g, 8, nq, 128)
+    want = binding.cache8_attention(q, cache, length, None, [0, nq])["out"].clone()
+    old = torch.zeros((2, int(cache.cu_rows[-1])), device="cuda")
+    for kw in (dict(want_mass=True), dict(mass=old), dict(mass_out=old)):
+        same = q.clone()
+        with pytest.raises(ValueError, match="may not be q"):
+            binding.cache8_attention(same, cache, length, None, [0, nq], out=same, **kw)
+        assert torch.equal(same, q)
+    assert torch.equal(binding.cache8_attention(same, cache, length, None, [0, nq], out=same)["out"], want)
