@@ -269,9 +269,11 @@ inline int64_t live_of(int n_seqs, const int64_t* cu_q) {  // sequences with que
   return n;
 }
 
-// 4 bits, bf16: with so much work (as above) and more than a row tile in the mean a wave takes two row tiles at
-// once.  One / two, us, 8 heads of 8, d 128: 3 queries over 32k rows 25 / 28, over 128k 58 / 50, over 64 caches of 4k 94 /
-// 72; 7 queries over 32k 34 / 36, over 64 caches of 4k 182 / 143.
+// A cache, bf16: with so much work (as above) and more than a row tile in the mean a wave takes two row tiles at
+// once.  4 bits, one / two, us, 8 heads of 8, d 128: 3 queries over 32k rows 25 / 28, over 128k 58 / 50, over 64 caches of 4k 94 /
+// 72; 7 queries over 32k 34 / 36, over 64 caches of 4k 182 / 143.  8 bits, joins included: 3 queries over 128k rows 63 / 55,
+// over 64 caches of 4k 154 / 101, 7 over these 303 / 162, 17 rows of one query head 154 / 100; d 64, 3 queries over 128k
+// 41 / 38, over 64 caches of 4k 83 / 53.
 constexpr int64_t kPairWork = 49152;
 
 // fp32: the kernel for many rows takes four row tiles a workgroup and does not split their keys, so it is taken where

@@ -83,7 +83,7 @@ constexpr int kAttnMostLds = 70 * 1024;
 constexpr int kAttnSeqWords = 6;
 constexpr int kAttnTile = 32;        // keys of a tile
 constexpr int kAttnRows = 16;        // rows of a tile
-constexpr int kAttnPairRows = 32;    // of an item whose waves take two row tiles at once (4 bits)
+constexpr int kAttnPairRows = 32;    // of an item whose waves take two row tiles at once (a cache, bf16)
 constexpr int kAttnWideRows = 64;    // of an item whose four waves take a tile each
 constexpr int kAttnBigRows = 128;    // rows and keys of the kernel for many rows
 constexpr int kAttnBigTile = 64;
@@ -95,8 +95,8 @@ struct AttnArgs {
   const char* v;
   char* out;
   int64_t q_head, q_token, k_head, k_token, v_head, v_token, o_head, o_token;  // bytes
-  Cache4 cache;          // k, v null: keys and values in 4 bits
-  const int32_t* len;    // [n_heads * n_seqs] rows in use (4 bits)
+  Cache4 cache;          // k, v null: keys and values in 4 or 8 bits
+  const int32_t* len;    // [n_heads * n_seqs] rows in use (of a cache)
   float* lse;            // nullable
   int64_t Tq;            // queries per head of lse
   float scale_log2;      // scale * log2(e)

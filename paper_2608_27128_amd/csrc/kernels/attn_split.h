@@ -1,5 +1,6 @@
-// What the two attention kernels that split a problem's keys share (over rows of keys and values, and
-// over the 4-bit cache).
+// What the kernels share that split a problem's keys: attention over rows of keys and values and over the caches in 4
+// and 8 bits, whose join is one (attn4.hip), and the accumulated weights of the 8-bit cache's rows.  (The accumulated
+// weights of rows take the loads to LDS and the infinity from here.)
 //
 // A row is one query of one query head; 16 rows make a tile.  Scores come as K q^T, so a lane holds one
 // row (lane % 16) and, of a tile of 32 keys, the 8 that its lane group g = lane / 16 owns; the product

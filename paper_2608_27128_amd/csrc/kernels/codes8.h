@@ -16,24 +16,5 @@ __device__ inline bf16x8 codes8_bf16(unsigned lo, unsigned hi) {
   const u32x2 a = codes4_bf16(lo), b = codes4_bf16(hi);
   return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
 }
-__device__ inline f32x4 codes4_f32(unsigned w) {
-  return f32x4{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24)};
-}
-
-// x as a sum of N bf16, the largest first.
-template <int N>
-__device__ inline void split8(const float (&x)[8], bf16x8 (&p)[N]) {
-  float r[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = x[e];
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[n][e] = (bf16)r[e];
-      r[e] -= (float)p[n][e];
-    }
-  }
-}
 
 }  // namespace twinkv

@@ -133,7 +133,9 @@ int launch_evict8_select(const Evict8Args& a, void* stream) {
   if (a.max_rows <= 512) return run<128, 512>(a, s);
   if (a.max_rows <= 2048) return run<256, 2048>(a, s);
   if (a.max_rows <= 4096) return run<512, 4096>(a, s);
-  // (more problems than CUs: 512 of 8000 rows 25 us, with 1024 threads 34; fewer, 8 of them 15, with 512 threads 17)
+  // (more problems than CUs: 512 of 8000 rows 25 us, with 1024 threads 34; fewer, with 512 threads in brackets: 8 of 4224
+  // rows 12.5 (14.1), of 6000 13.2 (14.8), of 8192 14.8 (16.6); 64 of 5000 14.6 (16.6); 256 of 4224 16.0 (17.9), of 8192 20.5
+  // (22.3))
   if (a.max_rows <= 8192 && a.n_heads * (int64_t)a.n_seqs > 256) return run<512, 8192>(a, s);
   if (a.max_rows <= 16384) return run<1024, 16384>(a, s);
   if (a.max_rows <= 32768) return run<1024, 32768>(a, s);

@@ -19,7 +19,7 @@
 // What bounds it at length is the matrix unit and the vector unit by turns: they hardly overlap from wave to wave, and a
 // weight costs a multiply-add, an addition and an exponential of twice their price.  So, per block of 32 rows:
 //  * kFused (bf16, d 128): one block's weights go between the next block's products, in the same wave.  A prompt of 32768
-//    tokens (8 heads of 4): 4.1 ms, 1070 TFLOP/s; apart 4.5.  Two blocks' accumulators: 233 registers, 2 waves a SIMD.
+//    tokens (8 heads of 4): 4.1 ms, 1070 TFLOP/s; apart 4.5.  Two blocks' accumulators: 244 registers, 2 waves a SIMD.
 //  * kApart (bf16 of d 64, fp32): products, then weights.  With half the products to hide behind, twice the waves count for
 //    more: 8192 tokens of d 64 190 us, fused 217.
 //  * kFew (bf16, at most kMassFew rows a key): the keys' way to the registers is the work, so one buffer of rows, and more
@@ -517,7 +517,9 @@ __global__ __launch_bounds__(kThreads, (kMassWaves<T, D, kMode>)) void mass_kern
   }
   // Such a sum is computed once more, where a row without weights counts for nothing whatever its scores are, and fp32
   // elements are multiplied as they are: an infinite one is not the sum of its parts.  (The same for the workgroup.  Where
-  // there is none the check costs nothing measurable: 32768 tokens 3891 us / 3898, 8192 of d 64 185.0 / 185.4.)
+  // there is none the check costs nothing measurable at length, 32768 tokens 3891 us / 3898, 8192 of d 64 185.0 / 185.4, and a
+  // barrier in short items: 56 rows over 64 caches of 4096 75.8 / 76.7.  Where the last query of 4096 is NaN a call takes 146
+  // us for 95, d 64 115 for 65, fp32 520 for 385.)
   if (row0 < row1) {
     if (__any(odd) && lane == 0) s_odd_sum = 1;
     __syncthreads();

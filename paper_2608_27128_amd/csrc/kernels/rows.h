@@ -72,4 +72,20 @@ struct Vec8<float> {
   }
 };
 
+// x as a sum of N bf16, the largest first.
+template <int N>
+__device__ inline void split8(const float (&x)[8], bf16x8 (&p)[N]) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[n][e] = (bf16)r[e];
+      r[e] -= (float)p[n][e];
+    }
+  }
+}
+
 }  // namespace twinkv
