@@ -593,7 +593,8 @@ int twinkv_cache8_read(const twinkv_cache8* cache, const int32_t* len, const int
  *   workspace  twinkv_cache8_attention_workspace_bytes(...) bytes (may be NULL when that is 0).
  * The products are exact in the cached values; scores, the running maximum and sums are fp32.  For bf16 the
  * weights, times the scale of their values, are rounded to bf16 (to nearest) for the product; for fp32 they keep
- * 24 bits.  mass adds weights that are not rounded.
+ * 24 bits.  (Weights are relative to a row's maximum, within 2^8, and divided by their sum at the end: values beyond 2^88
+ * may overflow, and below 2^-100 lose bits.)  mass adds weights that are not rounded.
  */
 int twinkv_cache8_attention(const void* q, int dtype, int group, const int64_t* cu_q, int64_t q_head_stride,
                             int64_t q_token_stride, const twinkv_cache8* cache, const int32_t* len, float scale,

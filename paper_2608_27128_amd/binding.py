@@ -1099,10 +1099,10 @@ class Cache8:
             raise ValueError("the cache must be on a GPU")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self.cu_rows, self.n_heads, self.n_seqs, self.d, self.device = cu, H, cu.size - 1, d, dev
-        self._spans = _spans(k_codes, k_scales, v_codes, v_scales)
         self._cu = (ctypes.c_int64 * cu.size).from_buffer(cu)
-        self._struct = _Cache8Struct(d, H, cu.size - 1, ctypes.cast(self._cu, _PI64), k_codes.data_ptr(),
-                                     k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
+        self._scales = H * (C // 32)
+        self._at = (k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
+        self._struct = _Cache8Struct(d, H, cu.size - 1, ctypes.cast(self._cu, _PI64), *self._at)
         self._handle = ctypes.addressof(self._struct)
 
     @classmethod
@@ -1117,6 +1117,13 @@ class Cache8:
 
     _lens = Cache4._lens
     _offsets = Cache4._offsets
+
+    def _spans(self) -> list:
+        """The bytes of the four arrays, (first, past the last) each."""
+        k, ks, v, vs = self._at
+        scales = self._scales
+        codes = 32 * scales * self.d
+        return [(k, k + codes), (ks, ks + scales), (v, v + codes), (vs, vs + scales)] if scales > 0 else []
 
     def _weights(self, x, name: str):
         return _small(x, (self.n_heads, int(self.cu_rows[-1])), _torch().float32, self.device, name)
@@ -1241,11 +1248,6 @@ def _ends(n_sink: int, n_recent: int):
     return min(int(n_sink), (1 << 31) - 1), min(int(n_recent), (1 << 31) - 1)
 
 
-def _spans(*arrays):
-    """The bytes that tensors take, (first, past the last) each."""
-    return [(x.data_ptr(), x.data_ptr() + _nbytes(x)) for x in arrays if x.numel() > 0]
-
-
 def _apart(spans) -> bool:
     """Whether no two of the spans have a byte in common."""
     end = 0
@@ -1270,7 +1272,7 @@ def cache8_evict(cache: Cache8, length, mass, budget, to: Cache8, n_sink: int = 
     dev = cache.device
     if (to.n_heads, to.n_seqs, to.d, to.device) != (cache.n_heads, cache.n_seqs, cache.d, dev):
         raise ValueError("the caches must have the same heads, sequences, channels and device")
-    if not _apart(cache._spans + to._spans):
+    if not _apart(cache._spans() + to._spans()):
         raise ValueError("the caches must not overlap")
     n = cache._lens(length, "length")
     if mass is None:

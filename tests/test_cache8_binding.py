@@ -41,7 +41,8 @@ def cache(H=2, rows=64, d=64, at=None):
             torch.zeros((H, C // 8, d, 8), dtype=torch.int8), torch.zeros((H, C // 32), dtype=torch.uint8))
     c.k_codes, c.k_scales, c.v_codes, c.v_scales = made if at is None else at
     c.cu_rows, c.n_heads, c.n_seqs, c.d, c.device = np.array([0, C]), H, 1, d, made[0].device
-    c._handle, c._spans = None, binding._spans(c.k_codes, c.k_scales, c.v_codes, c.v_scales)
+    c._handle, c._scales = None, H * (C // 32)
+    c._at = tuple(x.data_ptr() for x in (c.k_codes, c.k_scales, c.v_codes, c.v_scales))
     return c
 
 
@@ -103,7 +104,7 @@ def test_evict_refuses_caches_that_overlap(lib):
     assert refused > 20 and kept > 5
     with pytest.raises(ValueError, match="overlap"):
         evict(a, a)
-    assert cache(2, 0, 64)._spans == []  # no rows: nothing to share
+    assert cache(2, 0, 64)._spans() == []  # no rows: nothing to share
 
 
 def test_binding_refuses_inputs_that_require_a_gradient(lib):
